@@ -104,7 +104,7 @@ def draw(rng):
             return dict(c, b=b, lq=lq, lk=lk, ragged=rng.random() < 0.7, packed=False, grad=False)
         pairs = 16 * 16384 * 3500  # of the largest listed case
         l = min(_log_int(rng, 33, 12000), math.isqrt(2 * pairs // heads))
-        b = max(1, min(_log_int(rng, 1, 32), pairs // (heads * l * min(l // 2, (window or l) + sinks)), 100_000_000 // (l * heads * hd)))
+        b = max(1, min(_log_int(rng, 1, 32), pairs // (heads * l * min(l // 2, (window or l) + sinks)), 85_000_000 // (l * heads * hd)))
         return dict(c, b=b, lq=l, lk=l, ragged=False, packed=heads == kv and rng.random() < 0.6, grad=rng.random() < 0.75)
     V = _log_int(rng, 500, 131072)
     dtype = rng.choice(("bf16", "bf16", "f32"))
