@@ -13,8 +13,9 @@ The saved activations of one block are then exactly Table 7's list:
     x1, rstd1 | x2 (baseline) or z_q, z_k, z_v | q, k, v, two b x h x l
     buffers, x3 (shared by o) | x5, rstd2 | x6 or z_gate, z_up | x_gate, x_up
     (one storage), x_act | x7 or z_down
-and block_saved_bytes() gives that sum.  Rotary embeddings are left out: they
-save no activations and do not touch the linear layers.
+and block_saved_bytes() gives that sum.  Rotary positions (rope=Rotary(...)) turn q and k
+where they stand and save nothing; a window with sinks takes the place of the library's
+attention and saves the same list without its two scalars.
 """
 from __future__ import annotations
 
@@ -23,6 +24,7 @@ from torch.nn.modules import module as _module
 from torch.nn.attention import SDPBackend, sdpa_kernel
 
 from . import _block_ops as ops
+from .functional import distill_loss, rotary_split_qkv, window_attention
 from .nn import CompActAdam, CompActGroup, CompActLinear
 
 __all__ = ["RMSNorm", "DenseLinear", "LlamaBlock", "LlamaModel", "block_saved_bytes", "make_optimizers"]
@@ -107,11 +109,16 @@ class LlamaBlock(torch.nn.Module):
     the d-input layers (q, k, v, gate, up) and rank_down that of down
     (default ffn * rank / d); None for the uncompressed baseline.  compress_o
     also makes the attention output projection a CompAct layer (which saves
-    memory only where attention does not keep its output)."""
+    memory only where attention does not keep its output).  rope: a Rotary that
+    turns q and k; window, sinks: attention over the last `window` tokens and the
+    first `sinks` ones (window_attention)."""
 
     def __init__(self, d, heads, ffn, rank=None, rank_down=None, seeds=None, alpha=1.0,
-                 compress_o=False, device="cuda", weights=None, proj="gaussian"):
+                 compress_o=False, device="cuda", weights=None, proj="gaussian", rope=None, window=None, sinks=0):
         super().__init__()
+        if rope is not None and rope.dims > d // heads:
+            raise ValueError(f"rotary: {rope.dims} dims of heads of {d // heads}")
+        self.rope, self.window, self.sinks = rope, window, sinks
         self.d, self.heads, self.ffn = d, heads, ffn
         self.rank = rank
         self.rank_down = (rank_down or max(1, ffn * rank // d)) if rank else None
@@ -143,9 +150,12 @@ class LlamaBlock(torch.nn.Module):
         qkv = self.qkv(h.reshape(b * l, d)).reshape(b, l, 3, self.heads, d // self.heads)
         # (three slices would each scatter into a zero-filled tensor of q|k|v's size
         # in the backward, which are then summed)
-        q, k, v = ops.split_qkv(qkv)
-        with sdpa_kernel([SDPBackend.FLASH_ATTENTION]):
-            a = torch.nn.functional.scaled_dot_product_attention(q, k, v, is_causal=True)
+        q, k, v = ops.split_qkv(qkv) if self.rope is None else rotary_split_qkv(qkv, self.rope)
+        if self.window is not None:
+            a = window_attention(q, k, v, window=self.window, sinks=self.sinks)
+        else:
+            with sdpa_kernel([SDPBackend.FLASH_ATTENTION]):
+                a = torch.nn.functional.scaled_dot_product_attention(q, k, v, is_causal=True)
         o = self.o(a.transpose(1, 2).reshape(b * l, d)).reshape(b, l, d)
         if type(self.norm2) is RMSNorm:
             x5, h2 = self.norm2.add(x, o)
@@ -184,24 +194,31 @@ def block_saved_bytes(b, l, d, heads, ffn, rank=None, rank_down=None, compress_o
 
 class LlamaModel(torch.nn.Module):
     """Token embedding, n_layers blocks, final RMSNorm and the output layer
-    (uncompressed), with the mean cross-entropy of next-token prediction."""
+    (uncompressed), with the mean cross-entropy of next-token prediction, or, given
+    a teacher's (top_logits, top_ids), both (b, l, K), with distill_loss.  rope, window
+    and sinks as in LlamaBlock."""
 
-    def __init__(self, vocab, d, heads, ffn, n_layers, rank=None, alpha=1.0, device="cuda", proj="gaussian"):
+    def __init__(self, vocab, d, heads, ffn, n_layers, rank=None, alpha=1.0, device="cuda", proj="gaussian", rope=None,
+                 window=None, sinks=0):
         super().__init__()
         self.embed = torch.nn.Parameter((0.02 * torch.randn(vocab, d, device=device)).to(torch.bfloat16))
         self.blocks = torch.nn.ModuleList(
             LlamaBlock(d, heads, ffn, rank=rank, alpha=alpha, device=device, proj=proj,
-                       seeds=[((7 * i + j + 1) << 32) for j in range(7)])
+                       seeds=[((7 * i + j + 1) << 32) for j in range(7)], rope=rope, window=window, sinks=sinks)
             for i in range(n_layers))
         self.norm = RMSNorm(d, device=device)
         self.head = DenseLinear(d, vocab, device)
 
-    def forward(self, tokens, targets):
+    def forward(self, tokens, targets, teacher=None, temperature=1.0, weight=0.5):
         x = self.embed[tokens]
         for blk in self.blocks:
             x = blk(x)
         logits = self.head(self.norm(x))
-        return ops.cross_entropy(logits.reshape(-1, logits.shape[-1]), targets.reshape(-1))
+        logits, targets = logits.reshape(-1, logits.shape[-1]), targets.reshape(-1)
+        if teacher is None:
+            return ops.cross_entropy(logits, targets)
+        top, ids = (t.reshape(-1, t.shape[-1]) for t in teacher)
+        return distill_loss(logits, top, ids, targets=targets, temperature=temperature, weight=weight)
 
     def compact_modules(self):
         return [m for blk in self.blocks for m in blk.compact_modules()]

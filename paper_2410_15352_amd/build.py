@@ -27,6 +27,9 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
 UNITS = [
     ("compact_api.hip", []),
     ("block_ops.hip", []),
+    ("rotary.hip", []),
+    ("attention.hip", []),
+    ("distill.hip", []),
     ("kernels_tile.hip", ["-mllvm", "-enable-misched=false", "-mllvm", "-enable-post-misched=false"]),
     ("kernels_w4.hip", ["-mllvm", "-enable-misched=false", "-mllvm", "-enable-post-misched=false"]),
 ]

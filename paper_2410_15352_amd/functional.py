@@ -1,0 +1,592 @@
+"""Operators of long-context and distilled training, as functions and modules of their own:
+
+    Rotary             rotary positions: half and interleaved layouts, a part of the head,
+                       frequencies scaled for long contexts
+    window_attention   attention with a sliding window and a few first tokens that stay
+                       visible (sinks); training, prompts, and single tokens over a cache
+    distill_loss       distillation from a teacher's top logits, beside the targets
+
+On the current GPU they run the HIP kernels of libcompact.so (csrc/rotary.hip, attention.hip,
+distill.hip) on the current stream, forward and backward: bf16 (Rotary and distill_loss fp32
+too), any strides whose rows start on 16-byte boundaries (others are copied first).  Other
+types and places, autocast, tracing and functorch take the torch expressions beside each
+function, and so does a backward that is itself recorded or batched.  Arguments that no form
+takes are refused with ValueError or TypeError."""
+from __future__ import annotations
+
+import ctypes
+import math
+
+import torch
+
+from . import _block_ops as ops
+from ._block_ops import _eager, _i32, _i64, _plain, _stream, _vp
+
+__all__ = ["Rotary", "window_attention", "distill_loss"]
+
+_f32 = ctypes.c_float
+_bf16 = torch.bfloat16
+
+
+class _RotaryTensor(ctypes.Structure):
+    _fields_ = [("src", _vp), ("dst", _vp), ("src_b", _i64), ("src_l", _i64), ("src_h", _i64), ("dst_b", _i64),
+                ("dst_l", _i64), ("dst_h", _i64), ("heads", _i32), ("rotate", _i32)]
+
+
+class _RotaryArgs(ctypes.Structure):
+    _fields_ = [("t", _RotaryTensor * 3), ("turns", _vp), ("positions", _vp), ("pos_b", _i64), ("pos_l", _i64),
+                ("offset", _i64), ("tokens", _i64), ("l", _i32), ("hd", _i32), ("dims", _i32), ("count", _i32),
+                ("interleaved", _i32), ("inverse", _i32), ("pos32", _i32), ("f32", _i32), ("magnitude", _f32)]
+
+
+class _AttnArgs(ctypes.Structure):
+    _fields_ = [("q", _vp), ("k", _vp), ("v", _vp), ("o", _vp), ("lse", _vp), ("lengths", _vp), ("qs", _i64 * 3),
+                ("ks", _i64 * 3), ("vs", _i64 * 3), ("os", _i64 * 3), ("b", _i32), ("heads", _i32), ("kv", _i32),
+                ("lq", _i32), ("lk", _i32), ("hd", _i32), ("window", _i32), ("sinks", _i32), ("scale", _f32),
+                ("splits", _i32), ("part_o", _vp), ("part_lse", _vp)]
+
+
+class _AttnGradArgs(ctypes.Structure):
+    _fields_ = [("f", _AttnArgs), ("go", _vp), ("dq", _vp), ("dk", _vp), ("dv", _vp), ("delta", _vp), ("gs", _i64 * 3),
+                ("dqs", _i64 * 3), ("dks", _i64 * 3), ("dvs", _i64 * 3)]
+
+
+class _DistillArgs(ctypes.Structure):
+    _fields_ = [("x", _vp), ("top", _vp), ("ids", _vp), ("target", _vp), ("count", _vp), ("loss_row", _vp),
+                ("loss", _vp), ("dx", _vp), ("dloss", _vp), ("rows", _i64), ("V", _i64), ("top_ld", _i64),
+                ("ids_ld", _i64), ("ignore_index", _i64), ("K", _i32), ("f32", _i32), ("top32", _i32), ("ids32", _i32),
+                ("unless_one", _i32), ("temperature", _f32), ("weight", _f32)]
+
+
+ops._SIGNATURES.update({
+    "compact_rotary": [ctypes.POINTER(_RotaryArgs), _vp],
+    "compact_attention_fwd": [ctypes.POINTER(_AttnArgs), _vp],
+    "compact_attention_bwd": [ctypes.POINTER(_AttnGradArgs), _vp],
+    "compact_distill": [ctypes.POINTER(_DistillArgs), _vp],
+})
+
+
+def _here(t):
+    """A tensor of its own storage on the current GPU."""
+    return _plain(t) and t.get_device() >= 0 and t.get_device() == torch._C._cuda_getDevice()
+
+
+def _strides(t):
+    """The strides of the first three dimensions; 0 where a dimension has one element."""
+    return [s if n > 1 else 0 for s, n in zip(t.stride()[:3], t.shape)]
+
+
+def _rows(t):
+    """t (4-D, its last dimension dense and every row on a 16-byte boundary), or a copy of
+    it that is so, and its strides."""
+    s = _strides(t)
+    size = t.element_size()
+    if t.stride(3) != 1 or t.data_ptr() % 16 != 0 or any(x * size % 16 != 0 for x in s):
+        t = t.contiguous()
+        t = t if t.data_ptr() % 16 == 0 else t.clone()
+        s = _strides(t)
+    return t, s
+
+
+# ------------------------------- rotary -------------------------------------
+
+def _rotary_frequencies(dims, base, scaling, factor, original_length, low, high):
+    """Radians per position of each pair, and the factor on the rotated values."""
+    if scaling == "ntk":
+        base = base * factor ** (dims / (dims - 2))
+    f = [base ** (-2 * i / dims) for i in range(dims // 2)]
+    if scaling == "linear":
+        return [x / factor for x in f], 1.0
+    if scaling == "parts":
+        def part(x):
+            # 1: the pair turns at least `high` times over the trained length, and is kept; 0: at most `low` times
+            keep = min(1.0, max(0.0, (original_length * x / (2 * math.pi) - low) / (high - low)))
+            return x * (keep + (1 - keep) / factor)
+        return [part(x) for x in f], 0.1 * math.log(factor) + 1
+    return f, 1.0
+
+
+class Rotary(torch.nn.Module):
+    """Rotary positions: pair i of the first `dims` elements of a head turns by position x
+    base^(-2 i / dims), the rest of the head stays.
+
+    layout: "half" (element i with i + dims / 2) or "interleaved" (2 i with 2 i + 1).
+    scaling, for contexts `factor` times as long as the trained ones:
+      "none"
+      "linear"  every frequency divided by factor
+      "ntk"     base raised by factor^(dims / (dims - 2)): the slowest pair as with "linear",
+                the fastest as it was
+      "parts"   by the turns that a pair makes over original_length: `high` and more keep the
+                frequency, `low` and fewer divide it by factor, a ramp between; the rotated
+                values are multiplied by 0.1 ln(factor) + 1 (in q and in k)
+
+    rope(q, k, positions=...) rotates q (b, l, heads, hd) and, if given, k (b, l, kv, hd);
+    positions: None (0, 1, ...), an int (the first one's), or integers of shape (l,) or (b, l).
+    No parameters; the angles are exact for any position (fp64)."""
+
+    def __init__(self, dims, base=10000.0, layout="half", scaling="none", factor=1.0, original_length=2048, low=1.0,
+                 high=32.0):
+        super().__init__()
+        if dims < 2 or dims % 2 != 0:
+            raise ValueError("rotary dims: an even number from 2 on")
+        if layout not in ("half", "interleaved"):
+            raise ValueError('rotary layout: "half" or "interleaved"')
+        if scaling not in ("none", "linear", "ntk", "parts"):
+            raise ValueError('rotary scaling: "none", "linear", "ntk" or "parts"')
+        if not (base > 0 and factor >= 1 and original_length > 0 and high > low) or scaling == "ntk" and dims == 2:
+            raise ValueError("rotary: base > 0, factor >= 1, original_length > 0, high > low, and dims > 2 with ntk")
+        self.dims, self.interleaved = dims, layout == "interleaved"
+        f, self.magnitude = _rotary_frequencies(dims, float(base), scaling, float(factor), original_length, low, high)
+        # (not a buffer: module.to(dtype) must not round it)
+        self._turns = {torch.device("cpu"): torch.tensor([x / (2 * math.pi) for x in f], dtype=torch.float64)}
+
+    def turns(self, device):
+        """Revolutions per position of each pair, fp64."""
+        t = self._turns.get(device)
+        if t is None:
+            t = self._turns[device] = self._turns[torch.device("cpu")].to(device)
+        return t
+
+    def forward(self, q, k=None, positions=None):
+        self._check(q, k, positions)
+        if self._usable(q, k, positions):
+            out = _RotaryFn.apply(self, positions, q, k)
+            return out if k is not None else out[0]
+        out = _rotary_torch(self, positions, False, q, k)
+        return out if k is not None else out[0]
+
+    def _check(self, q, k, positions):
+        for t in (q, k):
+            if t is None:
+                continue
+            if t.dim() != 4 or t.shape[:2] != q.shape[:2] or t.shape[3] != q.shape[3]:
+                raise ValueError("rotary: q (b, l, heads, hd) and k (b, l, kv, hd)")
+            if not t.is_floating_point() or t.dtype != q.dtype or t.device != q.device:
+                raise TypeError("rotary: q and k of one floating type on one device")
+        if self.dims > q.shape[3]:
+            raise ValueError(f"rotary: {self.dims} dims of heads of {q.shape[3]}")
+        if isinstance(positions, torch.Tensor):
+            if positions.dtype not in (torch.int64, torch.int32) or positions.device != q.device:
+                raise TypeError("rotary positions: int64 or int32 on q's device")
+            if positions.shape not in (q.shape[1:2], q.shape[:2]):
+                raise ValueError("rotary positions: shape (l,) or (b, l)")
+        elif positions is not None and not isinstance(positions, int):
+            raise TypeError("rotary positions: None, an int or a tensor of integers")
+
+    def _usable(self, *tensors_and_positions):
+        if not _eager():
+            return False
+        q, k, positions = tensors_and_positions
+        if not all(_here(t) for t in (q, k) if t is not None) or q.dtype not in (_bf16, torch.float32):
+            return False
+        b, l, heads, hd = q.shape
+        n = 16 // q.element_size()
+        return (hd % n == 0 and n <= hd <= 1024 and min(q.shape) > 0 and (k is None or k.shape[2] > 0)
+                and (heads + (0 if k is None else k.shape[2])) * hd < 1 << 16 and b * l < ops.MAX_ROWS
+                and (not isinstance(positions, torch.Tensor) or _plain(positions)))
+
+
+def _rotary_call(rope, positions, inverse, jobs):
+    """jobs: (source, destination, rotated) of (b, l, heads, hd) tensors whose rows are dense
+    and on 16-byte boundaries."""
+    a = _RotaryArgs()
+    x = jobs[0][0]
+    b, l, _, hd = x.shape
+    for t, (src, dst, rotate) in zip(a.t, jobs):
+        t.src, t.dst, t.heads, t.rotate = src.data_ptr(), dst.data_ptr(), src.shape[2], rotate
+        t.src_b, t.src_l, t.src_h = _strides(src)
+        t.dst_b, t.dst_l, t.dst_h = _strides(dst)
+    a.turns = rope.turns(x.device).data_ptr()
+    if isinstance(positions, torch.Tensor):
+        a.positions, a.pos32 = positions.data_ptr(), positions.dtype == torch.int32
+        a.pos_b, a.pos_l = ([0, *positions.stride()] if positions.dim() == 1 else positions.stride())
+    else:
+        a.offset = positions or 0
+    a.tokens, a.l, a.hd, a.dims, a.count = b * l, l, hd, rope.dims, len(jobs)
+    a.interleaved, a.inverse, a.f32, a.magnitude = rope.interleaved, inverse, x.dtype == torch.float32, rope.magnitude
+    ops._call("compact_rotary", ctypes.byref(a), _stream(x))
+
+
+def _rotary_torch(rope, positions, inverse, *tensors):
+    """The rotation as torch expressions, in fp32 (fp64 for fp64)."""
+    x = tensors[0]
+    b, l = x.shape[:2]
+    if not isinstance(positions, torch.Tensor):
+        positions = torch.arange(l, device=x.device) + (positions or 0)
+    turn = positions.unsqueeze(-1).double() * rope.turns(x.device)
+    angle = 2 * math.pi * (turn - turn.round())
+    wide = torch.float64 if x.dtype == torch.float64 else torch.float32
+    cos = (rope.magnitude * torch.cos(angle)).to(wide).unsqueeze(-2)
+    sin = (rope.magnitude * torch.sin(angle)).to(wide).unsqueeze(-2)
+    sin = -sin if inverse else sin
+    out = []
+    D = rope.dims
+    for t in tensors:
+        if t is None:
+            out.append(None)
+            continue
+        y = t[..., :D].to(wide)
+        a, c = (y[..., 0::2], y[..., 1::2]) if rope.interleaved else (y[..., :D // 2], y[..., D // 2:])
+        pair = (a * cos - c * sin, c * cos + a * sin)
+        y = torch.stack(pair, -1).flatten(-2) if rope.interleaved else torch.cat(pair, -1)
+        out.append(torch.cat((y.to(t.dtype), t[..., D:]), -1))
+    return tuple(out)
+
+
+class _RotaryFn(torch.autograd.Function):
+    """q and k turned; nothing is kept but the positions."""
+
+    @staticmethod
+    def forward(ctx, rope, positions, q, k):
+        ctx.rope, ctx.positions, ctx.pair = rope, positions, k is not None
+        ctx.set_materialize_grads(False)
+        jobs = [(_rows(t)[0], torch.empty(t.shape, dtype=t.dtype, device=t.device), 1) for t in (q, k) if t is not None]
+        _rotary_call(rope, positions, 0, jobs)
+        return tuple(j[1] for j in jobs) + (() if ctx.pair else (None,))
+
+    @staticmethod
+    def backward(ctx, dq, dk):
+        given = [t for t in (dq, dk) if t is not None]
+        if not given:
+            return None, None, None, None
+        if torch.is_grad_enabled() or not ctx.rope._usable(given[0], given[-1], ctx.positions):
+            out = iter(_rotary_torch(ctx.rope, ctx.positions, True, *given))
+        else:
+            jobs = [(_rows(t)[0], torch.empty(t.shape, dtype=t.dtype, device=t.device), 1) for t in given]
+            _rotary_call(ctx.rope, ctx.positions, 1, jobs)
+            out = (j[1] for j in jobs)
+        dq, dk = (None if t is None else next(out) for t in (dq, dk))
+        return None, None, dq, dk
+
+
+class _RotaryQkvFn(torch.autograd.Function):
+    """q, k (turned in place) and v (b, heads, l, hd) as views of qkv (b, l, 3, heads, hd);
+    the backward turns back and joins their gradients in one pass."""
+
+    @staticmethod
+    def forward(ctx, rope, positions, qkv):
+        ctx.rope, ctx.positions, ctx.shape = rope, positions, qkv.shape
+        ctx.set_materialize_grads(False)
+        q, k, v = qkv.unbind(2)
+        _rotary_call(rope, positions, 0, [(q, q, 1), (k, k, 1)])
+        torch.autograd.graph.increment_version(qkv)  # whoever saved it is told
+        return tuple(t.transpose(1, 2) for t in (q, k, v))
+
+    @staticmethod
+    def backward(ctx, *grads):
+        some = next((g for g in grads if g is not None), None)
+        if some is None:
+            return None, None, None
+        grads = [torch.zeros_like(some) if g is None else g for g in grads]
+        dq, dk, dv = (g.transpose(1, 2) for g in grads)
+        if torch.is_grad_enabled() or not _here(dv) or not ctx.rope._usable(dq, dk, ctx.positions):
+            dq, dk = _rotary_torch(ctx.rope, ctx.positions, True, dq, dk)
+            return None, None, torch.stack((dq, dk, dv), 2)
+        out = torch.empty(ctx.shape, dtype=dq.dtype, device=dq.device)
+        _rotary_call(ctx.rope, ctx.positions, 1,
+                     [(_rows(g)[0], to, rotate) for g, to, rotate in zip((dq, dk, dv), out.unbind(2), (1, 1, 0))])
+        return None, None, out
+
+
+def rotary_split_qkv(qkv, rope, positions=None):
+    """q, k (turned) and v (b, heads, l, hd) of qkv (b, l, 3, heads, hd), which a projection
+    has just written: the kernel turns q and k where they stand, so the block keeps no more
+    than without positions."""
+    q, k, v = qkv.unbind(2)
+    rope._check(q, k, positions)
+    if (rope._usable(q, k, positions) and qkv.is_contiguous() and qkv.data_ptr() % 16 == 0
+            and not (qkv.is_leaf and qkv.requires_grad)):
+        return _RotaryQkvFn.apply(rope, positions, qkv)
+    q, k = _rotary_torch(rope, positions, False, q, k)
+    return tuple(t.transpose(1, 2) for t in (q, k, v))
+
+
+# ------------------------------ attention -----------------------------------
+
+NO_WINDOW = 1 << 30
+MAX_HD = 128
+
+
+def _visible(lq, lk, lengths, window, sinks, device):
+    """(b or 1, 1, lq, lk): key j is seen from row i."""
+    j = torch.arange(lk, device=device)
+    L = torch.full((1,), lk, device=device) if lengths is None else lengths.to(torch.int64).clamp(0, lk)
+    p = (torch.arange(lq, device=device) + (L.unsqueeze(-1) - lq)).unsqueeze(-1)
+    seen = j <= p
+    if window is not None:
+        seen = seen & ((p - j < window) | (j < sinks))
+    return seen.unsqueeze(1)
+
+
+def _attention_torch(q, k, v, window, sinks, lengths, scale):
+    """The attention as torch expressions, in fp32 (fp64 for fp64)."""
+    b, heads, lq, hd = q.shape
+    kv, lk = k.shape[1:3]
+    wide = torch.float64 if q.dtype == torch.float64 else torch.float32
+    qw, kw, vw = (t.to(wide) for t in (q, k, v))
+    if lk == 0:
+        return (qw * 0).to(q.dtype)
+    if kv != heads:
+        kw, vw = (t.repeat_interleave(heads // kv, 1) for t in (kw, vw))
+    seen = _visible(lq, lk, lengths, window, sinks, q.device)
+    s = torch.matmul(qw, kw.transpose(2, 3).contiguous()) * scale
+    s = torch.where(seen, s, -math.inf)
+    some = seen.any(-1, keepdim=True)
+    top = torch.where(some, s.detach().amax(-1, keepdim=True), 0.0)
+    e = torch.exp(s - top)
+    p = e / torch.where(some, e.sum(-1, keepdim=True), 1.0)
+    return torch.matmul(p, vw).to(q.dtype)
+
+
+def attention_splits(b, heads, kv, lq, lk, window, sinks):
+    """Ranges of keys for the form that splits them (0: the form that splits the queries).
+    A wave of the split form takes 32 rows of the heads that share keys and a range of the
+    keys; 2048 waves fill the card, and a range has at least 4 tiles of 32 keys."""
+    blocks = b * kv * -(-(heads // kv) * lq // 32)
+    if lq * (heads // kv) > 128 or b * kv > 65535:
+        return 0
+    tiles = -(-min(lk, window + sinks + lq) // 32)
+    return max(1, min(2048 // blocks, tiles // 4))
+
+
+def _attn_args(q, k, v, o, lse, lengths, window, sinks, scale):
+    a = _AttnArgs()
+    a.q, a.k, a.v, a.o, a.lse = q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr()
+    if lengths is not None:
+        a.lengths = lengths.data_ptr()
+    a.qs[:], a.ks[:], a.vs[:], a.os[:] = _strides(q), _strides(k), _strides(v), _strides(o)
+    a.b, a.heads, a.lq, a.hd = q.shape
+    a.kv, a.lk = k.shape[1:3]
+    a.window, a.sinks, a.scale = window, sinks, scale
+    return a
+
+
+def _attn_tensors(*tensors):
+    """bf16 (b, heads, l, hd) tensors as the kernels take them, or None."""
+    if not all(_here(t) and t.dtype == _bf16 and t.numel() > 0 for t in tensors):
+        return None
+    return [_rows(t)[0] for t in tensors]
+
+
+def _empty_heads(like, l=None):
+    """(b, heads, l, hd) that lies as (b, l, heads, hd), the layout the projections take."""
+    b, heads, n, hd = like.shape
+    return torch.empty(b, n, heads, hd, dtype=_bf16, device=like.device).transpose(1, 2)
+
+
+class _AttentionFn(torch.autograd.Function):
+    """Keeps q, k, v, o and one fp32 number a row."""
+
+    @staticmethod
+    def forward(ctx, q, k, v, window, sinks, lengths, scale):
+        qr, kr, vr = _attn_tensors(q, k, v)
+        b, heads, lq, hd = q.shape
+        kv, lk = k.shape[1:3]
+        o = _empty_heads(q)
+        lse = torch.empty(b, heads, lq, dtype=torch.float32, device=q.device)
+        w = NO_WINDOW if window is None else min(window, NO_WINDOW)
+        a = _attn_args(qr, kr, vr, o, lse, lengths, w, min(sinks, NO_WINDOW), scale)
+        a.splits = attention_splits(b, heads, kv, lq, lk, w, a.sinks)
+        if a.splits > 0:
+            part = torch.empty(a.splits * b * heads * lq * (hd + 1), dtype=torch.float32, device=q.device)
+            a.part_o, a.part_lse = part.data_ptr(), part.data_ptr() + 4 * a.splits * b * heads * lq * hd
+        ops._call("compact_attention_fwd", ctypes.byref(a), _stream(q))
+        ctx.rule = window, sinks, scale
+        ctx.save_for_backward(qr, kr, vr, o, lse, lengths)
+        return o
+
+    @staticmethod
+    def backward(ctx, do):
+        q, k, v, o, lse, lengths = ctx.saved_tensors
+        window, sinks, scale = ctx.rule
+        none = None, None, None, None
+        t = None
+        if not torch.is_grad_enabled() and _eager() and _plain(do) and ops._companion(lse, torch.float32, q.shape[:3].numel()):
+            t = _attn_tensors(q, k, v, o, do.to(_bf16))
+        if t is None:
+            recorded = torch.is_grad_enabled()
+            with torch.enable_grad():
+                leaves = [x if recorded and x.requires_grad else x.detach().requires_grad_(True) for x in (q, k, v)]
+                y = _attention_torch(*leaves, window, sinks, lengths, scale)
+                return (*torch.autograd.grad(y, leaves, do, create_graph=recorded), *none)
+        q, k, v, o, do = t
+        w = NO_WINDOW if window is None else min(window, NO_WINDOW)
+        g = _AttnGradArgs()
+        g.f = _attn_args(q, k, v, o, lse, lengths, w, min(sinks, NO_WINDOW), scale)
+        dq, delta = _empty_heads(q), torch.empty_like(lse)
+        g.go, g.dq, g.delta = do.data_ptr(), dq.data_ptr(), delta.data_ptr()
+        g.gs[:], g.dqs[:] = _strides(do), _strides(dq)
+        dk = dv = None
+        if ctx.needs_input_grad[1] or ctx.needs_input_grad[2]:
+            dk, dv = _empty_heads(k), _empty_heads(v)
+            g.dk, g.dv = dk.data_ptr(), dv.data_ptr()
+            g.dks[:], g.dvs[:] = _strides(dk), _strides(dv)
+        ops._call("compact_attention_bwd", ctypes.byref(g), _stream(q))
+        return dq, dk, dv, *none
+
+
+def window_attention(q, k, v, window=None, sinks=0, lengths=None, scale=None):
+    """softmax(scale q k^T) v over the keys that each row sees; q (b, heads, lq, hd), k and v
+    (b, kv, lk, hd), heads a multiple of kv (query head h reads head h kv // heads).
+
+    A sequence has L keys: lk, or lengths[b] of them (integers on the device, 0 .. lk; what lies
+    past them is not read).  Its rows are its last lq positions: row i stands at p = i + L - lq
+    and sees key j when j <= p and (p - j < window or j < sinks); window None: every j <= p.
+    A row that sees no key (lq > L) gives zeros and passes no gradient.  A key that a row does
+    not see has no part in it, whatever it holds.  scale: 1 / sqrt(hd) if None.
+
+    The kernels take bf16 with heads of up to 128 elements, a multiple of 8."""
+    if q.dim() != 4 or k.dim() != 4 or v.dim() != 4:
+        raise ValueError("window_attention: q (b, heads, lq, hd), k and v (b, kv, lk, hd)")
+    if k.shape != v.shape or q.shape[0] != k.shape[0] or q.shape[3] != k.shape[3]:
+        raise ValueError(f"window_attention: q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}")
+    if k.shape[1] == 0 or q.shape[1] % k.shape[1] != 0:
+        raise ValueError(f"window_attention: {q.shape[1]} query heads over {k.shape[1]} of k and v")
+    if not q.is_floating_point() or q.dtype != k.dtype or q.dtype != v.dtype or not q.device == k.device == v.device:
+        raise TypeError("window_attention: q, k and v of one floating type on one device")
+    if window is not None and window < 1 or sinks < 0:
+        raise ValueError("window_attention: window >= 1 (or None) and sinks >= 0")
+    if lengths is not None:
+        if lengths.shape != q.shape[:1] or lengths.device != q.device or lengths.dtype not in (torch.int32, torch.int64):
+            raise ValueError("window_attention: lengths (b,) of int32 or int64 on q's device")
+    scale = q.shape[3] ** -0.5 if scale is None else float(scale)
+    if not (scale > 0 and math.isfinite(scale)):
+        raise ValueError("window_attention: scale > 0")
+    if _eager() and _attention_usable(q, k, v):
+        if lengths is not None:
+            lengths = lengths.to(torch.int32).contiguous()
+        return _AttentionFn.apply(q, k, v, window, sinks, lengths, scale)
+    return _attention_torch(q, k, v, window, sinks, lengths, scale)
+
+
+def _attention_usable(q, k, v):
+    b, heads, lq, hd = q.shape
+    kv, lk = k.shape[1:3]
+    return (q.dtype == _bf16 and hd % 8 == 0 and 8 <= hd <= MAX_HD and min(b, lq, lk) > 0 and max(lq, lk) <= 1 << 30
+            and b * heads * -(-lq // 32) < 1 << 24 and b * kv * -(-lk // 32) < 1 << 24
+            and _here(q) and _here(k) and _here(v))
+
+
+# ----------------------------- distillation ---------------------------------
+
+MAX_TOP = 1024
+
+
+def _distill_torch(logits, top_logits, top_ids, targets, temperature, weight):
+    """The loss as torch expressions, in fp32 (fp64 for fp64)."""
+    rows, V = logits.shape
+    T, w = temperature, weight
+    wide = torch.float64 if logits.dtype == torch.float64 else torch.float32
+    counts = targets != ops.IGNORE if targets is not None else torch.ones(rows, dtype=torch.bool, device=logits.device)
+    # (a row that does not count has no part, whatever it holds)
+    x = torch.where(counts.unsqueeze(-1), logits.to(wide), 0.0)
+    there = (top_ids >= 0) & (top_ids < V)
+    ids = torch.where(there, top_ids, 0).to(torch.int64)
+    bad = (top_ids >= V).any(-1)
+    t = torch.where(top_ids >= 0, top_logits.to(wide) / T, -math.inf)
+    top = t.amax(-1, keepdim=True)
+    e = torch.exp(t - torch.where(top == -math.inf, 0.0, top))
+    s = e.sum(-1, keepdim=True)
+    p = e / torch.where(s == 0, 1.0, s)
+    logq = torch.log_softmax(x / T, -1).gather(1, ids)
+    part = (p != 0) & there
+    terms = torch.where(part, p, 1.0) * (torch.log(torch.where(part, p, 1.0)) - torch.where(part, logq, 0.0))
+    loss = w * T * T * torch.where(part, terms, 0.0).sum(-1)
+    if targets is not None and w != 1.0:
+        out = counts & ((targets < 0) | (targets >= V))
+        bad = bad | out
+        hard = torch.log_softmax(x, -1).gather(1, torch.where(counts & ~out, targets, 0).unsqueeze(-1)).squeeze(-1)
+        loss = loss - (1 - w) * hard
+    loss = loss * torch.where(bad, math.nan, 1.0)
+    return (torch.where(counts, loss, 0.0).sum() / counts.sum()).to(torch.float64 if wide == torch.float64 else torch.float32)
+
+
+def _distill_call(logits, top, ids, targets, count, temperature, weight, loss=None, dx=None, dloss=None, unless_one=False):
+    a = _DistillArgs()
+    a.x, a.top, a.ids = logits.data_ptr(), top.data_ptr(), ids.data_ptr()
+    a.rows, a.V = logits.shape
+    a.K, a.top_ld, a.ids_ld = top.shape[1], top.stride(0), ids.stride(0)
+    a.f32, a.top32, a.ids32 = logits.dtype == torch.float32, top.dtype == torch.float32, ids.dtype == torch.int32
+    if targets is not None:
+        a.target, a.count, a.ignore_index = targets.data_ptr(), count.data_ptr(), ops.IGNORE
+    if loss is not None:
+        row = torch.empty(logits.shape[0], dtype=torch.float32, device=logits.device)
+        a.loss_row, a.loss = row.data_ptr(), loss.data_ptr()
+    if dx is not None:
+        a.dx = dx.data_ptr()
+    if dloss is not None:
+        a.dloss, a.unless_one = dloss.data_ptr(), unless_one
+    a.temperature, a.weight = temperature, weight
+    ops._call("compact_distill", ctypes.byref(a), _stream(logits))
+
+
+class _DistillFn(torch.autograd.Function):
+    """The loss, and with it the gradient for dloss = 1, while a row is in registers: the
+    backward finds dloss to be 1 on the GPU and leaves it, or forms it again."""
+
+    @staticmethod
+    def forward(ctx, logits, top, ids, targets, temperature, weight):
+        loss = torch.empty((), dtype=torch.float32, device=logits.device)
+        count = torch.empty((), dtype=torch.float32, device=logits.device) if targets is not None else None
+        ctx.dx = torch.empty_like(logits) if ctx.needs_input_grad[0] else None
+        _distill_call(logits, top, ids, targets, count, temperature, weight, loss=loss, dx=ctx.dx)
+        ctx.rule = temperature, weight
+        ctx.save_for_backward(logits, top, ids, targets, count)
+        return loss
+
+    @staticmethod
+    def backward(ctx, dloss):
+        logits, top, ids, targets, count = ctx.saved_tensors
+        rule = ctx.rule
+        if torch.is_grad_enabled() or not _eager() or not _plain(dloss) or not _distill_usable(logits, top, ids, targets):
+            return (ops._torch_grad(lambda t: _distill_torch(t, top, ids, targets, *rule), logits, dloss),
+                    None, None, None, None, None)
+        dx, ctx.dx = ctx.dx, None
+        first = dx is not None  # a second backward over a retained graph forms its own
+        dx = dx if first else torch.empty_like(logits)
+        _distill_call(logits, top, ids, targets, count, *rule, dx=dx, dloss=dloss.float(), unless_one=first)
+        return dx, None, None, None, None, None
+
+
+def _distill_usable(logits, top, ids, targets):
+    return (logits.dtype in (_bf16, torch.float32) and top.dtype in (_bf16, torch.float32)
+            and all(_here(t) for t in (logits, top, ids)) and logits.is_contiguous() and logits.data_ptr() % 16 == 0
+            and 0 < logits.shape[0] < ops.MAX_ROWS and 0 < logits.shape[1] <= 1 << 30 and 1 <= top.shape[1] <= MAX_TOP
+            and top.stride(1) == 1 and ids.stride(1) == 1 and (targets is None or _here(targets) and targets.is_contiguous()))
+
+
+def distill_loss(logits, top_logits, top_ids, targets=None, temperature=1.0, weight=1.0):
+    """The mean over the rows of
+
+        weight T^2 sum_k p_k (log p_k - log q_id_k) + (1 - weight) (-log softmax(logits)_target)
+
+    for logits (rows, V), a teacher's K top logits of each row and their ids (rows, K), in any
+    order: p = softmax(top_logits / T) over a row's entries, q = softmax(logits / T) over all V.
+    An entry with a negative id, or a logit of -inf, is none; a row without entries has no first
+    part.  With targets (rows,) rows whose target is -100 do not count, and they are needed where
+    weight < 1.  An id or a target past V makes the loss, and its row's gradient, NaN.
+
+    fp32 scalar.  The kernels take dense bf16 or fp32 logits and K up to 1024."""
+    if logits.dim() != 2 or top_logits.dim() != 2 or top_logits.shape != top_ids.shape or top_logits.shape[0] != logits.shape[0]:
+        raise ValueError("distill_loss: logits (rows, V), top_logits and top_ids (rows, K)")
+    if top_logits.shape[1] < 1:
+        raise ValueError("distill_loss: at least one entry a row")
+    if not logits.is_floating_point() or not top_logits.is_floating_point() or top_ids.dtype not in (torch.int64, torch.int32):
+        raise TypeError("distill_loss: floating logits, int64 or int32 ids")
+    if targets is not None and (targets.shape != logits.shape[:1] or targets.dtype != torch.int64):
+        raise ValueError("distill_loss: targets (rows,) of int64")
+    if any(t is not None and t.device != logits.device for t in (top_logits, top_ids, targets)):
+        raise ValueError("distill_loss: tensors of one device")
+    temperature, weight = float(temperature), float(weight)
+    if not (temperature > 0 and math.isfinite(temperature)) or not 0 <= weight <= 1:
+        raise ValueError("distill_loss: temperature > 0 and weight in [0, 1]")
+    if targets is None and weight != 1:
+        raise ValueError("distill_loss: a weight below 1 needs targets")
+    if _eager() and logits.is_cuda:
+        dense = logits if logits.is_contiguous() else logits.contiguous()
+        dense = dense if dense.data_ptr() % 16 == 0 else dense.clone()
+        top, ids = (t.detach() if t.stride(1) == 1 else t.detach().contiguous() for t in (top_logits, top_ids))
+        targets = targets if targets is None else targets.contiguous()
+        if not (top_logits.requires_grad and torch.is_grad_enabled()) and _distill_usable(dense, top, ids, targets):
+            return _DistillFn.apply(dense, top, ids, targets, temperature, weight)
+    return _distill_torch(logits, top_logits, top_ids, targets, temperature, weight)

@@ -1,0 +1,567 @@
+"""Rotary positions, windowed attention and distillation on the GPU against float64, at the
+edges of their tiles, chunks, windows and lengths.
+
+Tolerances.  u = 2^-8 covers the rounding of a bf16 result (half of it would do) or of a bf16
+factor inside a product; a score is an fp32 sum of hd products, off by at most
+d = LAM sqrt(hd) 2^-24 scale sum |q||k|, and so is dO.v.  With the exponential's and the
+logarithm's 2^-20 on top a probability is off by e = 2 d + 2^-18 of itself, so that
+
+  o   is within u |o| + (u + e) P|v|
+  dv            u |dv| + (u + e) P^T|dO|
+  dS            u |dS| + e P (|dP| + |D|) + P (d' + dD), with D = sum(dO o) of a rounded o: dD = (u + e) sum |dO| (|o| + P|v|)
+  dq, dk        u |dq| + scale (the bound of dS) |k|, and with the fp32 sums' LAM sqrt(n) 2^-24 of their terms.
+
+fp32 results of the element-wise kernels are within a few 2^-24 of their terms' magnitudes."""
+import math
+
+import pytest
+
+from gpu_util import BF16_U, LAM, U32, dev
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+ops = pytest.importorskip("paper_2410_15352_amd._block_ops")
+F = pytest.importorskip("paper_2410_15352_amd.functional")
+blk = pytest.importorskip("paper_2410_15352_amd.block")
+
+
+def _rand(*shape, scale=1.0, seed=0, dtype=torch.bfloat16):
+    g = torch.Generator(device=dev()).manual_seed(seed + sum(shape))
+    return (scale * torch.randn(*shape, generator=g, device=dev())).to(dtype)
+
+
+def _within(a, ref, tol, what=""):
+    bad = ~((a.double() - ref).abs() <= tol + 1e-30)
+    assert a.shape == ref.shape and not bool(bad.any()), (what, int(bad.sum()), a.double()[bad][:3], ref[bad][:3], tol[bad][:3])
+
+
+def _kernel_ran(monkeypatch):
+    """The torch expressions are not what answers."""
+    def no(*a, **k):
+        raise AssertionError("torch expressions")
+    for name in ("_rotary_torch", "_attention_torch", "_distill_torch"):
+        monkeypatch.setattr(F, name, no)
+
+
+# ------------------------------- rotary -------------------------------------
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("b,l,heads,kv,hd,dims", [(1, 1, 1, 1, 8, 2), (2, 1, 16, 16, 64, 64), (3, 37, 5, 1, 80, 20),
+                                                 (2, 130, 4, 2, 96, 96), (1, 1025, 8, 8, 64, 32), (2, 9, 3, 3, 1024, 1024)])
+def test_rotary(monkeypatch, dtype, layout, b, l, heads, kv, hd, dims):
+    rope = F.Rotary(dims, layout=layout, scaling="parts", factor=4.0)
+    expect = F._rotary_torch
+    _kernel_ran(monkeypatch)
+    q, k = (_rand(b, l, n, hd, dtype=dtype, seed=n).requires_grad_(True) for n in (heads, kv))
+    gq, gk = (_rand(b, l, n, hd, dtype=dtype, seed=n + 7) for n in (heads, kv))
+    start = torch.randint(1_000_000, (b, 1), device=dev())
+    for pos in (None, 3, torch.arange(l, device=dev(), dtype=torch.int32) * 5, start + torch.arange(l, device=dev())):
+        out = rope(q, k, positions=pos)
+        grads = torch.autograd.grad(out, (q, k), (gq, gk))
+        for x, y, inverse in ((q, out[0], False), (k, out[1], False), (gq, grads[0], True), (gk, grads[1], True)):
+            X = x.detach().double()
+            ref = expect(rope, pos, inverse, X)[0]
+            # the two products of an element
+            mag = torch.zeros_like(X)
+            mag[..., :dims] = 2 * rope.magnitude * X[..., :dims].abs().amax(-1, keepdim=True)
+            _within(y, ref, (BF16_U if dtype == torch.bfloat16 else 0) * ref.abs() + 8 * U32 * mag)
+        # the transpose: <R x, g> = <x, R^T g>
+        left = sum((o.double() * g.double()).sum() for o, g in zip(out, (gq, gk)))
+        right = sum((x.double() * g.double()).sum() for x, g in zip((q, k), grads))
+        assert abs(left - right) <= (2 * BF16_U if dtype == torch.bfloat16 else 64 * U32) * rope.magnitude * (
+            q.double().norm() * gq.double().norm() + k.double().norm() * gk.double().norm())
+
+
+def test_rotary_strides_and_routes(monkeypatch):
+    rope = F.Rotary(32)
+    qkv = _rand(2, 9, 3, 4, 64)
+    q, k, _ = qkv.unbind(2)
+    plain = rope(q.contiguous(), k.contiguous())
+    for t in (rope(q, k), rope(q.transpose(1, 2).contiguous().transpose(1, 2), k)):
+        assert torch.equal(t[0], plain[0]) and torch.equal(t[1], plain[1])
+    shifted = torch.empty(2 * 9 * 4 * 64 + 1, dtype=torch.bfloat16, device=dev())[1:].view(2, 9, 4, 64).copy_(q)
+    assert torch.equal(rope(shifted), plain[0])
+    assert torch.equal(rope(q[:, :1].expand(2, 9, 4, 64)), rope(q[:, :1].expand(2, 9, 4, 64).contiguous()))
+    # only one of the results used; a recorded backward
+    a, c = q.detach().clone().requires_grad_(True), k.detach().clone().requires_grad_(True)
+    (g,) = torch.autograd.grad(rope(a, c)[1], c, torch.ones_like(c))
+    assert g.shape == c.shape
+    (g2,) = torch.autograd.grad(rope(a, c)[0], a, torch.ones_like(a), create_graph=True)
+    assert g2.shape == a.shape
+    # odd heads and fp64 are torch's
+    assert rope(_rand(1, 2, 1, 36)).shape == (1, 2, 1, 36)
+    assert rope(_rand(1, 2, 1, 64, dtype=torch.float64)).dtype == torch.float64
+    assert rope(_rand(1, 0, 1, 64)).shape == (1, 0, 1, 64)
+
+
+@pytest.mark.parametrize("layout,dims", [("half", 64), ("half", 24), ("interleaved", 20)])
+def test_rotary_in_place_of_qkv(layout, dims):
+    rope = F.Rotary(dims, layout=layout)
+    qkv = _rand(2, 33, 3, 4, 64).requires_grad_(True)
+    q, k, v = qkv.detach().unbind(2)
+    rq, rk = rope(q, k)
+    w = [_rand(2, 33, 4, 64, seed=s).transpose(1, 2) for s in (1, 2, 3)]
+    fresh = qkv * 1
+    version = fresh._version
+    out = F.rotary_split_qkv(fresh, rope)
+    assert out[0].data_ptr() == fresh.data_ptr() and fresh._version > version
+    for a, c in zip(out, (rq, rk, v)):
+        assert torch.equal(a, c.transpose(1, 2))
+    torch.autograd.backward(out, w)
+    dq, dk = (torch.autograd.grad(rope(x), x, g.transpose(1, 2))[0]
+              for x, g in ((t.detach().clone().requires_grad_(True), g) for t, g in zip((q, k), w)))
+    assert torch.equal(qkv.grad, torch.stack((dq, dk, w[2].transpose(1, 2)), 2))
+    # a leaf stays as it is
+    leaf = qkv.detach().clone().requires_grad_(True)
+    F.rotary_split_qkv(leaf, rope)
+    assert torch.equal(leaf, qkv)
+
+
+# ------------------------------ attention -----------------------------------
+
+def _reference(q, k, v, do, window, sinks, lengths, scale):
+    """float64 results, and the bounds of the docstring."""
+    b, heads, lq, hd = q.shape
+    kv, lk = k.shape[1:3]
+    G = heads // kv
+    Q, K, V, dO = (t.detach().double().cpu() for t in (q, k, v, do))
+    K, V = (t.repeat_interleave(G, 1) for t in (K, V))
+    seen = F._visible(lq, lk, None if lengths is None else lengths.cpu(), window, sinks, "cpu")
+    some = seen.any(-1, keepdim=True)
+    S = torch.where(seen, Q @ K.transpose(2, 3) * scale, -math.inf)
+    P = torch.where(seen, torch.exp(S - torch.where(some, S.amax(-1, keepdim=True), 0.0)), 0.0)
+    P = P / torch.where(some, P.sum(-1, keepdim=True), 1.0)
+    O = P @ V
+    dP = dO @ V.transpose(2, 3)
+    D = (dO * O).sum(-1, keepdim=True)
+    dS = P * (dP - D)
+    fold = lambda t: t.view(b, kv, G, lk, hd).sum(2)
+    dQ, dK, dV = scale * dS @ K, fold(scale * dS.transpose(2, 3) @ Q), fold(P.transpose(2, 3) @ dO)
+
+    acc = LAM * math.sqrt(hd) * U32
+    absS = Q.abs() @ K.abs().transpose(2, 3) * scale
+    top = torch.where(seen, absS, 0.0).amax(-1, keepdim=True)
+    e = 2 * acc * top + 2.0 ** -18
+    mag = P @ V.abs()
+    absdP = dO.abs() @ V.abs().transpose(2, 3)
+    u = BF16_U
+    tol_o = u * O.abs() + (u + e) * mag
+    dD = ((u + e) * (dO.abs() * (O.abs() + mag))).sum(-1, keepdim=True)
+    tol_s = u * dS.abs() + e * P * (dP.abs() + D.abs()) + P * (acc * absdP + dD)
+    sums = LAM * math.sqrt(lq * G + lk) * U32
+    tol_q = u * dQ.abs() + scale * ((tol_s + sums * dS.abs()) @ K.abs())
+    tol_k = u * dK.abs() + fold(scale * ((tol_s + sums * dS.abs()).transpose(2, 3) @ Q.abs()))
+    tol_v = u * dV.abs() + fold(((u + e + sums) * P).transpose(2, 3) @ dO.abs())
+    return (O, dQ, dK, dV), (tol_o, tol_q, tol_k, tol_v)
+
+
+def _check(got, q, k, v, do, window, sinks, lengths, scale, names="o dq dk dv"):
+    refs, tols = _reference(q, k, v, do, window, sinks, lengths, scale)
+    for name, a, r, t in zip(names.split(), got, refs, tols):
+        _within(a.detach().cpu(), r, t, name)
+
+
+CASES = [
+    # b, heads, kv, lq, lk, hd, window, sinks, lengths
+    (1, 1, 1, 1, 1, 8, None, 0, None),
+    (2, 3, 1, 33, 33, 24, None, 0, None),          # heads that share keys, half a tile
+    (2, 4, 2, 65, 65, 64, 7, 3, None),             # a tile and one row
+    (1, 2, 2, 300, 300, 128, 64, 70, None),        # more sinks than a tile and than the window
+    (1, 2, 1, 513, 513, 96, 1, 0, None),           # each row sees itself
+    (1, 6, 2, 700, 700, 64, 129, 1, None),         # sinks' tile apart from the window's
+    (1, 1, 1, 1100, 1100, 128, 200, 130, None),
+    (2, 2, 1, 130, 257, 96, 50, 1, [257, 40]),     # rows before a short sequence's start see nothing
+    (2, 2, 2, 300, 20, 64, None, 0, [20, 0]),      # more rows than keys; no key at all
+    (3, 8, 2, 1, 1000, 64, None, 0, [1000, 0, 1]), # single tokens over a cache
+    (2, 4, 4, 5, 777, 80, 100, 4, [777, 300]),     # a few drafted tokens
+    (1, 32, 1, 4, 2049, 128, None, 0, None),       # 128 rows share keys
+    (2, 8, 2, 40, 3000, 64, 513, 9, [2999, 1024]),
+]
+
+
+@pytest.mark.parametrize("case", CASES, ids=str)
+def test_attention(monkeypatch, case):
+    b, heads, kv, lq, lk, hd, window, sinks, lengths = case
+    _kernel_ran(monkeypatch)
+    q = _rand(b, heads, lq, hd, seed=1).requires_grad_(True)
+    k, v = (_rand(b, kv, lk, hd, seed=s).requires_grad_(True) for s in (2, 3))
+    do = _rand(b, heads, lq, hd, seed=4)
+    n = None if lengths is None else torch.tensor(lengths, device=dev())
+    scale = hd ** -0.5
+    o = F.window_attention(q, k, v, window=window, sinks=sinks, lengths=n)
+    grads = torch.autograd.grad(o, (q, k, v), do)
+    _check((o, *grads), q, k, v, do, window, sinks, n, scale)
+    # the other form of the forward, and the same again: bitwise
+    again = F.window_attention(q, k, v, window=window, sinks=sinks, lengths=n)
+    assert torch.equal(o, again)
+    for x, y in zip(grads, torch.autograd.grad(again, (q, k, v), do)):
+        assert torch.equal(x, y)
+    splits = F.attention_splits(b, heads, kv, lq, lk, F.NO_WINDOW if window is None else window, sinks)
+    monkeypatch.setattr(F, "attention_splits", lambda *a: 3 if splits == 0 else 0)
+    _check((F.window_attention(q, k, v, window=window, sinks=sinks, lengths=n),), q, k, v, do, window, sinks, n, scale, "o")
+
+
+@pytest.mark.parametrize("scale", [0.01, 3.0])
+def test_attention_sharp_and_flat(scale):
+    """Scores of up to some hundreds: the running maximum moves, one key takes all."""
+    q, k, v, do = (_rand(1, 2, 200, 64, seed=s, scale=1.5) for s in range(4))
+    q, k, v = (t.requires_grad_(True) for t in (q, k, v))
+    o = F.window_attention(q, k, v, window=150, sinks=2, scale=scale)
+    _check((o, *torch.autograd.grad(o, (q, k, v), do)), q, k, v, do, 150, 2, None, scale)
+
+
+def test_attention_strides():
+    """Slices of one buffer, other orders, rows off the 16-byte boundary, one head for all, one sequence for all."""
+    b, l, h, hd = 2, 70, 4, 64
+    buf = _rand(b, l, 3, h, hd)
+    q, k, v = (t.transpose(1, 2) for t in buf.unbind(2))
+    do = _rand(b, h, l, hd, seed=5)
+
+    def run(*t):
+        t = [x.detach().requires_grad_(True) for x in t]
+        o = F.window_attention(*t, window=30, sinks=2)
+        return [o, *torch.autograd.grad(o, t, do)]
+
+    plain = run(*(t.contiguous() for t in (q, k, v)))
+    off = torch.empty(q.numel() + 3, dtype=torch.bfloat16, device=dev())[3:].view(q.shape).copy_(q)
+    wide = torch.zeros(b, h, l, hd + 4, dtype=torch.bfloat16, device=dev())
+    wide[..., :hd] = k
+    for t in ((q, k, v), (off, wide[..., :hd], v), (q.contiguous(), k, v.permute(2, 0, 1, 3).contiguous().permute(1, 2, 0, 3))):
+        for x, y in zip(run(*t), plain):
+            assert torch.equal(x, y)
+    one = [t[:1, :1].expand(b, 1, l, hd) for t in (k, v)]
+    for x, y in zip(run(q, *one), run(q, *(t.contiguous() for t in one))):
+        assert torch.equal(x, y)
+    # the gradient as the sum over the broadcast
+    kk, vv = k[:1, :1].detach().clone().requires_grad_(True), v[:1, :1].detach().clone().requires_grad_(True)
+    o = F.window_attention(q, kk.expand(b, 1, l, hd), vv.expand(b, 1, l, hd), window=30, sinks=2)
+    gk, gv = torch.autograd.grad(o, (kk, vv), do)
+    full = run(q, *one)
+    assert torch.equal(gk, full[2].sum(0, keepdim=True)) and torch.equal(gv, full[3].sum(0, keepdim=True))
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
+def test_attention_of_what_is_not_seen(hd, value):
+    """Keys past a length, outside the window and ahead hold anything: the rows that do not
+    see them, and those rows' gradients, are as if it were not there."""
+    b, h, l = 2, 2, 200
+    q, k, v, do = (_rand(b, h, l, hd, seed=s) for s in range(4))
+    lengths = torch.tensor([l, 150], device=dev())
+    rule = dict(window=20, sinks=2, lengths=lengths)
+    seen = F._visible(l, l, lengths, 20, 2, dev())
+    for lq in (l, 3):  # either form of the forward
+        clean = F.window_attention(q[:, :, -lq:], k, v, **rule)
+        bk, bv = k.clone(), v.clone()
+        bk[:, :, 100], bv[:, :, 100] = value, value
+        bk[1, :, 150:], bv[1, :, 150:] = value, value
+        o = F.window_attention(q[:, :, -lq:], bk, bv, **rule)
+        hit = seen[:, :, -lq:, 100].expand(b, h, lq)
+        assert bool((~hit).any()) and torch.equal(o[~hit], clean[~hit])
+        if lq == l:
+            assert bool(hit.any()) and not torch.isfinite(o[hit]).any()
+    # gradients: a value in one row's gradient or query, or one key
+    def grads(q, k, v, do):
+        t = [x.clone().requires_grad_(True) for x in (q, k, v)]
+        return torch.autograd.grad(F.window_attention(*t, window=20, sinks=2), t, do)
+
+    base = grads(q, k, v, do)
+    sees = F._visible(l, l, None, 20, 2, dev())[0, 0]  # (row, key)
+    bd = do.clone()
+    bd[:, :, 90] = value
+    for x, y, touched in zip(grads(q, k, v, bd), base, (torch.arange(l, device=dev()) == 90, sees[90], sees[90])):
+        assert torch.equal(x[:, :, ~touched], y[:, :, ~touched])
+    bk = k.clone()
+    bk[:, :, 90] = value
+    rows = sees[:, 90]                     # rows whose scores it enters
+    keys = sees[rows].any(0)               # keys those rows see
+    for x, y, touched in zip(grads(q, bk, v, do), base, (rows, keys, keys)):
+        assert torch.equal(x[:, :, ~touched], y[:, :, ~touched])
+
+
+def test_attention_offsets_past_32_bits():
+    """Keys 2^26 elements apart: the last ones past 2^31."""
+    if torch.cuda.get_device_properties(0).total_memory < 32 << 30:
+        pytest.skip("memory")
+    lk, apart, hd = 40, 1 << 26, 64
+    buf = torch.empty(lk * apart, dtype=torch.bfloat16, device=dev())
+    k, v = (buf[o:].as_strided((1, 1, lk, hd), (0, 0, apart, 1)) for o in (0, hd))
+    k.copy_(_rand(1, 1, lk, hd, seed=1))
+    v.copy_(_rand(1, 1, lk, hd, seed=2))
+    for lq in (1, 40):
+        q, do = _rand(1, 4, lq, hd, seed=3).requires_grad_(True), _rand(1, 4, lq, hd, seed=4)
+        a, c = (F.window_attention(q, *t, window=30, sinks=1) for t in ((k, v), (k.contiguous(), v.contiguous())))
+        assert torch.equal(a, c)
+    kk, vv = k.detach().requires_grad_(True), v.detach().requires_grad_(True)
+    g = torch.autograd.grad(F.window_attention(q, kk, vv, window=30, sinks=1), (q, kk, vv), do)
+    kk, vv = (t.detach().contiguous().requires_grad_(True) for t in (k, v))
+    for x, y in zip(g, torch.autograd.grad(F.window_attention(q, kk, vv, window=30, sinks=1), (q, kk, vv), do)):
+        assert torch.equal(x, y)
+
+
+def test_attention_routes():
+    """What the kernels do not take is torch's, with the same results within bf16."""
+    q, k, v, do = (_rand(1, 2, 40, 64, seed=s) for s in range(4))
+    o = F.window_attention(q, k, v, window=9)
+    for t in (torch.float32, torch.float64):
+        y = F.window_attention(*(x.to(t) for x in (q, k, v)), window=9)
+        assert y.dtype == t and (y - o).abs().max() <= 4 * BF16_U * v.abs().max()
+    assert F.window_attention(*(_rand(1, 1, 5, 12, seed=s) for s in range(3))).shape == (1, 1, 5, 12)    # odd heads
+    assert F.window_attention(*(_rand(1, 1, 5, 136, seed=s) for s in range(3))).shape == (1, 1, 5, 136)  # wide ones
+    assert F.window_attention(q[:, :, :0], k, v).shape == (1, 2, 0, 64)
+    assert torch.equal(F.window_attention(q, k[:, :, :0], v[:, :, :0]), torch.zeros_like(q))
+    # a recorded backward, and second derivatives through it
+    t = [x.clone().requires_grad_(True) for x in (q, k, v)]
+    first = torch.autograd.grad(F.window_attention(*t, window=9), t, do)
+    recorded = torch.autograd.grad(F.window_attention(*t, window=9), t, do, create_graph=True)
+    for x, y in zip(first, recorded):
+        assert (x.double() - y.double()).norm() <= 4 * BF16_U * y.double().norm()
+    torch.autograd.grad(sum(x.float().sum() for x in recorded), t)
+    # q alone, k alone
+    for i in range(3):
+        t = [x.clone().requires_grad_(i == j) for j, x in enumerate((q, k, v))]
+        (g,) = torch.autograd.grad(F.window_attention(*t, window=9), t[i], do)
+        assert torch.equal(g, first[i])
+
+
+def test_attention_against_differences():
+    """The directional derivative of the fp64 loss by differences, against the kernel's gradient."""
+    q, k, v, do = (_rand(1, 2, 150, 64, seed=s) for s in range(4))
+    t = [x.clone().requires_grad_(True) for x in (q, k, v)]
+    grads = torch.autograd.grad(F.window_attention(*t, window=40, sinks=3), t, do)
+    loss = lambda a, c, d: (F.window_attention(a, c, d, window=40, sinks=3) * do.double()).sum()
+    X, h = [x.double() for x in (q, k, v)], 1e-5
+    for i in range(3):
+        u = _rand(*X[i].shape, seed=9 + i, dtype=torch.float64)
+        moved = [[x + (s * h * u if j == i else 0) for j, x in enumerate(X)] for s in (1, -1)]
+        diff = (loss(*moved[0]) - loss(*moved[1])) / (2 * h)
+        # the gradient's error is at most some roundings of it, in a random direction's inner product
+        assert abs(diff - (grads[i].double() * u).sum()) <= 4 * BF16_U * grads[i].double().norm() * LAM
+
+
+# ----------------------------- distillation ---------------------------------
+
+def _distill_inputs(rows, V, K, dtype, ids_dtype=torch.int64):
+    x = _rand(rows, V, scale=2.0, dtype=dtype)
+    g = torch.Generator(device=dev()).manual_seed(rows + V + K)
+    ids = torch.rand(rows, V, generator=g, device=dev()).argsort(1)[:, :K]
+    top = _rand(rows, K, scale=2.0, seed=3, dtype=dtype)
+    t = torch.randint(V, (rows,), generator=g, device=dev())
+    if rows > 5:
+        t[1] = ops.IGNORE
+        ids[2] = -1               # no entry
+        ids[3, K // 2:] = -1      # some
+        ids[4] = ids[4, 0]        # all of one id
+        top[5, 0] = -math.inf
+        t[4], t[5] = ids[4, 0], V - 1
+        ids[0, 0], t[0] = V - 1, 0
+        with torch.no_grad():
+            x[0, V // 2], x[5, V // 3] = -3.3895e38, -math.inf  # bf16's lowest value
+    return x, top, ids.to(ids_dtype), t
+
+
+def _distill_check(x, top, ids, t, T, w, loss, grad, dloss=1.0):
+    X = x.detach().double().requires_grad_(True)
+    ref = F._distill_torch(X, top.double(), ids, t, T, w)
+    (G,) = torch.autograd.grad(ref, X, torch.tensor(dloss, dtype=torch.float64, device=dev()))
+    assert loss.dtype == torch.float32 and loss.dim() == 0
+    # each row's terms are fp32 numbers of the logits' range (a teacher that names bf16's lowest value makes it wide)
+    span = 64.0 * (1 + w * T) + abs(ref.item())
+    assert abs(loss.item() - ref.item()) <= 2.0 ** -20 * span
+    n = len(x) if t is None else int((t != ops.IGNORE).sum())
+    # probabilities to 2^-17 of themselves, differences of probabilities of at most w T + 1 - w
+    P = w * T * torch.softmax(X.detach() / T, -1) + (1 - w) * torch.softmax(X.detach(), -1)
+    mag = (P + (P - G.abs() * n / max(abs(dloss), 1e-30)).abs()) * abs(dloss) / n
+    tol = (BF16_U if x.dtype == torch.bfloat16 else 4 * U32) * G.abs() + 2.0 ** -17 * (mag + G.abs())
+    _within(grad, G, tol + 2.0 ** -126)
+
+
+@pytest.mark.parametrize("rows,V,K,dtype", [
+    (1, 1, 1, torch.bfloat16), (7, 7, 3, torch.bfloat16), (9, 1003, 8, torch.float32), (9, 1001, 64, torch.bfloat16),
+    (33, 8192, 5, torch.bfloat16), (20, 12301, 300, torch.bfloat16), (20, 32000, 64, torch.bfloat16),
+    (8, 20001, 1000, torch.float32), (6, 131072, 7, torch.bfloat16), (6, 150001, 9, torch.bfloat16),
+    (6, 70001, 16, torch.float32)])
+@pytest.mark.parametrize("T,w,with_targets", [(1.0, 1.0, False), (2.0, 0.5, True), (0.7, 1.0, True), (1.0, 0.25, True),
+                                             (3.0, 0.0, True)])
+def test_distill(monkeypatch, rows, V, K, dtype, T, w, with_targets):
+    x, top, ids, t = _distill_inputs(rows, V, K, dtype, torch.int32 if K == 8 else torch.int64)
+    t = t if with_targets else None
+    expect = F._distill_torch
+    x.requires_grad_(True)
+    with monkeypatch.context() as m:
+        _kernel_ran(m)
+        loss = F.distill_loss(x, top, ids, targets=t, temperature=T, weight=w)
+        (g,) = torch.autograd.grad(loss, x, retain_graph=True)
+        (again,) = torch.autograd.grad(loss, x, retain_graph=True)   # the second time formed anew
+        assert torch.equal(g, again) and g.data_ptr() != again.data_ptr()
+        (third,) = torch.autograd.grad(loss, x, torch.tensor(3.0, device=dev()))
+        with torch.no_grad():
+            assert torch.equal(F.distill_loss(x, top, ids, targets=t, temperature=T, weight=w), loss)
+        loss3 = F.distill_loss(x, top, ids, targets=t, temperature=T, weight=w)
+        (g3,) = torch.autograd.grad(3.0 * loss3, x)                  # the first time, of another dloss
+        assert torch.equal(third, g3)
+    _distill_check(x, top, ids, t, T, w, loss, g)
+    _distill_check(x, top, ids, t, T, w, loss, g3, 3.0)
+    if with_targets and rows > 5:
+        assert torch.equal(g[1], torch.zeros_like(g[1]))
+
+
+def test_distill_not_finite_and_empty_mean(monkeypatch):
+    _kernel_ran(monkeypatch)
+    x, top, ids, t = _distill_inputs(8, 500, 4, torch.float32)
+
+    def run(x, top, ids, t, w=0.5):
+        x = x.clone().requires_grad_(True)
+        loss = F.distill_loss(x, top, ids, targets=t, weight=w)
+        return loss, torch.autograd.grad(loss, x)[0]
+
+    loss, g = run(x, top, ids, t)
+    # a row that does not count holds anything
+    bx, bt = x.clone(), top.clone()
+    bx[1], bt[1] = math.nan, math.inf
+    for a, c in zip(run(bx, bt, ids, t), (loss, g)):
+        assert torch.equal(a, c)
+    for bad in (math.nan, math.inf):
+        bx = x.clone()
+        bx[6, 3] = bad
+        l, d = run(bx, top, ids, t)
+        assert l.isnan() and d[6].isnan().all() and torch.equal(d[:6], g[:6])
+    for i, c in ((ids.clone(), t.clone()), (ids.clone(), t.clone())):
+        (i if c is t else i)[7, 1] = 500
+        l, d = run(x, top, i, c)
+        assert l.isnan() and d[7].isnan().all() and torch.equal(d[:7], g[:7])
+    c = t.clone()
+    c[7] = 500
+    l, d = run(x, top, ids, c)
+    assert l.isnan() and d[7].isnan().all()
+    l, d = run(x, top, ids, torch.full_like(t, ops.IGNORE))
+    assert l.isnan() and torch.equal(d, torch.zeros_like(d))
+    # a student without a logit where the teacher has some
+    bx = x.clone()
+    bx[6, ids[6, 0]] = -math.inf
+    l, d = run(bx, top, ids, None, 1.0)
+    assert torch.isposinf(l) and d[6].isfinite().all()
+
+
+def test_distill_routes():
+    x, top, ids, t = _distill_inputs(8, 500, 4, torch.bfloat16)
+    loss = F.distill_loss(x, top, ids, targets=t, weight=0.5)
+    wide = torch.zeros(8, 504, dtype=x.dtype, device=dev())
+    wide[:, :500] = x
+    assert torch.equal(F.distill_loss(wide[:, :500], top, ids, targets=t, weight=0.5), loss)
+    off = torch.empty(x.numel() + 1, dtype=x.dtype, device=dev())[1:].view(8, 500).copy_(x)
+    assert torch.equal(F.distill_loss(off, top, ids, targets=t, weight=0.5), loss)
+    more = torch.cat((top, top), 1), torch.cat((ids, -torch.ones_like(ids)), 1)
+    assert torch.equal(F.distill_loss(x, more[0][:, :4], more[1][:, :4], targets=t, weight=0.5), loss)
+    assert torch.equal(F.distill_loss(x, top.t().contiguous().t(), ids.t().contiguous().t(), targets=t, weight=0.5), loss)
+    for y in (F.distill_loss(x.double(), top.double(), ids, targets=t, weight=0.5),
+              F.distill_loss(x.float(), top.float(), ids, targets=t, weight=0.5)):
+        assert abs(y.item() - loss.item()) <= 1e-4
+    # the teacher's gradient, recorded backwards, many entries: torch's
+    s = top.float().requires_grad_(True)
+    F.distill_loss(x, s, ids, targets=t, weight=0.5).backward()
+    assert s.grad.abs().sum() > 0
+    z = x.float().requires_grad_(True)
+    (g,) = torch.autograd.grad(F.distill_loss(z, top, ids), z, create_graph=True)
+    torch.autograd.grad(g.square().sum(), z)
+    many = torch.arange(1100, device=dev()).expand(8, 1100) % 500
+    assert torch.isposinf(F.distill_loss(x, torch.zeros(8, 1100, device=dev()), many))  # (x[5, 166] is -inf)
+    assert F.distill_loss(x[:5], torch.zeros(5, 1100, device=dev()), many[:5]).isfinite()
+
+
+def test_distill_against_differences():
+    x, top, ids, t = _distill_inputs(16, 300, 5, torch.float32)
+    x = x.clamp(min=-20).requires_grad_(True)
+    (g,) = torch.autograd.grad(F.distill_loss(x, top, ids, targets=t, temperature=2.0, weight=0.5), x)
+    u, h, X = _rand(16, 300, seed=5, dtype=torch.float64), 1e-5, x.detach().double()
+    f = lambda a: F.distill_loss(a, top.double(), ids, targets=t, temperature=2.0, weight=0.5)
+    diff = (f(X + h * u) - f(X - h * u)) / (2 * h)
+    assert abs(diff - (g.double() * u).sum()) <= 2.0 ** -16 * g.double().norm() * LAM
+
+
+# ------------------------------- together -----------------------------------
+
+def _model(**kw):
+    torch.manual_seed(0)
+    rope = F.Rotary(64, scaling="parts", factor=2.0, original_length=64)
+    return blk.LlamaModel(512, 128, 2, 344, 2, rank=32, rope=rope, window=48, sinks=2, **kw)
+
+
+def test_model_learns_from_a_teacher(monkeypatch):
+    """Rotary positions, window and teacher in one training run, on the kernels alone."""
+    model = _model()
+    _kernel_ran(monkeypatch)
+    opts = blk.make_optimizers(model, lr=3e-3)
+    g = torch.Generator(device=dev()).manual_seed(0)
+    tokens = torch.randint(512, (4, 129), generator=g, device=dev())
+    top, ids = 4 * torch.rand(4, 128, 8, generator=g, device=dev()), torch.randint(512, (4, 128, 8), generator=g, device=dev())
+    ids[..., 0] = tokens[:, 1:]
+    losses = []
+    for _ in range(60):
+        for o in opts:
+            o.zero_grad()
+        loss = model(tokens[:, :-1], tokens[:, 1:], teacher=(top, ids), temperature=2.0, weight=0.5)
+        loss.backward()
+        for o in opts:
+            o.step()
+        losses.append(loss.item())
+    assert all(map(math.isfinite, losses)) and losses[-1] < 0.5 * losses[0]
+
+
+def test_block_gradients_of_the_window():
+    """A block's gradients with the kernels, against the same block whose attention and
+    rotation are the torch expressions."""
+    torch.manual_seed(0)
+    b = blk.LlamaBlock(128, 2, 256, rope=F.Rotary(32), window=20, sinks=1)
+    x = _rand(2, 100, 128).requires_grad_(True)
+    dy = _rand(2, 100, 128, seed=1)
+    params = [x, *b.parameters()]
+    got = torch.autograd.grad(b(x), params, dy)
+    usable, F._attention_usable = F._attention_usable, lambda *a: False
+    rotary, F.Rotary._usable = F.Rotary._usable, lambda *a: False
+    try:
+        ref = torch.autograd.grad(b(x), params, dy)
+    finally:
+        F._attention_usable, F.Rotary._usable = usable, rotary
+    for a, r in zip(got, ref):
+        assert (a.double() - r.double()).norm() <= 8 * BF16_U * r.double().norm()
+
+
+def test_other_streams_and_graphs():
+    """On a stream of the caller's, and replayed from a graph: the same, each time."""
+    rope = F.Rotary(64)
+    qkv = _rand(2, 130, 3, 2, 64).requires_grad_(True)
+    do = _rand(2, 2, 130, 64, seed=2)
+    x, top, ids, t = _distill_inputs(16, 1000, 4, torch.bfloat16)
+    x.requires_grad_(True)
+
+    def step():
+        q, k, v = F.rotary_split_qkv(qkv * 1, rope)
+        o = F.window_attention(q, k, v, window=40, sinks=1)
+        one = F.window_attention(q[:, :, -1:], k, v, window=40, sinks=1)
+        loss = F.distill_loss(x, top, ids, targets=t, weight=0.5)
+        return [o, one, loss, *torch.autograd.grad((o, loss), (qkv, x), (do, torch.ones_like(loss)))]
+
+    ref = [r.detach().clone() for r in step()]
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        for _ in range(2):
+            out = step()
+    torch.cuda.current_stream().wait_stream(s)
+    for a, r in zip(out, ref):
+        assert torch.equal(a, r)
+    del out
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for _ in range(3):
+        for a in out:
+            a.detach().zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, r in zip(out, ref):
+            assert torch.equal(a, r)
+        step()
