@@ -26,6 +26,7 @@ namespace {
 
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
+typedef __attribute__((address_space(3))) void lds_void;
 
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr int kBN = 64;  // keys (or queries) per staged tile
@@ -67,7 +68,27 @@ struct Tile {
   }
 };
 
-// This thread's chunks of a tile on their way from memory to LDS: rows j0 .. j0 + ROWS - 1 of
+// What a tile's values become on their way into LDS.  A value that is infinite or NaN meets
+// factors of zero in the rows that do not see it, and 0 x inf must stay 0 there.  The kernels
+// form their products plainly and look at their sums at the end, where such a NaN cannot
+// hide; only then they do their work again:
+//   kClean     such values as zeros
+//   kPos, kNeg 1 where the value is +inf or NaN, -inf or NaN, else 0
+enum Values { kPlain, kClean, kPos, kNeg };
+
+__device__ __forceinline__ uint32_t value_pair(uint32_t w, int mode) {
+  uint32_t out = 0;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const uint32_t x = (w >> (16 * h)) & 0xFFFFu;
+    const bool bad = (x & 0x7F80u) == 0x7F80u, nan = bad && (x & 0x7Fu) != 0;
+    const bool one = nan || x == (mode == kPos ? 0x7F80u : 0xFF80u);
+    out |= (mode == kClean ? (bad ? 0u : x) : one ? 0x3F80u : 0u) << (16 * h);
+  }
+  return out;
+}
+
+// This wave's chunks of a tile on their way from memory to LDS: rows j0 .. j0 + ROWS - 1 of
 // a matrix, rows at or past `rows` and columns at or past hd as zeros.
 template <int HD, int ROWS, int THREADS>
 struct Stage {
@@ -88,7 +109,74 @@ struct Stage {
       *reinterpret_cast<u32x4*>(t + Tile<HD>::at(idx / (HD / 8), idx % (HD / 8))) = w[i];
     }
   }
+  // bad[r] = 1 for a row r with an infinity or NaN
+  __device__ __forceinline__ void convert(int mode, int* bad, int tid) {
+#pragma unroll
+    for (int i = 0; i < kN; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t x = value_pair(w[i][e], mode);
+        if (bad != nullptr && x != w[i][e]) bad[(tid + THREADS * i) / (HD / 8)] = 1;
+        w[i][e] = x;
+      }
+  }
 };
+
+// A tile's way into LDS without registers: each wave copies kN blocks of 1 KB, lane after lane
+// 16 bytes, fetching for each place of the tile the chunk that belongs there.  Rows at or past
+// `rows` and columns at or past hd read as zeros (the buffer's range check).  A tile's bytes
+// lie within 2^31 (row strides below kMaxStride), the tile's own start is a 64-bit address.
+constexpr int64_t kMaxStride = (int64_t(1) << 24) - 512;
+
+template <int HD>
+struct Copy {
+  static constexpr int kN = Tile<HD>::kBytes / 1024 / 4;
+  int off[kN];
+  __device__ __forceinline__ void init(int64_t stride, int hd, int tid) {
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      const int idx = ((tid >> 6) * kN + i) * 64 + (tid & 63), r = idx / (HD / 8), c = (idx % (HD / 8)) ^ Tile<HD>::swz(r);
+      off[i] = c * 8 < hd ? r * static_cast<int>(stride) * 2 + c * 16 : 0x7FFFFFF0;
+    }
+  }
+  __device__ __forceinline__ void issue(const uint16_t* base, int64_t stride, int j0, int rows, int hd, char* t, int wave) const {
+    const int n = min(rows - j0, kBN);
+    const int bytes = n > 0 ? ((n - 1) * static_cast<int>(stride) + hd) * 2 : 0;
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<uint16_t*>(base + j0 * stride), static_cast<short>(0), bytes, 0x00020000);
+#pragma unroll
+    for (int i = 0; i < kN; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)(t + (wave * kN + i) * 1024), 16, off[i], 0, 0, 0);
+  }
+};
+
+// kBN fp32 values v[r0 ..] of `rows`, by one wave.
+__device__ __forceinline__ void copy_row_values(const float* v, int r0, int rows, char* t, int lane) {
+  const int n = min(rows - r0, kBN);
+  const __amdgpu_buffer_rsrc_t rs =
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(v + r0), static_cast<short>(0), n > 0 ? n * 4 : 0, 0x00020000);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)t, 4, lane * 4, 0, 0, 0);
+}
+
+// This wave's copies have arrived and its reads are done, and every wave's.
+__device__ __forceinline__ void copies_done() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory"); }
+
+// A tile's values converted where they are; bad[r] = 1 for a row r with an infinity or NaN.
+template <int HD>
+__device__ __forceinline__ void convert_tile(char* t, int mode, int* bad, int tid) {
+#pragma unroll 1
+  for (int idx = tid; idx < kBN * (HD / 8); idx += 256) {
+    u32x4* at = reinterpret_cast<u32x4*>(t + Tile<HD>::at(idx / (HD / 8), idx % (HD / 8)));
+    u32x4 w = *at;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t x = value_pair(w[e], mode);
+      if (bad != nullptr && x != w[e]) bad[idx / (HD / 8)] = 1;
+      w[e] = x;
+    }
+    *at = w;
+  }
+}
 
 // B operand straight from memory: column (row of the matrix) `row`, 8 values 16 s + 8 (lane / 32).
 template <int HD>
@@ -102,7 +190,22 @@ __device__ __forceinline__ void load_frags(u32x4 (&f)[HD / 16], const uint16_t* 
   }
 }
 
-__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, 64); }
+// v of this lane and of the lane in the other half-wave: (lower half's, upper half's).
+__device__ __forceinline__ void both_halves(float v, float& lo, float& hi) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  lo = __uint_as_float(r[0]);
+  hi = __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float halves_max(float v) {
+  float lo, hi;
+  both_halves(v, lo, hi);
+  return fmaxf(lo, hi);
+}
+__device__ __forceinline__ float halves_sum(float v) {
+  float lo, hi;
+  both_halves(v, lo, hi);
+  return lo + hi;
+}
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -124,46 +227,15 @@ __device__ __forceinline__ void pack_steps(const f32x16& p, u32x4 (&out)[2]) {
     for (int w = 0; w < 4; ++w) out[t][w] = pack_bf16x2(p[8 * t + 2 * w], p[8 * t + 2 * w + 1]);
 }
 
-__device__ __forceinline__ bool not_finite(const u32x4& a) {
-  bool bad = false;
+// A sum that met an infinity or NaN.
+template <int N>
+__device__ __forceinline__ bool not_finite(const f32x16 (&acc)[N]) {
+  float z = 0.0f;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) bad |= (a[w] & 0x7F80u) == 0x7F80u || (a[w] & 0x7F800000u) == 0x7F800000u;
-  return bad;
-}
-
-// acc + A B where a value of A may be infinite or NaN beside rows whose factor in B is zero
-// because they do not see it: 0 x inf must stay 0 there.  Such values enter as 1 in products
-// of their own, and wherever those are not zero the result is what the sum would be (`grad`:
-// NaN, as B's sign is not looked at; else the infinity or NaN).
-template <bool GRAD>
-__device__ __forceinline__ f32x16 mfma_seen(const u32x4& a, const u32x4& b, f32x16 acc) {
-  if (!__any(not_finite(a))) return mfma32x32x16(a, b, acc);
-  u32x4 clean, pos, neg, mag;
+  for (int d = 0; d < N; ++d)
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    uint32_t cl = 0, po = 0, ne = 0;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const uint32_t x = (a[w] >> (16 * h)) & 0xFFFFu;
-      const bool bad = (x & 0x7F80u) == 0x7F80u, nan = bad && (x & 0x7Fu) != 0;
-      if (!bad) cl |= x << (16 * h);
-      if (nan || x == 0x7F80u) po |= 0x3F80u << (16 * h);
-      if (nan || x == 0xFF80u) ne |= 0x3F80u << (16 * h);
-    }
-    clean[w] = cl;
-    pos[w] = po;
-    neg[w] = ne;
-    mag[w] = b[w] & 0x7FFF7FFFu;
-  }
-  acc = mfma32x32x16(clean, b, acc);
-  const f32x16 up = mfma32x32x16(pos, mag, zero16()), down = mfma32x32x16(neg, mag, zero16());
-#pragma unroll
-  for (int v = 0; v < 16; ++v) {
-    // (a NaN in B is a NaN in both)
-    if (!(up[v] == 0.0f)) acc[v] += GRAD ? __builtin_nanf("") : __builtin_inff();
-    if (!(down[v] == 0.0f)) acc[v] += GRAD ? __builtin_nanf("") : -__builtin_inff();
-  }
-  return acc;
+    for (int v = 0; v < 16; ++v) z = __builtin_fmaf(acc[d][v], 0.0f, z);
+  return !(z == 0.0f);
 }
 
 // The tiles of TN keys that rows at positions pmin .. pmax (of L keys) see: the sinks' tiles
@@ -186,7 +258,8 @@ struct Walk {
 };
 
 __device__ __forceinline__ bool seen(int j, int p, int window, int sinks) {
-  return j <= p && (p - j < window || j < sinks);
+  // (no short cuts: element by element they would become branches)
+  return (j <= p) & ((p - j < window) | (j < sinks));
 }
 
 // No key of j0 .. j0 + n - 1 is seen from a position in pmin .. pmax / all are from all of them.
@@ -219,6 +292,36 @@ __device__ __forceinline__ void store_rows(const f32x16 (&acc)[HD / 32], float f
     }
 }
 
+template <int HD>
+__device__ __forceinline__ void store_row_values(const f32x16 (&acc)[HD / 32], float f, float* row, int hd, int lane) {
+#pragma unroll
+  for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int c = 32 * d + 8 * g + 4 * (lane >> 5);
+      if (c < hd) {
+        const f32x4 w = {acc[d][4 * g] * f, acc[d][4 * g + 1] * f, acc[d][4 * g + 2] * f, acc[d][4 * g + 3] * f};
+        *reinterpret_cast<f32x4*>(row + c) = w;
+      }
+    }
+}
+
+// Columns of a transposed sum of products with kPos or kNeg values: the rows' elements where it
+// is not zero become what they are with an infinity (of that sign) or NaN in their sum.
+template <int HD, typename T>
+__device__ __forceinline__ void mark_rows(const f32x16 (&acc)[HD / 32], int mode, T* row, int hd, int lane) {
+#pragma unroll
+  for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      const int c = 32 * d + acc_row(v, lane);
+      if (c >= hd || acc[d][v] == 0.0f) continue;
+      const float inf = mode == kPos ? __builtin_inff() : -__builtin_inff();
+      if constexpr (sizeof(T) == 2) row[c] = f32_to_bf16(bf16_to_f32(row[c]) + inf);
+      else row[c] += inf;
+    }
+}
+
 // Running maximum (in units of log2, scaled) and sum of one query column, with its rows of O^T.
 template <int HD>
 struct Softmax {
@@ -231,14 +334,14 @@ struct Softmax {
     l = 0.0f;
   }
   // A new maximum of scaled scores `top` (both halves' own): what was summed so far is scaled.
-  // The reference moves only when a score lies more than 2^8 above it: P <= 256 costs no
-  // accuracy in fp32 sums and bf16 factors, and most tiles leave O alone.
+  // The reference of a row moves only when a score lies more than 2^8 above it: P <= 256 costs
+  // no accuracy in fp32 sums and bf16 factors, and most tiles leave O alone.
   __device__ __forceinline__ void raise(float top) {
-    top = fmaxf(top, other_half(top));
-    if (__any(top > m + 8.0f)) {
-      const float nm = fmaxf(m, top);
-      const float f = nm == -__builtin_inff() ? 1.0f : exp2_fast(m - nm);
-      m = nm;
+    top = halves_max(top);
+    const bool up = top > m + 8.0f;
+    if (__any(up)) {
+      const float f = up ? exp2_fast(m - top) : 1.0f;
+      m = up ? top : m;
       l *= f;
 #pragma unroll
       for (int d = 0; d < HD / 32; ++d)
@@ -250,15 +353,20 @@ struct Softmax {
 };
 
 // ------------------------------- forward ------------------------------------
-// A workgroup of four waves takes 128 NQ queries of one head, NQ columns of 32 per wave.
+// A workgroup of four waves takes 128 NQ queries of one head, NQ columns of 32 per wave, and
+// walks the keys they see in tiles of 64, the next tile's copies in flight under the work on
+// one.  (Each of the two buffers is a variable of its own: so the compiler knows which reads
+// a copy in flight has nothing to do with.)  The work with V's values of `mode`; false: not
+// finite, to be done by modes.
+template <int HD>
+struct TilePair {
+  char k[Tile<HD>::kBytes], v[Tile<HD>::kBytes];
+};
+
 template <int HD, int NQ>
-__global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnArgs a) {
-  constexpr int BM = 128 * NQ, KS = HD / 16;
-  extern __shared__ __attribute__((aligned(16))) char lds[];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int nqb = (a.lq + BM - 1) / BM;
-  const uint32_t id = xcd_remap(blockIdx.x, gridDim.x);
-  const int bh = static_cast<int>(id / nqb), qb = nqb - 1 - static_cast<int>(id % nqb);
+__device__ __forceinline__ bool attn_fwd(const AttnArgs& a, TilePair<HD>& even, TilePair<HD>& odd, int bh, int q0, int mode) {
+  constexpr int KS = HD / 16;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), w0 = q0 + wave * 32 * NQ;
   const int b = bh / a.heads, h = bh % a.heads, hk = h / (a.heads / a.kv);
   const int L = length_of(a, b), off = L - a.lq;
   const uint16_t* q = a.q + b * a.qs[0] + h * a.qs[1];
@@ -266,38 +374,34 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnArgs a) {
   const uint16_t* v = a.v + b * a.vs[0] + hk * a.vs[1];
   const float c = a.scale * kLog2e;
 
-  const int q0 = qb * BM, last = min(a.lq, q0 + BM) - 1;
+  const int last = min(a.lq, q0 + 128 * NQ) - 1;
   const Walk<kBN> walk(q0 + off, last + off, L, a.window, a.sinks);
-  const int w0 = q0 + wave * 32 * NQ;
+  const int pmin = w0 + off, pmax = min(w0 + 32 * NQ - 1, last) + off;
+  Copy<HD> ck, cv;
+  ck.init(a.ks[2], a.hd, tid);
+  cv.init(a.vs[2], a.hd, tid);
+  auto fetch = [&](int t, TilePair<HD>& to) {
+    ck.issue(k, a.ks[2], walk.key(t), L, a.hd, to.k, wave);
+    cv.issue(v, a.vs[2], walk.key(t), L, a.hd, to.v, wave);
+  };
+  if (walk.count > 0) fetch(0, even);
   u32x4 qf[NQ][KS];
   Softmax<HD> sm[NQ];
-  int p[NQ];
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
-    const int row = w0 + 32 * n + (lane & 31);
-    load_frags<HD>(qf[n], q, a.qs[2], row, a.lq, a.hd, lane);
+    load_frags<HD>(qf[n], q, a.qs[2], w0 + 32 * n + (lane & 31), a.lq, a.hd, lane);
     sm[n].init();
-    p[n] = row + off;
   }
-  const int pmin = w0 + off, pmax = min(w0 + 32 * NQ - 1, last) + off;
 
-  Stage<HD, kBN, 256> sk, sv;
-  if (walk.count > 0) {
-    sk.load(k, a.ks[2], walk.key(0), L, a.hd, tid);
-    sv.load(v, a.vs[2], walk.key(0), L, a.hd, tid);
-  }
-  for (int t = 0; t < walk.count; ++t) {
-    char* tk = lds + (t & 1) * 2 * Tile<HD>::kBytes;
-    char* tv = tk + Tile<HD>::kBytes;
-    sk.store(tk, tid);
-    sv.store(tv, tid);
-    __syncthreads();
-    if (t + 1 < walk.count) {
-      sk.load(k, a.ks[2], walk.key(t + 1), L, a.hd, tid);
-      sv.load(v, a.vs[2], walk.key(t + 1), L, a.hd, tid);
+  auto step = [&](int t, TilePair<HD>& now, TilePair<HD>& next) {
+    copies_done();
+    if (t + 1 < walk.count) fetch(t + 1, next);
+    if (mode != kPlain) {
+      convert_tile<HD>(now.v, mode, nullptr, tid);
+      __syncthreads();
     }
     const int j0 = walk.key(t);
-    if (w0 > last || none_seen(j0, kBN, pmin, pmax, a.window, a.sinks)) continue;
+    if (w0 > last || none_seen(j0, kBN, pmin, pmax, a.window, a.sinks)) return;
     f32x16 s[NQ][2];
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
@@ -305,20 +409,20 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnArgs a) {
       for (int n = 0; n < NQ; ++n) s[n][kb] = zero16();
 #pragma unroll
       for (int st = 0; st < KS; ++st) {
-        const u32x4 kf = Tile<HD>::row_frag(tk, 32 * kb, st, lane);
+        const u32x4 kf = Tile<HD>::row_frag(now.k, 32 * kb, st, lane);
 #pragma unroll
         for (int n = 0; n < NQ; ++n) s[n][kb] = mfma32x32x16(kf, qf[n][st], s[n][kb]);
       }
     }
-    const bool edge = !all_seen(j0, kBN, pmin, pmax, a.window, a.sinks);
-    if (edge) {
+    if (!all_seen(j0, kBN, pmin, pmax, a.window, a.sinks)) {
 #pragma unroll
       for (int n = 0; n < NQ; ++n)
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
           for (int e = 0; e < 16; ++e)
-            if (!seen(j0 + 32 * kb + acc_row(e, lane), p[n], a.window, a.sinks)) s[n][kb][e] = -__builtin_inff();
+            s[n][kb][e] = seen(j0 + 32 * kb + acc_row(e, lane), w0 + 32 * n + (lane & 31) + off, a.window, a.sinks)
+                              ? s[n][kb][e] : -__builtin_inff();
     }
     u32x4 pf[NQ][4];
 #pragma unroll
@@ -347,24 +451,49 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnArgs a) {
     for (int st = 0; st < 4; ++st)
 #pragma unroll
       for (int d = 0; d < HD / 32; ++d) {
-        const u32x4 vf = Tile<HD>::col_frag(tv, 16 * st, d, lane);
-        if (edge) {
+        const u32x4 vf = Tile<HD>::col_frag(now.v, 16 * st, d, lane);
 #pragma unroll
-          for (int n = 0; n < NQ; ++n) sm[n].o[d] = mfma_seen<false>(vf, pf[n][st], sm[n].o[d]);
-        } else {
-#pragma unroll
-          for (int n = 0; n < NQ; ++n) sm[n].o[d] = mfma32x32x16(vf, pf[n][st], sm[n].o[d]);
-        }
+        for (int n = 0; n < NQ; ++n) sm[n].o[d] = mfma32x32x16(vf, pf[n][st], sm[n].o[d]);
       }
+  };
+  for (int t = 0; t < walk.count; t += 2) {
+    step(t, even, odd);
+    if (t + 1 < walk.count) step(t + 1, odd, even);
+  }
+  if (mode == kPlain) {
+    bool bad = false;
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) bad |= not_finite(sm[n].o);
+    if (__syncthreads_or(bad)) return false;
   }
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
     const int row = w0 + 32 * n + (lane & 31);
-    const float l = sm[n].l + other_half(sm[n].l);
+    const float l = halves_sum(sm[n].l);
     if (row >= a.lq) continue;
+    uint16_t* out = a.o + b * a.os[0] + h * a.os[1] + row * a.os[2];
+    if (mode >= kPos) {
+      mark_rows<HD>(sm[n].o, mode, out, a.hd, lane);
+      continue;
+    }
     const bool empty = sm[n].m == -__builtin_inff() && l == 0.0f;
-    store_rows<HD>(sm[n].o, empty ? 0.0f : 1.0f / l, a.o + b * a.os[0] + h * a.os[1] + row * a.os[2], a.hd, lane);
+    store_rows<HD>(sm[n].o, empty ? 0.0f : 1.0f / l, out, a.hd, lane);
     if (lane < 32) a.lse[int64_t(bh) * a.lq + row] = empty ? __builtin_inff() : sm[n].m + log2f(l);
+  }
+  return true;
+}
+
+template <int HD, int NQ, int WAVES>
+__global__ __launch_bounds__(256, WAVES) void k_attn_fwd(AttnArgs a) {
+  constexpr int BM = 128 * NQ;
+  __shared__ __attribute__((aligned(16))) TilePair<HD> even, odd;
+  const int nqb = (a.lq + BM - 1) / BM;
+  const uint32_t id = xcd_remap(blockIdx.x, gridDim.x);
+  const int bh = static_cast<int>(id / nqb), q0 = (nqb - 1 - static_cast<int>(id % nqb)) * BM;
+#pragma unroll 1
+  for (int mode = kPlain; mode <= kNeg; ++mode) {
+    if (attn_fwd<HD, NQ>(a, even, odd, bh, q0, mode) && mode == kPlain) break;
+    __syncthreads();
   }
 }
 
@@ -373,14 +502,10 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnArgs a) {
 // are the columns of one wave, and each wave takes a range of the keys on its own, K straight
 // from memory as the A operand, V through its own part of LDS.
 template <int HD>
-__global__ __launch_bounds__(256) void k_attn_split(AttnArgs a) {
+__device__ __forceinline__ bool attn_split(const AttnArgs& a, char* tv, int split, int r0, int b, int hk, int mode) {
   constexpr int KS = HD / 16, TN = 32;
-  extern __shared__ __attribute__((aligned(16))) char lds[];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int lane = threadIdx.x & 63;
   const int G = a.heads / a.kv, R = G * a.lq;
-  const int split = static_cast<int>(blockIdx.x) * 4 + wave, r0 = static_cast<int>(blockIdx.y) * 32;
-  const int b = static_cast<int>(blockIdx.z) / a.kv, hk = static_cast<int>(blockIdx.z) % a.kv;
-  if (split >= a.splits) return;
   const int L = length_of(a, b), off = L - a.lq;
   const uint16_t* k = a.k + b * a.ks[0] + hk * a.ks[1];
   const uint16_t* v = a.v + b * a.vs[0] + hk * a.vs[1];
@@ -399,7 +524,6 @@ __global__ __launch_bounds__(256) void k_attn_split(AttnArgs a) {
   load_frags<HD>(qf, a.q + b * a.qs[0] + (hk * G + g) * a.qs[1], a.qs[2], r < R ? i : a.lq, a.lq, a.hd, lane);
   Softmax<HD> sm;
   sm.init();
-  char* tv = lds + wave * (TN * HD * 2);
   u32x4 kf[KS], kn[KS];
   Stage<HD, TN, 64> sv;
   if (t0 < t1) {
@@ -410,6 +534,7 @@ __global__ __launch_bounds__(256) void k_attn_split(AttnArgs a) {
     const int j0 = walk.key(t);
 #pragma unroll
     for (int s = 0; s < KS; ++s) kf[s] = kn[s];
+    if (mode != kPlain) sv.convert(mode, nullptr, lane);
     sv.store(tv, lane);
     if (t + 1 < t1) {
       load_frags<HD>(kn, k, a.ks[2], walk.key(t + 1) + (lane & 31), L, a.hd, lane);
@@ -418,11 +543,10 @@ __global__ __launch_bounds__(256) void k_attn_split(AttnArgs a) {
     f32x16 s = zero16();
 #pragma unroll
     for (int st = 0; st < KS; ++st) s = mfma32x32x16(kf[st], qf[st], s);
-    const bool edge = !all_seen(j0, TN, pmin, pmax, a.window, a.sinks);
-    if (edge) {
+    if (!all_seen(j0, TN, pmin, pmax, a.window, a.sinks)) {
 #pragma unroll
       for (int e = 0; e < 16; ++e)
-        if (!seen(j0 + acc_row(e, lane), p, a.window, a.sinks)) s[e] = -__builtin_inff();
+        s[e] = seen(j0 + acc_row(e, lane), p, a.window, a.sinks) ? s[e] : -__builtin_inff();
     }
     float top = s[0];
 #pragma unroll
@@ -441,26 +565,35 @@ __global__ __launch_bounds__(256) void k_attn_split(AttnArgs a) {
 #pragma unroll
       for (int d = 0; d < HD / 32; ++d) {
         const u32x4 vf = Tile<HD>::col_frag(tv, 16 * st, d, lane);
-        sm.o[d] = edge ? mfma_seen<false>(vf, pf[st], sm.o[d]) : mfma32x32x16(vf, pf[st], sm.o[d]);
+        sm.o[d] = mfma32x32x16(vf, pf[st], sm.o[d]);
       }
   }
-  const float l = sm.l + other_half(sm.l);
-  if (r >= R) return;
+  if (mode == kPlain && __any(not_finite(sm.o))) return false;
+  const float l = halves_sum(sm.l);
+  if (r >= R) return true;
   const int64_t row = (int64_t(b) * a.heads + hk * G + g) * a.lq + i, rows = int64_t(a.b) * a.heads * a.lq;
+  float* out = a.part_o + (split * rows + row) * a.hd;
+  if (mode >= kPos) {
+    mark_rows<HD>(sm.o, mode, out, a.hd, lane);
+    return true;
+  }
   const bool empty = sm.m == -__builtin_inff() && l == 0.0f;
   if (lane < 32) a.part_lse[split * rows + row] = empty ? -__builtin_inff() : sm.m + log2f(l);
-  const float f = empty ? 0.0f : 1.0f / l;
-  float* out = a.part_o + (split * rows + row) * a.hd;
-#pragma unroll
-  for (int d = 0; d < HD / 32; ++d)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int cc = 32 * d + 8 * e + 4 * (lane >> 5);
-      if (cc < a.hd) {
-        f32x4 w = {sm.o[d][4 * e] * f, sm.o[d][4 * e + 1] * f, sm.o[d][4 * e + 2] * f, sm.o[d][4 * e + 3] * f};
-        *reinterpret_cast<f32x4*>(out + cc) = w;
-      }
-    }
+  store_row_values<HD>(sm.o, empty ? 0.0f : 1.0f / l, out, a.hd, lane);
+  return true;
+}
+
+template <int HD>
+__global__ __launch_bounds__(256, 2) void k_attn_split(AttnArgs a) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const int wave = threadIdx.x >> 6;
+  char* tv = lds + wave * (32 * HD * 2);
+  const int split = static_cast<int>(blockIdx.x) * 4 + wave, r0 = static_cast<int>(blockIdx.y) * 32;
+  const int b = static_cast<int>(blockIdx.z) / a.kv, hk = static_cast<int>(blockIdx.z) % a.kv;
+  if (split >= a.splits) return;
+#pragma unroll 1
+  for (int mode = kPlain; mode <= kNeg; ++mode)
+    if (attn_split<HD>(a, tv, split, r0, b, hk, mode) && mode == kPlain) break;
 }
 
 // The splits' rows joined: o = sum 2^(lse_i - lse) o_i; a wave per row, two columns per lane.
@@ -502,29 +635,34 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
 
 // ------------------------------ gradient of q --------------------------------
 // As the forward, with S^T and dP^T = V dO^T; D = sum(dO o) on the way (o as it was rounded),
-// for the other kernel too.
+// for the other kernel too.  Where the sums are not finite the work is done again with clean
+// values, and NaN in the rows that see a key that had others.
 template <int HD, int NQ>
-__global__ __launch_bounds__(256, 2) void k_attn_dq(AttnGradArgs ga) {
-  constexpr int BM = 128 * NQ, KS = HD / 16;
+__device__ __forceinline__ bool attn_dq(const AttnGradArgs& ga, TilePair<HD>& even, TilePair<HD>& odd, int* bad_key, int bh,
+                                        int q0, int mode) {
+  constexpr int KS = HD / 16;
   const AttnArgs& a = ga.f;
-  extern __shared__ __attribute__((aligned(16))) char lds[];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int nqb = (a.lq + BM - 1) / BM;
-  const uint32_t id = xcd_remap(blockIdx.x, gridDim.x);
-  const int bh = static_cast<int>(id / nqb), qb = nqb - 1 - static_cast<int>(id % nqb);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), w0 = q0 + wave * 32 * NQ;
   const int b = bh / a.heads, h = bh % a.heads, hk = h / (a.heads / a.kv);
   const int L = length_of(a, b), off = L - a.lq;
   const uint16_t* k = a.k + b * a.ks[0] + hk * a.ks[1];
   const uint16_t* v = a.v + b * a.vs[0] + hk * a.vs[1];
   const float c = a.scale * kLog2e;
 
-  const int q0 = qb * BM, last = min(a.lq, q0 + BM) - 1;
+  const int last = min(a.lq, q0 + 128 * NQ) - 1;
   const Walk<kBN> walk(q0 + off, last + off, L, a.window, a.sinks);
-  const int w0 = q0 + wave * 32 * NQ;
+  const int pmin = w0 + off, pmax = min(w0 + 32 * NQ - 1, last) + off;
+  Copy<HD> ck, cv;
+  ck.init(a.ks[2], a.hd, tid);
+  cv.init(a.vs[2], a.hd, tid);
+  auto fetch = [&](int t, TilePair<HD>& to) {
+    ck.issue(k, a.ks[2], walk.key(t), L, a.hd, to.k, wave);
+    cv.issue(v, a.vs[2], walk.key(t), L, a.hd, to.v, wave);
+  };
+  if (walk.count > 0) fetch(0, even);
   u32x4 qf[NQ][KS], gf[NQ][KS];
   f32x16 dq[NQ][HD / 32];
   float lse[NQ], delta[NQ];
-  int p[NQ];
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
     const int row = w0 + 32 * n + (lane & 31);
@@ -538,42 +676,35 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnGradArgs ga) {
         s = __builtin_fmaf(__uint_as_float(qf[n][st][w] << 16), __uint_as_float(gf[n][st][w] << 16), s);
         s = __builtin_fmaf(__uint_as_float(qf[n][st][w] & 0xFFFF0000u), __uint_as_float(gf[n][st][w] & 0xFFFF0000u), s);
       }
-    delta[n] = s + other_half(s);
+    delta[n] = halves_sum(s);
     lse[n] = row < a.lq ? a.lse[int64_t(bh) * a.lq + row] : __builtin_inff();
     if (row < a.lq && lane < 32) ga.delta[int64_t(bh) * a.lq + row] = delta[n];
     load_frags<HD>(qf[n], a.q + b * a.qs[0] + h * a.qs[1], a.qs[2], row, a.lq, a.hd, lane);
-    p[n] = row + off;
 #pragma unroll
     for (int d = 0; d < HD / 32; ++d) dq[n][d] = zero16();
   }
-  const int pmin = w0 + off, pmax = min(w0 + 32 * NQ - 1, last) + off;
 
-  Stage<HD, kBN, 256> sk, sv;
-  if (walk.count > 0) {
-    sk.load(k, a.ks[2], walk.key(0), L, a.hd, tid);
-    sv.load(v, a.vs[2], walk.key(0), L, a.hd, tid);
-  }
-  for (int t = 0; t < walk.count; ++t) {
-    char* tk = lds + (t & 1) * 2 * Tile<HD>::kBytes;
-    char* tv = tk + Tile<HD>::kBytes;
-    sk.store(tk, tid);
-    sv.store(tv, tid);
-    __syncthreads();
-    if (t + 1 < walk.count) {
-      sk.load(k, a.ks[2], walk.key(t + 1), L, a.hd, tid);
-      sv.load(v, a.vs[2], walk.key(t + 1), L, a.hd, tid);
+  auto step = [&](int t, TilePair<HD>& now, TilePair<HD>& next) {
+    copies_done();
+    if (t + 1 < walk.count) fetch(t + 1, next);
+    if (mode != kPlain) {
+      if (tid < kBN) bad_key[tid] = 0;
+      __syncthreads();
+      convert_tile<HD>(now.k, mode, bad_key, tid);
+      convert_tile<HD>(now.v, mode, bad_key, tid);
+      __syncthreads();
     }
     const int j0 = walk.key(t);
-    if (w0 > last || none_seen(j0, kBN, pmin, pmax, a.window, a.sinks)) continue;
-    const bool edge = !all_seen(j0, kBN, pmin, pmax, a.window, a.sinks);
-#pragma unroll
+    if (w0 > last || none_seen(j0, kBN, pmin, pmax, a.window, a.sinks)) return;
+    const bool edge = mode != kPlain || !all_seen(j0, kBN, pmin, pmax, a.window, a.sinks);
+#pragma unroll (HD == 64 ? 2 : 1)
     for (int kb = 0; kb < 2; ++kb) {
       f32x16 s[NQ], dp[NQ];
 #pragma unroll
       for (int n = 0; n < NQ; ++n) s[n] = dp[n] = zero16();
 #pragma unroll
       for (int st = 0; st < KS; ++st) {
-        const u32x4 kf = Tile<HD>::row_frag(tk, 32 * kb, st, lane), vf = Tile<HD>::row_frag(tv, 32 * kb, st, lane);
+        const u32x4 kf = Tile<HD>::row_frag(now.k, 32 * kb, st, lane), vf = Tile<HD>::row_frag(now.v, 32 * kb, st, lane);
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
           s[n] = mfma32x32x16(kf, qf[n][st], s[n]);
@@ -588,8 +719,11 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnGradArgs ga) {
           s[n][e] = exp2_fast(__builtin_fmaf(s[n][e], c, -lse[n])) * (dp[n][e] - delta[n]);
         if (edge) {
 #pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (!seen(j0 + 32 * kb + acc_row(e, lane), p[n], a.window, a.sinks)) s[n][e] = 0.0f;
+          for (int e = 0; e < 16; ++e) {
+            const int j = 32 * kb + acc_row(e, lane);
+            const float v = mode != kPlain && bad_key[j] ? __builtin_nanf("") : s[n][e];
+            s[n][e] = seen(j0 + j, w0 + 32 * n + (lane & 31) + off, a.window, a.sinks) ? v : 0.0f;
+          }
         }
         pack_steps(s[n], ds[n]);
       }
@@ -597,16 +731,21 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnGradArgs ga) {
       for (int st = 0; st < 2; ++st)
 #pragma unroll
         for (int d = 0; d < HD / 32; ++d) {
-          const u32x4 kf = Tile<HD>::col_frag(tk, 32 * kb + 16 * st, d, lane);
-          if (edge) {
+          const u32x4 kf = Tile<HD>::col_frag(now.k, 32 * kb + 16 * st, d, lane);
 #pragma unroll
-            for (int n = 0; n < NQ; ++n) dq[n][d] = mfma_seen<true>(kf, ds[n][st], dq[n][d]);
-          } else {
-#pragma unroll
-            for (int n = 0; n < NQ; ++n) dq[n][d] = mfma32x32x16(kf, ds[n][st], dq[n][d]);
-          }
+          for (int n = 0; n < NQ; ++n) dq[n][d] = mfma32x32x16(kf, ds[n][st], dq[n][d]);
         }
     }
+  };
+  for (int t = 0; t < walk.count; t += 2) {
+    step(t, even, odd);
+    if (t + 1 < walk.count) step(t + 1, odd, even);
+  }
+  if (mode == kPlain) {
+    bool bad = false;
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) bad |= not_finite(dq[n]);
+    if (__syncthreads_or(bad)) return false;
   }
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
@@ -614,25 +753,78 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnGradArgs ga) {
     if (row < a.lq)
       store_rows<HD>(dq[n], a.scale, ga.dq + b * ga.dqs[0] + h * ga.dqs[1] + row * ga.dqs[2], a.hd, lane);
   }
+  return true;
+}
+
+template <int HD, int NQ, int WAVES>
+__global__ __launch_bounds__(256, WAVES) void k_attn_dq(AttnGradArgs ga) {
+  constexpr int BM = 128 * NQ;
+  __shared__ __attribute__((aligned(16))) TilePair<HD> even, odd;
+  __shared__ int bad_key[kBN];
+  const int nqb = (ga.f.lq + BM - 1) / BM;
+  const uint32_t id = xcd_remap(blockIdx.x, gridDim.x);
+  const int bh = static_cast<int>(id / nqb), q0 = (nqb - 1 - static_cast<int>(id % nqb)) * BM;
+#pragma unroll 1
+  for (int mode = kPlain; mode <= kClean; ++mode) {
+    if (attn_dq<HD, NQ>(ga, even, odd, bad_key, bh, q0, mode)) break;
+    __syncthreads();
+  }
 }
 
 // --------------------------- gradients of k and v ----------------------------
-// A workgroup takes 128 keys, 32 per wave, and walks the query tiles of every head that
-// shares them (their sum is formed here, in order).
+// A workgroup takes 128 keys, 32 per wave, and walks the query tiles of the heads that share
+// them in order.  Two things would leave the card to a few long workgroups: few keys and heads
+// (then `parts` workgroups share a block's tiles), and the sinks, which every row sees.  Pairs
+// beyond the window ("far") are a work of their own: 64 of the sinks, 32 to a pair of waves
+// that share a tile's rows, in `chunks` of the tiles.  What several workgroups form lies in
+// fp32 in slots of `part`, and k_attn_dkv_sum adds the slots in order:
+//   near [parts][b kv][near_keys][2][hd], then far [2 chunks][b kv][far_keys][2][hd].
 template <int HD>
-__global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnGradArgs ga) {
-  constexpr int BK = 128, KS = HD / 16;
+struct RowPair {
+  char q[Tile<HD>::kBytes], g[Tile<HD>::kBytes];
+  float lse[kBN], delta[kBN];
+};
+
+struct DkvJob {
+  int bk, k0, slot, far;
+};
+
+template <int HD>
+__device__ __forceinline__ bool attn_dkv(const AttnGradArgs& ga, RowPair<HD>& even, RowPair<HD>& odd, int* bad_row,
+                                         const DkvJob& job, int mode) {
+  constexpr int KS = HD / 16;
   const AttnArgs& a = ga.f;
-  extern __shared__ __attribute__((aligned(16))) char lds[];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int nkb = (a.lk + BK - 1) / BK, G = a.heads / a.kv;
-  const uint32_t id = xcd_remap(blockIdx.x, gridDim.x);
-  const int bk = static_cast<int>(id / nkb), kb = static_cast<int>(id % nkb);
-  const int b = bk / a.kv, hk = bk % a.kv;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), G = a.heads / a.kv;
+  const int b = job.bk / a.kv, hk = job.bk % a.kv;
   const int L = length_of(a, b), off = L - a.lq;
-  const int k0 = kb * BK, w0 = k0 + wave * 32, j = w0 + (lane & 31);
+  const bool far = job.far != 0;
+  const int w0 = job.k0 + 32 * (far ? wave >> 1 : wave), j = w0 + (lane & 31);
   const float c = a.scale * kLog2e;
 
+  // the rows that see some key of the block
+  const int kl = min(job.k0 + (far ? 64 : 128), far ? min(L, a.sinks) : L) - 1;
+  int i0 = max(0, job.k0 + (far ? a.window : 0) - off), i1 = a.lq;
+  if (!far && int64_t(kl) + a.window - off < i1) i1 = kl + a.window - off;
+  i0 = i0 / kBN;
+  // a pair is this work's when apart <= p - j < apart + span; a key that is not, far ahead
+  const int apart = far ? a.window : 0, jj = j <= kl ? j : 1 << 30;
+  const uint32_t span = far ? 1u << 30 : static_cast<uint32_t>(a.window);
+  const int tiles = kl < job.k0 || i1 <= i0 * kBN ? 0 : (i1 + kBN - 1) / kBN - i0;
+  const int per = (tiles * G + (far ? ga.chunks : ga.parts) - 1) / (far ? ga.chunks : ga.parts);
+  const int first = job.slot * per, steps = max(0, min(tiles * G, first + per) - first);
+
+  Copy<HD> cq, cg;
+  cq.init(a.qs[2], a.hd, tid);
+  cg.init(ga.gs[2], a.hd, tid);
+  auto fetch = [&](int t, RowPair<HD>& to) {
+    const int h = hk * G + (first + t) / tiles, r0 = (i0 + (first + t) % tiles) * kBN;
+    cq.issue(a.q + b * a.qs[0] + h * a.qs[1], a.qs[2], r0, a.lq, a.hd, to.q, wave);
+    cg.issue(ga.go + b * ga.gs[0] + h * ga.gs[1], ga.gs[2], r0, a.lq, a.hd, to.g, wave);
+    const int64_t row = (int64_t(b) * a.heads + h) * a.lq;
+    if (wave == 0) copy_row_values(a.lse + row, r0, a.lq, reinterpret_cast<char*>(to.lse), lane);
+    if (wave == 1) copy_row_values(ga.delta + row, r0, a.lq, reinterpret_cast<char*>(to.delta), lane);
+  };
+  if (steps > 0) fetch(0, even);
   u32x4 kf[KS], vf[KS];
   load_frags<HD>(kf, a.k + b * a.ks[0] + hk * a.ks[1], a.ks[2], j, L, a.hd, lane);
   load_frags<HD>(vf, a.v + b * a.vs[0] + hk * a.vs[1], a.vs[2], j, L, a.hd, lane);
@@ -640,56 +832,34 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnGradArgs ga) {
 #pragma unroll
   for (int d = 0; d < HD / 32; ++d) dk[d] = dv[d] = zero16();
 
-  // the rows that see some key of the block
-  const int kl = min(k0 + BK, L) - 1;
-  int i0 = max(0, k0 - off), i1 = a.lq;
-  if (k0 >= a.sinks && int64_t(kl) + a.window - off < i1) i1 = kl + a.window - off;
-  i0 = i0 / kBN;
-  const int tiles = kl < k0 || i1 <= i0 * kBN ? 0 : (i1 + kBN - 1) / kBN - i0;
-  const int steps = tiles * G;
-
-  Stage<HD, kBN, 256> sq, sg;
-  float rl = 0.0f, rd = 0.0f;  // thread 0 .. 63: lse and D of a row
-  auto fetch = [&](int t) {
-    const int h = hk * G + t / tiles, r0 = (i0 + t % tiles) * kBN;
-    sq.load(a.q + b * a.qs[0] + h * a.qs[1], a.qs[2], r0, a.lq, a.hd, tid);
-    sg.load(ga.go + b * ga.gs[0] + h * ga.gs[1], ga.gs[2], r0, a.lq, a.hd, tid);
-    if (tid < kBN) {
-      const int64_t at = (int64_t(b) * a.heads + h) * a.lq + r0 + tid;
-      const bool in = r0 + tid < a.lq;
-      rl = in ? a.lse[at] : __builtin_inff();
-      rd = in ? ga.delta[at] : 0.0f;
+  auto step = [&](int t, RowPair<HD>& now, RowPair<HD>& next) {
+    copies_done();
+    if (t + 1 < steps) fetch(t + 1, next);
+    if (mode != kPlain) {
+      if (tid < kBN) bad_row[tid] = 0;
+      __syncthreads();
+      convert_tile<HD>(now.q, mode, bad_row, tid);
+      convert_tile<HD>(now.g, mode, bad_row, tid);
+      __syncthreads();
     }
-  };
-  if (steps > 0) fetch(0);
-  for (int t = 0; t < steps; ++t) {
-    char* tq = lds + (t & 1) * (2 * Tile<HD>::kBytes + 2 * kBN * 4);
-    char* tg = tq + Tile<HD>::kBytes;
-    float* sl = reinterpret_cast<float*>(tg + Tile<HD>::kBytes);
-    sq.store(tq, tid);
-    sg.store(tg, tid);
-    if (tid < kBN) {
-      sl[tid] = rl;
-      sl[kBN + tid] = rd;
-    }
-    __syncthreads();
-    if (t + 1 < steps) fetch(t + 1);
-    const int r0 = (i0 + t % tiles) * kBN;
-#pragma unroll
+    const int r0 = (i0 + (first + t) % tiles) * kBN;
+#pragma unroll (HD == 64 ? 2 : 1)
     for (int qb = 0; qb < 2; ++qb) {
-      const int pmin = r0 + 32 * qb + off, pmax = pmin + 31;
-      if (w0 >= L || none_seen(w0, 32, pmin, pmax, a.window, a.sinks)) continue;
-      const bool edge = r0 + 32 * qb + 31 >= a.lq || w0 + 31 >= L || !all_seen(w0, 32, pmin, pmax, a.window, a.sinks);
+      const int i1st = r0 + 32 * qb, pmin = i1st + off, pmax = pmin + 31;
+      if (w0 > kl || i1st >= a.lq) continue;
+      if (far ? (wave & 1) != qb || pmax - w0 < a.window : w0 > pmax || pmin - (w0 + 31) >= a.window) continue;
+      const bool all = far ? w0 + 31 < a.sinks && pmin - (w0 + 31) >= a.window : w0 + 31 <= pmin && pmax - w0 < a.window;
+      const bool edge = mode != kPlain || i1st + 31 >= a.lq || w0 + 31 > kl || !all;
       f32x16 s = zero16(), dp = zero16();
 #pragma unroll
       for (int st = 0; st < KS; ++st) {
-        s = mfma32x32x16(Tile<HD>::row_frag(tq, 32 * qb, st, lane), kf[st], s);
-        dp = mfma32x32x16(Tile<HD>::row_frag(tg, 32 * qb, st, lane), vf[st], dp);
+        s = mfma32x32x16(Tile<HD>::row_frag(now.q, 32 * qb, st, lane), kf[st], s);
+        dp = mfma32x32x16(Tile<HD>::row_frag(now.g, 32 * qb, st, lane), vf[st], dp);
       }
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        const f32x4 l4 = *reinterpret_cast<const f32x4*>(sl + 32 * qb + 8 * g + 4 * (lane >> 5));
-        const f32x4 d4 = *reinterpret_cast<const f32x4*>(sl + kBN + 32 * qb + 8 * g + 4 * (lane >> 5));
+        const f32x4 l4 = *reinterpret_cast<const f32x4*>(now.lse + 32 * qb + 8 * g + 4 * (lane >> 5));
+        const f32x4 d4 = *reinterpret_cast<const f32x4*>(now.delta + 32 * qb + 8 * g + 4 * (lane >> 5));
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float pr = exp2_fast(__builtin_fmaf(s[4 * g + e], c, -l4[e]));
@@ -700,8 +870,10 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnGradArgs ga) {
       if (edge) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          const int i = r0 + 32 * qb + acc_row(e, lane);
-          if (i >= a.lq || j >= L || !seen(j, i + off, a.window, a.sinks)) s[e] = dp[e] = 0.0f;
+          const int r = 32 * qb + acc_row(e, lane), p = r0 + r + off;
+          const bool in = (static_cast<uint32_t>(p - jj - apart) < span) & (p < L), nan = mode != kPlain && bad_row[r];
+          s[e] = in ? (nan ? __builtin_nanf("") : s[e]) : 0.0f;
+          dp[e] = in ? (nan ? __builtin_nanf("") : dp[e]) : 0.0f;
         }
       }
       u32x4 pf[2], df[2];
@@ -711,22 +883,95 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnGradArgs ga) {
       for (int st = 0; st < 2; ++st)
 #pragma unroll
         for (int d = 0; d < HD / 32; ++d) {
-          const u32x4 gt = Tile<HD>::col_frag(tg, 32 * qb + 16 * st, d, lane);
-          const u32x4 qt = Tile<HD>::col_frag(tq, 32 * qb + 16 * st, d, lane);
-          if (edge) {
-            dv[d] = mfma_seen<true>(gt, pf[st], dv[d]);
-            dk[d] = mfma_seen<true>(qt, df[st], dk[d]);
-          } else {
-            dv[d] = mfma32x32x16(gt, pf[st], dv[d]);
-            dk[d] = mfma32x32x16(qt, df[st], dk[d]);
-          }
+          dv[d] = mfma32x32x16(Tile<HD>::col_frag(now.g, 32 * qb + 16 * st, d, lane), pf[st], dv[d]);
+          dk[d] = mfma32x32x16(Tile<HD>::col_frag(now.q, 32 * qb + 16 * st, d, lane), df[st], dk[d]);
         }
     }
+  };
+  for (int t = 0; t < steps; t += 2) {
+    step(t, even, odd);
+    if (t + 1 < steps) step(t + 1, odd, even);
   }
-  if (j < a.lk) {
+  if (mode == kPlain && __syncthreads_or(not_finite(dk) || not_finite(dv))) return false;
+  const int64_t bk_all = int64_t(a.b) * a.kv;
+  if (far || j < ga.near_keys) {
+    if (j >= (far ? ga.far_keys : ga.near_keys)) return true;
+    float* out = ga.part;
+    if (far) out += (ga.parts * bk_all * ga.near_keys + ((2 * job.slot + (wave & 1)) * bk_all + job.bk) * ga.far_keys + j) * 2 * a.hd;
+    else out += ((job.slot * bk_all + job.bk) * ga.near_keys + j) * 2 * a.hd;
+    store_row_values<HD>(dk, a.scale, out, a.hd, lane);
+    store_row_values<HD>(dv, 1.0f, out + a.hd, a.hd, lane);
+  } else if (j < a.lk) {
     store_rows<HD>(dk, a.scale, ga.dk + b * ga.dks[0] + hk * ga.dks[1] + j * ga.dks[2], a.hd, lane);
     store_rows<HD>(dv, 1.0f, ga.dv + b * ga.dvs[0] + hk * ga.dvs[1] + j * ga.dvs[2], a.hd, lane);
   }
+  return true;
+}
+
+template <int HD, int WAVES>
+__global__ __launch_bounds__(256, WAVES) void k_attn_dkv(AttnGradArgs ga) {
+  __shared__ __attribute__((aligned(16))) RowPair<HD> even, odd;
+  __shared__ int bad_row[kBN];
+  const int nkb = (ga.f.lk + 127) / 128, nfb = (ga.far_keys + 63) / 64, bk_all = ga.f.b * ga.f.kv;
+  const int far = bk_all * nfb * ga.chunks;
+  const int near_id = static_cast<int>(xcd_remap(blockIdx.x, gridDim.x)) - far, id = near_id < 0 ? near_id + far : near_id;
+  const int slots = near_id < 0 ? ga.chunks : ga.parts, blocks = near_id < 0 ? nfb : nkb;
+  const DkvJob job = {id / (slots * blocks), id / slots % blocks * (near_id < 0 ? 64 : 128), id % slots, near_id < 0};
+#pragma unroll 1
+  for (int mode = kPlain; mode <= kClean; ++mode) {
+    if (attn_dkv<HD>(ga, even, odd, bad_row, job, mode)) break;
+    __syncthreads();
+  }
+}
+
+// The slots' sum of the first near_keys (or, without near parts, far_keys) keys: four columns
+// of dk or dv per thread.
+__global__ __launch_bounds__(256) void k_attn_dkv_sum(AttnGradArgs ga) {
+  const AttnArgs& a = ga.f;
+  const int cols = 2 * a.hd / 4;
+  const int64_t u = int64_t(blockIdx.x) * 256 + threadIdx.x, bk_all = int64_t(a.b) * a.kv, row = u / cols;
+  const int col = static_cast<int>(u % cols) * 4, j = static_cast<int>(row % ga.near_keys);
+  const int64_t bk = row / ga.near_keys;
+  if (bk >= bk_all) return;
+  f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int p = 0; p < ga.parts; ++p)
+    s += *reinterpret_cast<const f32x4*>(ga.part + ((p * bk_all + bk) * ga.near_keys + j) * 2 * a.hd + col);
+  if (j < ga.far_keys) {
+    const float* far = ga.part + ga.parts * bk_all * ga.near_keys * 2 * a.hd;
+    for (int p = 0; p < 2 * ga.chunks; ++p)
+      s += *reinterpret_cast<const f32x4*>(far + ((p * bk_all + bk) * ga.far_keys + j) * 2 * a.hd + col);
+  }
+  const int b = static_cast<int>(bk / a.kv), hk = static_cast<int>(bk % a.kv);
+  uint16_t* out = col < a.hd ? ga.dk + b * ga.dks[0] + hk * ga.dks[1] + j * ga.dks[2] + col
+                             : ga.dv + b * ga.dvs[0] + hk * ga.dvs[1] + j * ga.dvs[2] + col - a.hd;
+  const u32x2 w = {pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3])};
+  *reinterpret_cast<u32x2*>(out) = w;
+}
+
+// How the gradients of k and v are split (AttnGradArgs), and the floats of `part`.
+// parts: 512 workgroups (two per CU) of at least 4 tiles where the blocks of keys are fewer.
+// chunks: a far workgroup walks as many tiles as a near one, at least 16.
+int64_t plan_dkv(AttnGradArgs* g) {
+  const AttnArgs& a = g->f;
+  const int64_t bk = int64_t(a.b) * a.kv, G = a.heads / a.kv;
+  const int64_t blocks = bk * ceil_div(a.lk, 128);
+  const int64_t rows = a.window < a.lk ? (int64_t(a.window) + 127 < a.lq ? int64_t(a.window) + 127 : a.lq) : a.lq;
+  const int64_t tiles = G * ceil_div(rows, kBN);
+  int64_t parts = ceil_div(512, blocks);
+  if (parts > tiles / 4) parts = tiles / 4;
+  if (parts < 1) parts = 1;
+  g->parts = static_cast<int>(parts);
+  const bool far = a.sinks > 0 && a.window < a.lk;
+  g->far_keys = far ? (a.sinks < a.lk ? a.sinks : a.lk) : 0;
+  g->near_keys = parts > 1 ? a.lk : g->far_keys;
+  g->chunks = 0;
+  if (far) {
+    const int64_t far_rows = a.lk - a.window < a.lq ? a.lk - a.window : a.lq, far_tiles = G * ceil_div(far_rows, kBN);
+    const int64_t own = ceil_div(tiles, parts);
+    int64_t chunks = ceil_div(far_tiles, own < 16 ? 16 : own);
+    g->chunks = static_cast<int>(chunks > 64 ? 64 : chunks);
+  }
+  return 2 * a.hd * bk * (parts * g->near_keys + 2 * int64_t(g->chunks) * g->far_keys);
 }
 
 bool args_ok(const AttnArgs& a) {
@@ -735,14 +980,17 @@ bool args_ok(const AttnArgs& a) {
       a.hd > 128 || a.window < 1 || a.sinks < 0 || a.lq > most || a.lk > most || a.window > most || a.sinks > most ||
       !(a.scale > 0.0f))
     return false;
+  for (const int64_t* s : {a.qs, a.ks, a.vs, a.os})
+    if (s[0] < 0 || s[1] < 0 || s[2] < 0 || s[2] > kMaxStride) return false;
+  if ((a.lq > 1 && a.qs[2] < a.hd) || (a.lk > 1 && (a.ks[2] < a.hd || a.vs[2] < a.hd))) return false;
   return int64_t(a.b) * a.heads * ceil_div(a.lq, 32) < (int64_t(1) << 24) &&
          int64_t(a.b) * a.kv * ceil_div(a.lk, 32) < (int64_t(1) << 24);
 }
 
-template <int HD, int NQ>
+template <int HD, int NQ, int WAVES>
 void launch_fwd(const AttnArgs& a, hipStream_t s) {
   const int grid = a.b * a.heads * static_cast<int>(ceil_div(a.lq, 128 * NQ));
-  hipLaunchKernelGGL((k_attn_fwd<HD, NQ>), dim3(grid), dim3(256), 4 * Tile<HD>::kBytes, s, a);
+  hipLaunchKernelGGL((k_attn_fwd<HD, NQ, WAVES>), dim3(grid), dim3(256), 0, s, a);
 }
 
 template <int HD>
@@ -754,13 +1002,18 @@ void launch_split(const AttnArgs& a, hipStream_t s) {
   hipLaunchKernelGGL(k_attn_join, dim3(static_cast<uint32_t>(ceil_div(rows, 4))), dim3(256), 0, s, a);
 }
 
-template <int HD, int NQ>
+template <int HD, int NQ, int WQ, int WK>
 void launch_bwd(const AttnGradArgs& a, bool kv, hipStream_t s) {
   const int grid = a.f.b * a.f.heads * static_cast<int>(ceil_div(a.f.lq, 128 * NQ));
-  hipLaunchKernelGGL((k_attn_dq<HD, NQ>), dim3(grid), dim3(256), 4 * Tile<HD>::kBytes, s, a);
+  hipLaunchKernelGGL((k_attn_dq<HD, NQ, WQ>), dim3(grid), dim3(256), 0, s, a);
   if (!kv) return;
-  const int keys = a.f.b * a.f.kv * static_cast<int>(ceil_div(a.f.lk, 128));
-  hipLaunchKernelGGL((k_attn_dkv<HD>), dim3(keys), dim3(256), 2 * (2 * Tile<HD>::kBytes + 2 * kBN * 4), s, a);
+  const int bk = a.f.b * a.f.kv;
+  const int grid_kv = bk * (static_cast<int>(ceil_div(a.f.lk, 128)) * a.parts + static_cast<int>(ceil_div(a.far_keys, 64)) * a.chunks);
+  hipLaunchKernelGGL((k_attn_dkv<HD, WK>), dim3(grid_kv), dim3(256), 0, s, a);
+  if (a.near_keys > 0) {
+    const int64_t threads = int64_t(bk) * a.near_keys * (a.f.hd / 2);
+    hipLaunchKernelGGL(k_attn_dkv_sum, dim3(static_cast<uint32_t>(ceil_div(threads, 256))), dim3(256), 0, s, a);
+  }
 }
 
 int status() { return hipGetLastError() == hipSuccess ? 0 : -5; }
@@ -780,20 +1033,31 @@ int compact_attention_fwd(const AttnArgs* a, void* stream) {
     if (a->hd <= 64) launch_split<64>(*a, s);
     else if (a->hd <= 96) launch_split<96>(*a, s);
     else launch_split<128>(*a, s);
-  } else if (a->hd <= 64) launch_fwd<64, 2>(*a, s);
-  else if (a->hd <= 96) launch_fwd<96, 1>(*a, s);
-  else launch_fwd<128, 1>(*a, s);
+  } else if (a->hd <= 64) launch_fwd<64, 1, 2>(*a, s);
+  else if (a->hd <= 96) launch_fwd<96, 1, 2>(*a, s);
+  else launch_fwd<128, 1, 2>(*a, s);
   return status();
 }
 
+// The floats of scratch (`part`) that the backward needs; -1: sizes it does not take.
+int64_t compact_attention_bwd_scratch(const AttnArgs* a) {
+  if (!args_ok(*a)) return -1;
+  AttnGradArgs g = {};
+  g.f = *a;
+  return plan_dkv(&g);
+}
+
 // dk and dv are left out where dk is NULL.
-int compact_attention_bwd(const AttnGradArgs* a, void* stream) {
-  if (!args_ok(a->f)) return -1;
+int compact_attention_bwd(const AttnGradArgs* args, void* stream) {
+  AttnGradArgs plan = *args;
+  const AttnGradArgs* a = &plan;
+  if (!args_ok(a->f) || a->gs[2] < 0 || a->gs[2] > kMaxStride || (a->f.lq > 1 && a->gs[2] < a->f.hd)) return -1;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const bool kv = a->dk != nullptr;
-  if (a->f.hd <= 64) launch_bwd<64, 1>(*a, kv, s);
-  else if (a->f.hd <= 96) launch_bwd<96, 1>(*a, kv, s);
-  else launch_bwd<128, 1>(*a, kv, s);
+  if (plan_dkv(&plan) > 0 && kv && a->part == nullptr) return -1;
+  if (a->f.hd <= 64) launch_bwd<64, 1, 2, 2>(*a, kv, s);
+  else if (a->f.hd <= 96) launch_bwd<96, 1, 2, 1>(*a, kv, s);
+  else launch_bwd<128, 1, 2, 1>(*a, kv, s);
   return status();
 }
 

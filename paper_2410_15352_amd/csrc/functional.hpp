@@ -49,6 +49,8 @@ struct AttnGradArgs {
   uint16_t *dq, *dk, *dv;        // dq of q's shape, dk and dv of k's
   float* delta;                  // [b heads][lq] scratch
   int64_t gs[3], dqs[3], dks[3], dvs[3];
+  float* part;                   // [compact_attention_bwd_scratch()]
+  int32_t parts, near_keys, chunks, far_keys;  // set by the entry point
 };
 
 struct DistillArgs {

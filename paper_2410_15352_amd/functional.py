@@ -20,6 +20,7 @@ import math
 import torch
 
 from . import _block_ops as ops
+from . import _lib
 from ._block_ops import _eager, _i32, _i64, _plain, _stream, _vp
 
 __all__ = ["Rotary", "window_attention", "distill_loss"]
@@ -48,7 +49,7 @@ class _AttnArgs(ctypes.Structure):
 
 class _AttnGradArgs(ctypes.Structure):
     _fields_ = [("f", _AttnArgs), ("go", _vp), ("dq", _vp), ("dk", _vp), ("dv", _vp), ("delta", _vp), ("gs", _i64 * 3),
-                ("dqs", _i64 * 3), ("dks", _i64 * 3), ("dvs", _i64 * 3)]
+                ("dqs", _i64 * 3), ("dks", _i64 * 3), ("dvs", _i64 * 3), ("part", _vp), ("plan", _i32 * 4)]
 
 
 class _DistillArgs(ctypes.Structure):
@@ -305,6 +306,7 @@ def rotary_split_qkv(qkv, rope, positions=None):
 
 NO_WINDOW = 1 << 30
 MAX_HD = 128
+MAX_ROW_STRIDE = (1 << 24) - 512
 
 
 def _visible(lq, lk, lengths, window, sinks, device):
@@ -365,13 +367,20 @@ def _attn_tensors(*tensors):
     """bf16 (b, heads, l, hd) tensors as the kernels take them, or None."""
     if not all(_here(t) and t.dtype == _bf16 and t.numel() > 0 for t in tensors):
         return None
-    return [_rows(t)[0] for t in tensors]
+    # (rows that lie on one another, or so far apart that a tile of 64 passes 2^31 bytes, are copied)
+    return [_rows(t if t.shape[2] == 1 or t.shape[3] <= t.stride(2) <= MAX_ROW_STRIDE else t.contiguous())[0] for t in tensors]
 
 
 def _empty_heads(like, l=None):
     """(b, heads, l, hd) that lies as (b, l, heads, hd), the layout the projections take."""
     b, heads, n, hd = like.shape
     return torch.empty(b, n, heads, hd, dtype=_bf16, device=like.device).transpose(1, 2)
+
+
+def _attn_scratch(args):
+    fn = _lib.load().compact_attention_bwd_scratch
+    fn.restype, fn.argtypes = _i64, [ctypes.POINTER(_AttnArgs)]
+    return fn(ctypes.byref(args))
 
 
 class _AttentionFn(torch.autograd.Function):
@@ -421,6 +430,10 @@ class _AttentionFn(torch.autograd.Function):
             dk, dv = _empty_heads(k), _empty_heads(v)
             g.dk, g.dv = dk.data_ptr(), dv.data_ptr()
             g.dks[:], g.dvs[:] = _strides(dk), _strides(dv)
+            floats = _attn_scratch(g.f)
+            if floats > 0:
+                part = torch.empty(floats, dtype=torch.float32, device=q.device)
+                g.part = part.data_ptr()
         ops._call("compact_attention_bwd", ctypes.byref(g), _stream(q))
         return dq, dk, dv, *none
 
