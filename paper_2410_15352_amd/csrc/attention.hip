@@ -88,49 +88,20 @@ __device__ __forceinline__ uint32_t value_pair(uint32_t w, int mode) {
   return out;
 }
 
-// This wave's chunks of a tile on their way from memory to LDS: rows j0 .. j0 + ROWS - 1 of
-// a matrix, rows at or past `rows` and columns at or past hd as zeros.
-template <int HD, int ROWS, int THREADS>
-struct Stage {
-  static constexpr int kN = ROWS * (HD / 8) / THREADS;
-  u32x4 w[kN];
-  __device__ __forceinline__ void load(const uint16_t* base, int64_t stride, int j0, int rows, int hd, int tid) {
-#pragma unroll
-    for (int i = 0; i < kN; ++i) {
-      const int idx = tid + THREADS * i, r = idx / (HD / 8), c = idx % (HD / 8);
-      w[i] = u32x4{0u, 0u, 0u, 0u};
-      if (j0 + r < rows && c * 8 < hd) w[i] = *reinterpret_cast<const u32x4*>(base + (int64_t(j0) + r) * stride + c * 8);
-    }
-  }
-  __device__ __forceinline__ void store(char* t, int tid) const {
-#pragma unroll
-    for (int i = 0; i < kN; ++i) {
-      const int idx = tid + THREADS * i;
-      *reinterpret_cast<u32x4*>(t + Tile<HD>::at(idx / (HD / 8), idx % (HD / 8))) = w[i];
-    }
-  }
-  // bad[r] = 1 for a row r with an infinity or NaN
-  __device__ __forceinline__ void convert(int mode, int* bad, int tid) {
-#pragma unroll
-    for (int i = 0; i < kN; ++i)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t x = value_pair(w[i][e], mode);
-        if (bad != nullptr && x != w[i][e]) bad[(tid + THREADS * i) / (HD / 8)] = 1;
-        w[i][e] = x;
-      }
-  }
-};
-
 // A tile's way into LDS without registers: each wave copies kN blocks of 1 KB, lane after lane
 // 16 bytes, fetching for each place of the tile the chunk that belongs there.  Rows at or past
 // `rows` and columns at or past hd read as zeros (the buffer's range check).  A tile's bytes
 // lie within 2^31 (row strides below kMaxStride), the tile's own start is a 64-bit address.
 constexpr int64_t kMaxStride = (int64_t(1) << 24) - 512;
 
-template <int HD>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_rows(const uint16_t* base, int64_t stride, int j0, int n, int hd) {
+  const int bytes = n > 0 ? ((n - 1) * static_cast<int>(stride) + hd) * 2 : 0;
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(base + j0 * stride), static_cast<short>(0), bytes, 0x00020000);
+}
+
+template <int HD, int ROWS = kBN, int WAVES = 4>
 struct Copy {
-  static constexpr int kN = Tile<HD>::kBytes / 1024 / 4;
+  static constexpr int kN = ROWS * HD * 2 / 1024 / WAVES;
   int off[kN];
   __device__ __forceinline__ void init(int64_t stride, int hd, int tid) {
 #pragma unroll
@@ -140,10 +111,7 @@ struct Copy {
     }
   }
   __device__ __forceinline__ void issue(const uint16_t* base, int64_t stride, int j0, int rows, int hd, char* t, int wave) const {
-    const int n = min(rows - j0, kBN);
-    const int bytes = n > 0 ? ((n - 1) * static_cast<int>(stride) + hd) * 2 : 0;
-    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<uint16_t*>(base + j0 * stride), static_cast<short>(0), bytes, 0x00020000);
+    const __amdgpu_buffer_rsrc_t rs = tile_rows(base, stride, j0, min(rows - j0, ROWS), hd);
 #pragma unroll
     for (int i = 0; i < kN; ++i)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)(t + (wave * kN + i) * 1024), 16, off[i], 0, 0, 0);
@@ -162,10 +130,10 @@ __device__ __forceinline__ void copy_row_values(const float* v, int r0, int rows
 __device__ __forceinline__ void copies_done() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory"); }
 
 // A tile's values converted where they are; bad[r] = 1 for a row r with an infinity or NaN.
-template <int HD>
+template <int HD, int ROWS = kBN, int THREADS = 256>
 __device__ __forceinline__ void convert_tile(char* t, int mode, int* bad, int tid) {
 #pragma unroll 1
-  for (int idx = tid; idx < kBN * (HD / 8); idx += 256) {
+  for (int idx = tid; idx < ROWS * (HD / 8); idx += THREADS) {
     u32x4* at = reinterpret_cast<u32x4*>(t + Tile<HD>::at(idx / (HD / 8), idx % (HD / 8)));
     u32x4 w = *at;
 #pragma unroll
@@ -364,7 +332,8 @@ struct TilePair {
 };
 
 template <int HD, int NQ>
-__device__ __forceinline__ bool attn_fwd(const AttnArgs& a, TilePair<HD>& even, TilePair<HD>& odd, int bh, int q0, int mode) {
+__device__ __forceinline__ bool attn_fwd(const AttnArgs& a, TilePair<HD>& even, TilePair<HD>& odd, int bh, int q0, int split,
+                                         int mode) {
   constexpr int KS = HD / 16;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), w0 = q0 + wave * 32 * NQ;
   const int b = bh / a.heads, h = bh % a.heads, hk = h / (a.heads / a.kv);
@@ -384,7 +353,10 @@ __device__ __forceinline__ bool attn_fwd(const AttnArgs& a, TilePair<HD>& even, 
     ck.issue(k, a.ks[2], walk.key(t), L, a.hd, to.k, wave);
     cv.issue(v, a.vs[2], walk.key(t), L, a.hd, to.v, wave);
   };
-  if (walk.count > 0) fetch(0, even);
+  // the tiles of this split (all of them without splits)
+  const int per = a.splits > 0 ? (walk.count + a.splits - 1) / a.splits : walk.count;
+  const int t0 = split * per, t1 = min(walk.count, t0 + per);
+  if (t0 < t1) fetch(t0, even);
   u32x4 qf[NQ][KS];
   Softmax<HD> sm[NQ];
 #pragma unroll
@@ -395,7 +367,7 @@ __device__ __forceinline__ bool attn_fwd(const AttnArgs& a, TilePair<HD>& even, 
 
   auto step = [&](int t, TilePair<HD>& now, TilePair<HD>& next) {
     copies_done();
-    if (t + 1 < walk.count) fetch(t + 1, next);
+    if (t + 1 < t1) fetch(t + 1, next);
     if (mode != kPlain) {
       convert_tile<HD>(now.v, mode, nullptr, tid);
       __syncthreads();
@@ -456,9 +428,9 @@ __device__ __forceinline__ bool attn_fwd(const AttnArgs& a, TilePair<HD>& even, 
         for (int n = 0; n < NQ; ++n) sm[n].o[d] = mfma32x32x16(vf, pf[n][st], sm[n].o[d]);
       }
   };
-  for (int t = 0; t < walk.count; t += 2) {
+  for (int t = t0; t < t1; t += 2) {
     step(t, even, odd);
-    if (t + 1 < walk.count) step(t + 1, odd, even);
+    if (t + 1 < t1) step(t + 1, odd, even);
   }
   if (mode == kPlain) {
     bool bad = false;
@@ -471,13 +443,24 @@ __device__ __forceinline__ bool attn_fwd(const AttnArgs& a, TilePair<HD>& even, 
     const int row = w0 + 32 * n + (lane & 31);
     const float l = halves_sum(sm[n].l);
     if (row >= a.lq) continue;
+    const bool empty = sm[n].m == -__builtin_inff() && l == 0.0f;
+    const float f = empty ? 0.0f : 1.0f / l;
+    if (a.splits > 0) {
+      const int64_t rows = int64_t(a.b) * a.heads * a.lq, at = split * rows + int64_t(bh) * a.lq + row;
+      if (mode >= kPos) {
+        mark_rows<HD>(sm[n].o, mode, a.part_o + at * a.hd, a.hd, lane);
+        continue;
+      }
+      store_row_values<HD>(sm[n].o, f, a.part_o + at * a.hd, a.hd, lane);
+      if (lane < 32) a.part_lse[at] = empty ? -__builtin_inff() : sm[n].m + log2f(l);
+      continue;
+    }
     uint16_t* out = a.o + b * a.os[0] + h * a.os[1] + row * a.os[2];
     if (mode >= kPos) {
       mark_rows<HD>(sm[n].o, mode, out, a.hd, lane);
       continue;
     }
-    const bool empty = sm[n].m == -__builtin_inff() && l == 0.0f;
-    store_rows<HD>(sm[n].o, empty ? 0.0f : 1.0f / l, out, a.hd, lane);
+    store_rows<HD>(sm[n].o, f, out, a.hd, lane);
     if (lane < 32) a.lse[int64_t(bh) * a.lq + row] = empty ? __builtin_inff() : sm[n].m + log2f(l);
   }
   return true;
@@ -487,24 +470,32 @@ template <int HD, int NQ, int WAVES>
 __global__ __launch_bounds__(256, WAVES) void k_attn_fwd(AttnArgs a) {
   constexpr int BM = 128 * NQ;
   __shared__ __attribute__((aligned(16))) TilePair<HD> even, odd;
-  const int nqb = (a.lq + BM - 1) / BM;
-  const uint32_t id = xcd_remap(blockIdx.x, gridDim.x);
+  const int nqb = (a.lq + BM - 1) / BM, splits = a.splits > 0 ? a.splits : 1;
+  const uint32_t id0 = xcd_remap(blockIdx.x, gridDim.x), id = id0 / splits;
+  const int split = static_cast<int>(id0 % splits);
   const int bh = static_cast<int>(id / nqb), q0 = (nqb - 1 - static_cast<int>(id % nqb)) * BM;
 #pragma unroll 1
   for (int mode = kPlain; mode <= kNeg; ++mode) {
-    if (attn_fwd<HD, NQ>(a, even, odd, bh, q0, mode) && mode == kPlain) break;
+    if (attn_fwd<HD, NQ>(a, even, odd, bh, q0, split, mode) && mode == kPlain) break;
     __syncthreads();
   }
 }
 
 // ------------------------- forward, split over the keys ----------------------
 // Few rows over many keys: the rows of the heads that share keys (32 of the G lq at a time)
-// are the columns of one wave, and each wave takes a range of the keys on its own, K straight
-// from memory as the A operand, V through its own part of LDS.
+// are the columns of one wave, and each wave takes a range of the keys on its own: K straight
+// from memory as the A operand, V by copies into its own part of LDS, both a tile of 32 keys
+// ahead.
 template <int HD>
-__device__ __forceinline__ bool attn_split(const AttnArgs& a, char* tv, int split, int r0, int b, int hk, int mode) {
+struct WaveTiles {
+  char v[4][32 * HD * 2];
+};
+
+template <int HD>
+__device__ __forceinline__ bool attn_split(const AttnArgs& a, WaveTiles<HD>& even, WaveTiles<HD>& odd, int split, int r0, int b,
+                                           int hk, int mode) {
   constexpr int KS = HD / 16, TN = 32;
-  const int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int G = a.heads / a.kv, R = G * a.lq;
   const int L = length_of(a, b), off = L - a.lq;
   const uint16_t* k = a.k + b * a.ks[0] + hk * a.ks[1];
@@ -520,29 +511,34 @@ __device__ __forceinline__ bool attn_split(const AttnArgs& a, char* tv, int spli
   const int per = (walk.count + a.splits - 1) / a.splits;
   const int t0 = split * per, t1 = min(walk.count, t0 + per);
 
-  u32x4 qf[KS];
+  u32x4 qf[KS], kf[KS];
+  Copy<HD, TN, 1> cv;
+  cv.init(a.vs[2], a.hd, lane);
+  const int koff = (lane & 31) * static_cast<int>(a.ks[2]) * 2 + 16 * (lane >> 5);
+  // always issued, past the last tile with no rows: a wait then counts the loads behind it
+  auto rows_of = [&](int t) { return t < t1 ? min(L - walk.key(t), TN) : 0; };
+  auto fetch_v = [&](int t, WaveTiles<HD>& to) {
+    cv.issue(v, a.vs[2], walk.key(t), walk.key(t) + rows_of(t), a.hd, to.v[wave], 0);
+  };
+  auto fetch_k = [&](int t) {
+    const __amdgpu_buffer_rsrc_t rs = tile_rows(k, a.ks[2], walk.key(t), rows_of(t), a.hd);
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+      kf[s] = __builtin_amdgcn_raw_buffer_load_b128(rs, 16 * s + 8 * (lane >> 5) < a.hd ? koff + 32 * s : 0x7FFFFFF0, 0, 0);
+  };
+  fetch_v(t0, even);
+  fetch_k(t0);
   load_frags<HD>(qf, a.q + b * a.qs[0] + (hk * G + g) * a.qs[1], a.qs[2], r < R ? i : a.lq, a.lq, a.hd, lane);
   Softmax<HD> sm;
   sm.init();
-  u32x4 kf[KS], kn[KS];
-  Stage<HD, TN, 64> sv;
-  if (t0 < t1) {
-    load_frags<HD>(kn, k, a.ks[2], walk.key(t0) + (lane & 31), L, a.hd, lane);
-    sv.load(v, a.vs[2], walk.key(t0), L, a.hd, lane);
-  }
-  for (int t = t0; t < t1; ++t) {
+  auto step = [&](int t, WaveTiles<HD>& now, WaveTiles<HD>& next) {
     const int j0 = walk.key(t);
-#pragma unroll
-    for (int s = 0; s < KS; ++s) kf[s] = kn[s];
-    if (mode != kPlain) sv.convert(mode, nullptr, lane);
-    sv.store(tv, lane);
-    if (t + 1 < t1) {
-      load_frags<HD>(kn, k, a.ks[2], walk.key(t + 1) + (lane & 31), L, a.hd, lane);
-      sv.load(v, a.vs[2], walk.key(t + 1), L, a.hd, lane);
-    }
+    fetch_v(t + 1, next);
+    if (mode != kPlain) convert_tile<HD, TN, 64>(now.v[wave], mode, nullptr, lane);
     f32x16 s = zero16();
 #pragma unroll
     for (int st = 0; st < KS; ++st) s = mfma32x32x16(kf[st], qf[st], s);
+    fetch_k(t + 1);
     if (!all_seen(j0, TN, pmin, pmax, a.window, a.sinks)) {
 #pragma unroll
       for (int e = 0; e < 16; ++e)
@@ -563,10 +559,12 @@ __device__ __forceinline__ bool attn_split(const AttnArgs& a, char* tv, int spli
 #pragma unroll
     for (int st = 0; st < 2; ++st)
 #pragma unroll
-      for (int d = 0; d < HD / 32; ++d) {
-        const u32x4 vf = Tile<HD>::col_frag(tv, 16 * st, d, lane);
-        sm.o[d] = mfma32x32x16(vf, pf[st], sm.o[d]);
-      }
+      for (int d = 0; d < HD / 32; ++d)
+        sm.o[d] = mfma32x32x16(Tile<HD>::col_frag(now.v[wave], 16 * st, d, lane), pf[st], sm.o[d]);
+  };
+  for (int t = t0; t < t1; t += 2) {
+    step(t, even, odd);
+    if (t + 1 < t1) step(t + 1, odd, even);
   }
   if (mode == kPlain && __any(not_finite(sm.o))) return false;
   const float l = halves_sum(sm.l);
@@ -585,24 +583,25 @@ __device__ __forceinline__ bool attn_split(const AttnArgs& a, char* tv, int spli
 
 template <int HD>
 __global__ __launch_bounds__(256, 2) void k_attn_split(AttnArgs a) {
-  extern __shared__ __attribute__((aligned(16))) char lds[];
-  const int wave = threadIdx.x >> 6;
-  char* tv = lds + wave * (32 * HD * 2);
-  const int split = static_cast<int>(blockIdx.x) * 4 + wave, r0 = static_cast<int>(blockIdx.y) * 32;
+  __shared__ __attribute__((aligned(16))) WaveTiles<HD> even, odd;
+  const int split = static_cast<int>(blockIdx.x) * 4 + static_cast<int>(threadIdx.x >> 6), r0 = static_cast<int>(blockIdx.y) * 32;
   const int b = static_cast<int>(blockIdx.z) / a.kv, hk = static_cast<int>(blockIdx.z) % a.kv;
   if (split >= a.splits) return;
 #pragma unroll 1
   for (int mode = kPlain; mode <= kNeg; ++mode)
-    if (attn_split<HD>(a, tv, split, r0, b, hk, mode) && mode == kPlain) break;
+    if (attn_split<HD>(a, even, odd, __builtin_amdgcn_readfirstlane(split), r0, b, hk, mode) && mode == kPlain) break;
 }
 
-// The splits' rows joined: o = sum 2^(lse_i - lse) o_i; a wave per row, two columns per lane.
+// The splits' rows joined: o = sum 2^(lse_i - lse) o_i.  A workgroup per row, 32 lanes over
+// its columns, the splits dealt to 8 such groups: few loads one after another.
 __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t rows = int64_t(a.b) * a.heads * a.lq, row = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
-  if (row >= rows) return;
+  __shared__ float red[4];
+  __shared__ f32x4 sums[8][32];
+  __shared__ float weights[8];
+  const int tid = threadIdx.x, lane = tid & 31, group = tid >> 5;
+  const int64_t rows = int64_t(a.b) * a.heads * a.lq, row = blockIdx.x;
   float m = -__builtin_inff();
-  for (int s = lane; s < a.splits; s += 64) {
+  for (int s = tid; s < a.splits; s += 256) {
     const float x = a.part_lse[s * rows + row];
     m = x > m || x != x ? x : m;
   }
@@ -611,25 +610,39 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
     const float x = __shfl_xor(m, d, 64);
     m = x > m || x != x ? x : m;
   }
+  if ((tid & 63) == 0) red[tid >> 6] = m;
+  __syncthreads();
+  m = red[0];
+  for (int w = 1; w < 4; ++w) m = red[w] > m || red[w] != red[w] ? red[w] : m;
   const bool empty = m == -__builtin_inff();
-  float l = 0.0f, o0 = 0.0f, o1 = 0.0f;
-  const int c = 2 * lane;
-  for (int s = 0; s < a.splits; ++s) {
-    const float x = a.part_lse[s * rows + row];
-    if (x == -__builtin_inff()) continue;
-    const float f = exp2_fast(x - m);
+  const float shift = empty ? 0.0f : m;
+  float l = 0.0f;
+  f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+  const int c = 4 * lane;
+  for (int s = group; s < a.splits; s += 8) {
+    const float f = exp2_fast(a.part_lse[s * rows + row] - shift);
     l += f;
     if (c < a.hd) {
-      const float2 w = *reinterpret_cast<const float2*>(a.part_o + (s * rows + row) * a.hd + c);
-      o0 += f * w.x;
-      o1 += f * w.y;
+      const f32x4 w = *reinterpret_cast<const f32x4*>(a.part_o + (s * rows + row) * a.hd + c);
+      // (a split without keys holds zeros)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(f, w[e], o[e]);
     }
+  }
+  sums[group][lane] = o;
+  if (lane == 0) weights[group] = l;
+  __syncthreads();
+  if (group != 0) return;
+  for (int g = 1; g < 8; ++g) {
+    o += sums[g][lane];
+    l += weights[g];
   }
   const float f = empty ? 0.0f : 1.0f / l;
   const int bh = static_cast<int>(row / a.lq), i = static_cast<int>(row % a.lq);
-  if (c < a.hd)
-    *reinterpret_cast<uint32_t*>(a.o + (bh / a.heads) * a.os[0] + (bh % a.heads) * a.os[1] + i * a.os[2] + c) =
-        pack_bf16x2(o0 * f, o1 * f);
+  if (c < a.hd) {
+    const u32x2 w = {pack_bf16x2(o[0] * f, o[1] * f), pack_bf16x2(o[2] * f, o[3] * f)};
+    *reinterpret_cast<u32x2*>(a.o + (bh / a.heads) * a.os[0] + (bh % a.heads) * a.os[1] + i * a.os[2] + c) = w;
+  }
   if (lane == 0) a.lse[row] = empty ? __builtin_inff() : m + log2f(l);
 }
 
@@ -987,19 +1000,23 @@ bool args_ok(const AttnArgs& a) {
          int64_t(a.b) * a.kv * ceil_div(a.lk, 32) < (int64_t(1) << 24);
 }
 
+void launch_join(const AttnArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL(k_attn_join, dim3(static_cast<uint32_t>(int64_t(a.b) * a.heads * a.lq)), dim3(256), 0, s, a);
+}
+
 template <int HD, int NQ, int WAVES>
 void launch_fwd(const AttnArgs& a, hipStream_t s) {
-  const int grid = a.b * a.heads * static_cast<int>(ceil_div(a.lq, 128 * NQ));
+  const int grid = a.b * a.heads * static_cast<int>(ceil_div(a.lq, 128 * NQ)) * (a.splits > 0 ? a.splits : 1);
   hipLaunchKernelGGL((k_attn_fwd<HD, NQ, WAVES>), dim3(grid), dim3(256), 0, s, a);
+  if (a.splits > 0) launch_join(a, s);
 }
 
 template <int HD>
-void launch_split(const AttnArgs& a, hipStream_t s) {
+void launch_waves(const AttnArgs& a, hipStream_t s) {
   const dim3 grid(static_cast<uint32_t>(ceil_div(a.splits, 4)),
                   static_cast<uint32_t>(ceil_div(int64_t(a.heads / a.kv) * a.lq, 32)), static_cast<uint32_t>(a.b * a.kv));
-  hipLaunchKernelGGL((k_attn_split<HD>), grid, dim3(256), 4 * 32 * HD * 2, s, a);
-  const int64_t rows = int64_t(a.b) * a.heads * a.lq;
-  hipLaunchKernelGGL(k_attn_join, dim3(static_cast<uint32_t>(ceil_div(rows, 4))), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((k_attn_split<HD>), grid, dim3(256), 0, s, a);
+  launch_join(a, s);
 }
 
 template <int HD, int NQ, int WQ, int WK>
@@ -1028,11 +1045,12 @@ extern "C" {
 int compact_attention_fwd(const AttnArgs* a, void* stream) {
   if (!args_ok(*a)) return -1;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (a->splits > 0) {
+  if (a->splits > 0 && (int64_t(a->b) * a->heads * a->lq >= int64_t(1) << 24 || a->part_o == nullptr)) return -1;
+  if (a->splits > 0 && a->waves) {
     if (int64_t(a->b) * a->kv > 65535 || ceil_div(int64_t(a->heads / a->kv) * a->lq, 32) > 65535) return -1;
-    if (a->hd <= 64) launch_split<64>(*a, s);
-    else if (a->hd <= 96) launch_split<96>(*a, s);
-    else launch_split<128>(*a, s);
+    if (a->hd <= 64) launch_waves<64>(*a, s);
+    else if (a->hd <= 96) launch_waves<96>(*a, s);
+    else launch_waves<128>(*a, s);
   } else if (a->hd <= 64) launch_fwd<64, 1, 2>(*a, s);
   else if (a->hd <= 96) launch_fwd<96, 1, 2>(*a, s);
   else launch_fwd<128, 1, 2>(*a, s);

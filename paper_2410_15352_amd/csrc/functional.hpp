@@ -38,8 +38,9 @@ struct AttnArgs {
   int32_t b, heads, kv, lq, lk, hd;
   int32_t window, sinks;         // key j of position p: j <= p and (p - j < window or j < sinks)
   float scale;
-  int32_t splits;                // > 0: the split form, by this many ranges of keys
-  float* part_o;                 // split form: [splits][b heads lq][hd]
+  int32_t splits;                // > 0: this many ranges of keys apart, then joined
+  int32_t waves;                 // split form of few rows: a wave for 32 rows of the heads that share keys
+  float* part_o;                 // with splits: [splits][b heads lq][hd]
   float* part_lse;               // [splits][b heads lq]
 };
 

@@ -16,54 +16,32 @@ from __future__ import annotations
 
 import ctypes
 import math
+import struct
 
 import torch
 
 from . import _block_ops as ops
 from . import _lib
-from ._block_ops import _eager, _i32, _i64, _plain, _stream, _vp
+from ._block_ops import _eager, _i64, _plain, _stream, _vp
 
 __all__ = ["Rotary", "window_attention", "distill_loss"]
 
-_f32 = ctypes.c_float
 _bf16 = torch.bfloat16
 
-
-class _RotaryTensor(ctypes.Structure):
-    _fields_ = [("src", _vp), ("dst", _vp), ("src_b", _i64), ("src_l", _i64), ("src_h", _i64), ("dst_b", _i64),
-                ("dst_l", _i64), ("dst_h", _i64), ("heads", _i32), ("rotate", _i32)]
-
-
-class _RotaryArgs(ctypes.Structure):
-    _fields_ = [("t", _RotaryTensor * 3), ("turns", _vp), ("positions", _vp), ("pos_b", _i64), ("pos_l", _i64),
-                ("offset", _i64), ("tokens", _i64), ("l", _i32), ("hd", _i32), ("dims", _i32), ("count", _i32),
-                ("interleaved", _i32), ("inverse", _i32), ("pos32", _i32), ("f32", _i32), ("magnitude", _f32)]
-
-
-class _AttnArgs(ctypes.Structure):
-    _fields_ = [("q", _vp), ("k", _vp), ("v", _vp), ("o", _vp), ("lse", _vp), ("lengths", _vp), ("qs", _i64 * 3),
-                ("ks", _i64 * 3), ("vs", _i64 * 3), ("os", _i64 * 3), ("b", _i32), ("heads", _i32), ("kv", _i32),
-                ("lq", _i32), ("lk", _i32), ("hd", _i32), ("window", _i32), ("sinks", _i32), ("scale", _f32),
-                ("splits", _i32), ("part_o", _vp), ("part_lse", _vp)]
-
-
-class _AttnGradArgs(ctypes.Structure):
-    _fields_ = [("f", _AttnArgs), ("go", _vp), ("dq", _vp), ("dk", _vp), ("dv", _vp), ("delta", _vp), ("gs", _i64 * 3),
-                ("dqs", _i64 * 3), ("dks", _i64 * 3), ("dvs", _i64 * 3), ("part", _vp), ("plan", _i32 * 4)]
-
-
-class _DistillArgs(ctypes.Structure):
-    _fields_ = [("x", _vp), ("top", _vp), ("ids", _vp), ("target", _vp), ("count", _vp), ("loss_row", _vp),
-                ("loss", _vp), ("dx", _vp), ("dloss", _vp), ("rows", _i64), ("V", _i64), ("top_ld", _i64),
-                ("ids_ld", _i64), ("ignore_index", _i64), ("K", _i32), ("f32", _i32), ("top32", _i32), ("ids32", _i32),
-                ("unless_one", _i32), ("temperature", _f32), ("weight", _f32)]
-
+# The argument blocks of csrc/functional.hpp as native struct layouts (a ctypes.Structure
+# costs ten times as much to fill), passed by address.
+_ROTARY = struct.Struct("@" + 3 * "2Q6q2i" + "2Q4q8if").pack
+_ATTN = "6Q12q8if2i2Q"
+_attn_pack = struct.Struct("@" + _ATTN).pack
+_attn_grad_pack = struct.Struct("@" + _ATTN + "5Q12qQ4i").pack
+_distill_pack = struct.Struct("@9Q5q5i2f").pack
+_block = ctypes.c_char_p
 
 ops._SIGNATURES.update({
-    "compact_rotary": [ctypes.POINTER(_RotaryArgs), _vp],
-    "compact_attention_fwd": [ctypes.POINTER(_AttnArgs), _vp],
-    "compact_attention_bwd": [ctypes.POINTER(_AttnGradArgs), _vp],
-    "compact_distill": [ctypes.POINTER(_DistillArgs), _vp],
+    "compact_rotary": [_block, _vp],
+    "compact_attention_fwd": [_block, _vp],
+    "compact_attention_bwd": [_block, _vp],
+    "compact_distill": [_block, _vp],
 })
 
 
@@ -74,19 +52,24 @@ def _here(t):
 
 def _strides(t):
     """The strides of the first three dimensions; 0 where a dimension has one element."""
-    return [s if n > 1 else 0 for s, n in zip(t.stride()[:3], t.shape)]
+    x, y, z, _ = t.stride()
+    b, c, d, _ = t.shape
+    return (x if b > 1 else 0, y if c > 1 else 0, z if d > 1 else 0)
 
 
 def _rows(t):
-    """t (4-D, its last dimension dense and every row on a 16-byte boundary), or a copy of
-    it that is so, and its strides."""
-    s = _strides(t)
-    size = t.element_size()
-    if t.stride(3) != 1 or t.data_ptr() % 16 != 0 or any(x * size % 16 != 0 for x in s):
+    """t (4-D), or a copy of it, whose last dimension is dense and whose every row is on a
+    16-byte boundary."""
+    x, y, z = _strides(t)
+    if t.stride(3) != 1 or (t.data_ptr() | (x | y | z) * t.element_size()) % 16 != 0:
         t = t.contiguous()
         t = t if t.data_ptr() % 16 == 0 else t.clone()
-        s = _strides(t)
-    return t, s
+    return t
+
+
+def _tracked(*tensors):
+    """A gradient of some tensor is wanted."""
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
 
 
 # ------------------------------- rotary -------------------------------------
@@ -150,10 +133,12 @@ class Rotary(torch.nn.Module):
 
     def forward(self, q, k=None, positions=None):
         self._check(q, k, positions)
-        if self._usable(q, k, positions):
+        if not self._usable(q, k, positions):
+            out = _rotary_torch(self, positions, False, q, k)
+        elif _tracked(q, k):
             out = _RotaryFn.apply(self, positions, q, k)
-            return out if k is not None else out[0]
-        out = _rotary_torch(self, positions, False, q, k)
+        else:
+            out = _rotary_apply(self, positions, 0, q, k)
         return out if k is not None else out[0]
 
     def _check(self, q, k, positions):
@@ -187,25 +172,33 @@ class Rotary(torch.nn.Module):
                 and (not isinstance(positions, torch.Tensor) or _plain(positions)))
 
 
+_NO_TENSOR = (0,) * 10
+
+
 def _rotary_call(rope, positions, inverse, jobs):
     """jobs: (source, destination, rotated) of (b, l, heads, hd) tensors whose rows are dense
     and on 16-byte boundaries."""
-    a = _RotaryArgs()
     x = jobs[0][0]
     b, l, _, hd = x.shape
-    for t, (src, dst, rotate) in zip(a.t, jobs):
-        t.src, t.dst, t.heads, t.rotate = src.data_ptr(), dst.data_ptr(), src.shape[2], rotate
-        t.src_b, t.src_l, t.src_h = _strides(src)
-        t.dst_b, t.dst_l, t.dst_h = _strides(dst)
-    a.turns = rope.turns(x.device).data_ptr()
+    fields = []
+    for src, dst, rotate in jobs:
+        fields += (src.data_ptr(), dst.data_ptr(), *_strides(src), *_strides(dst), src.shape[2], rotate)
+    fields += _NO_TENSOR * (3 - len(jobs))
+    at, pos_b, pos_l, offset, pos32 = 0, 0, 0, 0, 0
     if isinstance(positions, torch.Tensor):
-        a.positions, a.pos32 = positions.data_ptr(), positions.dtype == torch.int32
-        a.pos_b, a.pos_l = ([0, *positions.stride()] if positions.dim() == 1 else positions.stride())
+        at, pos32 = positions.data_ptr(), positions.dtype == torch.int32
+        pos_b, pos_l = (0, *positions.stride()) if positions.dim() == 1 else positions.stride()
     else:
-        a.offset = positions or 0
-    a.tokens, a.l, a.hd, a.dims, a.count = b * l, l, hd, rope.dims, len(jobs)
-    a.interleaved, a.inverse, a.f32, a.magnitude = rope.interleaved, inverse, x.dtype == torch.float32, rope.magnitude
-    ops._call("compact_rotary", ctypes.byref(a), _stream(x))
+        offset = positions or 0
+    ops._call("compact_rotary",
+              _ROTARY(*fields, rope.turns(x.device).data_ptr(), at, pos_b, pos_l, offset, b * l, l, hd, rope.dims,
+                      len(jobs), rope.interleaved, inverse, pos32, x.dtype == torch.float32, rope.magnitude), _stream(x))
+
+
+def _rotary_apply(rope, positions, inverse, *tensors):
+    jobs = [(_rows(t), torch.empty(t.shape, dtype=t.dtype, device=t.device), 1) for t in tensors if t is not None]
+    _rotary_call(rope, positions, inverse, jobs)
+    return [j[1] for j in jobs]
 
 
 def _rotary_torch(rope, positions, inverse, *tensors):
@@ -241,9 +234,8 @@ class _RotaryFn(torch.autograd.Function):
     def forward(ctx, rope, positions, q, k):
         ctx.rope, ctx.positions, ctx.pair = rope, positions, k is not None
         ctx.set_materialize_grads(False)
-        jobs = [(_rows(t)[0], torch.empty(t.shape, dtype=t.dtype, device=t.device), 1) for t in (q, k) if t is not None]
-        _rotary_call(rope, positions, 0, jobs)
-        return tuple(j[1] for j in jobs) + (() if ctx.pair else (None,))
+        out = _rotary_apply(rope, positions, 0, q, k)
+        return tuple(out) if ctx.pair else (out[0], None)
 
     @staticmethod
     def backward(ctx, dq, dk):
@@ -253,9 +245,7 @@ class _RotaryFn(torch.autograd.Function):
         if torch.is_grad_enabled() or not ctx.rope._usable(given[0], given[-1], ctx.positions):
             out = iter(_rotary_torch(ctx.rope, ctx.positions, True, *given))
         else:
-            jobs = [(_rows(t)[0], torch.empty(t.shape, dtype=t.dtype, device=t.device), 1) for t in given]
-            _rotary_call(ctx.rope, ctx.positions, 1, jobs)
-            out = (j[1] for j in jobs)
+            out = iter(_rotary_apply(ctx.rope, ctx.positions, 1, *given))
         dq, dk = (None if t is None else next(out) for t in (dq, dk))
         return None, None, dq, dk
 
@@ -285,7 +275,7 @@ class _RotaryQkvFn(torch.autograd.Function):
             return None, None, torch.stack((dq, dk, dv), 2)
         out = torch.empty(ctx.shape, dtype=dq.dtype, device=dq.device)
         _rotary_call(ctx.rope, ctx.positions, 1,
-                     [(_rows(g)[0], to, rotate) for g, to, rotate in zip((dq, dk, dv), out.unbind(2), (1, 1, 0))])
+                     [(_rows(g), to, rotate) for g, to, rotate in zip((dq, dk, dv), out.unbind(2), (1, 1, 0))])
         return None, None, out
 
 
@@ -340,35 +330,47 @@ def _attention_torch(q, k, v, window, sinks, lengths, scale):
     return torch.matmul(p, vw).to(q.dtype)
 
 
+FEW_ROWS = 128  # of the heads that share keys
+
+
 def attention_splits(b, heads, kv, lq, lk, window, sinks):
-    """Ranges of keys for the form that splits them (0: the form that splits the queries).
-    A wave of the split form takes 32 rows of the heads that share keys and a range of the
-    keys; 2048 waves fill the card, and a range has at least 4 tiles of 32 keys."""
-    blocks = b * kv * -(-(heads // kv) * lq // 32)
-    if lq * (heads // kv) > 128 or b * kv > 65535:
+    """Ranges of keys that are worked on apart and joined (0: the rows alone fill the card).
+    Up to FEW_ROWS rows share keys: a wave takes 32 of them and a range, of at least 4 tiles of
+    32 keys, or 8 past 1024 waves, and 2048 waves at most.  More rows: a workgroup takes 128 of
+    one head; ranges of at least 8 tiles of 64 keys where 256 workgroups are not reached.
+    One token, us by ranges (the rule's *), heads of 128: 4 sequences of up to 70000 keys, 8
+    heads of k: 16 270, 32 196, 64* 192, 128 186; one sequence: 64 77, 128 66, 256* 72, 512 86;
+    32 of 8192: 2 194, 8* 202, 16 213; heads of 64, 16 x 16 of 1028 keys: 2 18, 4* 19, 8 20, 16
+    21.  1000 rows of 16 heads over 20000 keys: 1 508, 2 281, 4* 191, 8 204."""
+    share = heads // kv * lq
+    if share <= FEW_ROWS and b * kv <= 65535:
+        blocks = b * kv * -(-share // 32)
+        tiles = -(-min(lk, window + sinks + lq) // 32)
+        splits = max(1, min(-(-2048 // blocks), tiles // 4))
+        return splits if blocks * splits <= 1024 else min(splits, max(-(-1024 // blocks), tiles // 8))
+    blocks = b * heads * -(-lq // 128)
+    if blocks >= 256 or b * heads * lq >= 1 << 24:
         return 0
-    tiles = -(-min(lk, window + sinks + lq) // 32)
-    return max(1, min(2048 // blocks, tiles // 4))
+    splits = min(512 // blocks, -(-min(lk, window + sinks + 128) // 64) // 8)
+    return splits if splits > 1 else 0
 
 
-def _attn_args(q, k, v, o, lse, lengths, window, sinks, scale):
-    a = _AttnArgs()
-    a.q, a.k, a.v, a.o, a.lse = q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr()
-    if lengths is not None:
-        a.lengths = lengths.data_ptr()
-    a.qs[:], a.ks[:], a.vs[:], a.os[:] = _strides(q), _strides(k), _strides(v), _strides(o)
-    a.b, a.heads, a.lq, a.hd = q.shape
-    a.kv, a.lk = k.shape[1:3]
-    a.window, a.sinks, a.scale = window, sinks, scale
-    return a
+def _attn_fields(q, k, v, o, lse, lengths, window, sinks, scale, splits=0, waves=0, part=0, part_lse=0):
+    b, heads, lq, hd = q.shape
+    _, kv, lk, _ = k.shape
+    return (q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
+            0 if lengths is None else lengths.data_ptr(), *_strides(q), *_strides(k), *_strides(v), *_strides(o), b, heads,
+            kv, lq, lk, hd, NO_WINDOW if window is None or window > NO_WINDOW else window, min(sinks, NO_WINDOW), scale,
+            splits, waves, part, part_lse)
 
 
-def _attn_tensors(*tensors):
-    """bf16 (b, heads, l, hd) tensors as the kernels take them, or None."""
-    if not all(_here(t) and t.dtype == _bf16 and t.numel() > 0 for t in tensors):
-        return None
-    # (rows that lie on one another, or so far apart that a tile of 64 passes 2^31 bytes, are copied)
-    return [_rows(t if t.shape[2] == 1 or t.shape[3] <= t.stride(2) <= MAX_ROW_STRIDE else t.contiguous())[0] for t in tensors]
+def _attn_tensor(t):
+    """A bf16 (b, heads, l, hd) tensor as the kernels take it: rows that lie on one another, or
+    so far apart that a tile of 64 passes 2^31 bytes, are copied too."""
+    _, _, l, hd = t.shape
+    if l > 1 and not hd <= t.stride(2) <= MAX_ROW_STRIDE:
+        t = t.contiguous()
+    return _rows(t)
 
 
 def _empty_heads(like, l=None):
@@ -377,10 +379,33 @@ def _empty_heads(like, l=None):
     return torch.empty(b, n, heads, hd, dtype=_bf16, device=like.device).transpose(1, 2)
 
 
-def _attn_scratch(args):
-    fn = _lib.load().compact_attention_bwd_scratch
-    fn.restype, fn.argtypes = _i64, [ctypes.POINTER(_AttnArgs)]
-    return fn(ctypes.byref(args))
+def _attn_scratch(block):
+    fn = _fns.get("scratch")
+    if fn is None:
+        fn = _fns["scratch"] = _lib.load().compact_attention_bwd_scratch
+        fn.restype, fn.argtypes = _i64, [_block]
+    return fn(block)
+
+
+_fns = {}
+
+
+def _attention_apply(q, k, v, window, sinks, lengths, scale):
+    """(q, k, v as the kernels take them, o, lse)"""
+    q, k, v = _attn_tensor(q), _attn_tensor(k), _attn_tensor(v)
+    b, heads, lq, hd = q.shape
+    _, kv, lk, _ = k.shape
+    o = _empty_heads(q)
+    lse = torch.empty(b, heads, lq, dtype=torch.float32, device=q.device)
+    splits = attention_splits(b, heads, kv, lq, lk, NO_WINDOW if window is None else window, sinks)
+    split = ()
+    if splits > 0:
+        rows = splits * b * heads * lq
+        part = torch.empty(rows * (hd + 1), dtype=torch.float32, device=q.device)
+        split = (splits, heads // kv * lq <= FEW_ROWS, part.data_ptr(), part.data_ptr() + 4 * rows * hd)
+    ops._call("compact_attention_fwd", _attn_pack(*_attn_fields(q, k, v, o, lse, lengths, window, sinks, scale, *split)),
+              _stream(q))
+    return q, k, v, o, lse
 
 
 class _AttentionFn(torch.autograd.Function):
@@ -388,53 +413,37 @@ class _AttentionFn(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, q, k, v, window, sinks, lengths, scale):
-        qr, kr, vr = _attn_tensors(q, k, v)
-        b, heads, lq, hd = q.shape
-        kv, lk = k.shape[1:3]
-        o = _empty_heads(q)
-        lse = torch.empty(b, heads, lq, dtype=torch.float32, device=q.device)
-        w = NO_WINDOW if window is None else min(window, NO_WINDOW)
-        a = _attn_args(qr, kr, vr, o, lse, lengths, w, min(sinks, NO_WINDOW), scale)
-        a.splits = attention_splits(b, heads, kv, lq, lk, w, a.sinks)
-        if a.splits > 0:
-            part = torch.empty(a.splits * b * heads * lq * (hd + 1), dtype=torch.float32, device=q.device)
-            a.part_o, a.part_lse = part.data_ptr(), part.data_ptr() + 4 * a.splits * b * heads * lq * hd
-        ops._call("compact_attention_fwd", ctypes.byref(a), _stream(q))
+        kept = _attention_apply(q, k, v, window, sinks, lengths, scale)
         ctx.rule = window, sinks, scale
-        ctx.save_for_backward(qr, kr, vr, o, lse, lengths)
-        return o
+        ctx.save_for_backward(*kept, lengths)
+        return kept[3]
 
     @staticmethod
     def backward(ctx, do):
         q, k, v, o, lse, lengths = ctx.saved_tensors
         window, sinks, scale = ctx.rule
         none = None, None, None, None
-        t = None
-        if not torch.is_grad_enabled() and _eager() and _plain(do) and ops._companion(lse, torch.float32, q.shape[:3].numel()):
-            t = _attn_tensors(q, k, v, o, do.to(_bf16))
-        if t is None:
+        if (torch.is_grad_enabled() or not _eager() or not _here(do) or not ops._companion(lse, torch.float32, q.shape[:3].numel())
+                or not all(_here(t) and t.dtype == _bf16 for t in (q, k, v, o))):
             recorded = torch.is_grad_enabled()
             with torch.enable_grad():
                 leaves = [x if recorded and x.requires_grad else x.detach().requires_grad_(True) for x in (q, k, v)]
                 y = _attention_torch(*leaves, window, sinks, lengths, scale)
                 return (*torch.autograd.grad(y, leaves, do, create_graph=recorded), *none)
-        q, k, v, o, do = t
-        w = NO_WINDOW if window is None else min(window, NO_WINDOW)
-        g = _AttnGradArgs()
-        g.f = _attn_args(q, k, v, o, lse, lengths, w, min(sinks, NO_WINDOW), scale)
+        q, k, v, o, do = (_attn_tensor(t) for t in (q, k, v, o, do.to(_bf16)))
+        fields = _attn_fields(q, k, v, o, lse, lengths, window, sinks, scale)
         dq, delta = _empty_heads(q), torch.empty_like(lse)
-        g.go, g.dq, g.delta = do.data_ptr(), dq.data_ptr(), delta.data_ptr()
-        g.gs[:], g.dqs[:] = _strides(do), _strides(dq)
         dk = dv = None
+        outs, strides, part = (0, 0), (0,) * 6, None
         if ctx.needs_input_grad[1] or ctx.needs_input_grad[2]:
             dk, dv = _empty_heads(k), _empty_heads(v)
-            g.dk, g.dv = dk.data_ptr(), dv.data_ptr()
-            g.dks[:], g.dvs[:] = _strides(dk), _strides(dv)
-            floats = _attn_scratch(g.f)
+            outs, strides = (dk.data_ptr(), dv.data_ptr()), _strides(dk) + _strides(dv)
+            floats = _attn_scratch(_attn_pack(*fields))
             if floats > 0:
                 part = torch.empty(floats, dtype=torch.float32, device=q.device)
-                g.part = part.data_ptr()
-        ops._call("compact_attention_bwd", ctypes.byref(g), _stream(q))
+        ops._call("compact_attention_bwd",
+                  _attn_grad_pack(*fields, do.data_ptr(), dq.data_ptr(), *outs, delta.data_ptr(), *_strides(do), *_strides(dq),
+                                  *strides, 0 if part is None else part.data_ptr(), 0, 0, 0, 0), _stream(q))
         return dq, dk, dv, *none
 
 
@@ -468,7 +477,9 @@ def window_attention(q, k, v, window=None, sinks=0, lengths=None, scale=None):
     if _eager() and _attention_usable(q, k, v):
         if lengths is not None:
             lengths = lengths.to(torch.int32).contiguous()
-        return _AttentionFn.apply(q, k, v, window, sinks, lengths, scale)
+        if _tracked(q, k, v):
+            return _AttentionFn.apply(q, k, v, window, sinks, lengths, scale)
+        return _attention_apply(q, k, v, window, sinks, lengths, scale)[3]
     return _attention_torch(q, k, v, window, sinks, lengths, scale)
 
 
@@ -515,22 +526,19 @@ def _distill_torch(logits, top_logits, top_ids, targets, temperature, weight):
 
 
 def _distill_call(logits, top, ids, targets, count, temperature, weight, loss=None, dx=None, dloss=None, unless_one=False):
-    a = _DistillArgs()
-    a.x, a.top, a.ids = logits.data_ptr(), top.data_ptr(), ids.data_ptr()
-    a.rows, a.V = logits.shape
-    a.K, a.top_ld, a.ids_ld = top.shape[1], top.stride(0), ids.stride(0)
-    a.f32, a.top32, a.ids32 = logits.dtype == torch.float32, top.dtype == torch.float32, ids.dtype == torch.int32
-    if targets is not None:
-        a.target, a.count, a.ignore_index = targets.data_ptr(), count.data_ptr(), ops.IGNORE
-    if loss is not None:
-        row = torch.empty(logits.shape[0], dtype=torch.float32, device=logits.device)
-        a.loss_row, a.loss = row.data_ptr(), loss.data_ptr()
-    if dx is not None:
-        a.dx = dx.data_ptr()
-    if dloss is not None:
-        a.dloss, a.unless_one = dloss.data_ptr(), unless_one
-    a.temperature, a.weight = temperature, weight
-    ops._call("compact_distill", ctypes.byref(a), _stream(logits))
+    rows, V = logits.shape
+    row = torch.empty(rows, dtype=torch.float32, device=logits.device) if loss is not None else None
+    at = lambda x: 0 if x is None else x.data_ptr()
+    ops._call("compact_distill",
+              _distill_pack(logits.data_ptr(), top.data_ptr(), ids.data_ptr(), at(targets), at(count), at(row), at(loss), at(dx),
+                            at(dloss), rows, V, top.stride(0), ids.stride(0), ops.IGNORE, top.shape[1],
+                            logits.dtype == torch.float32, top.dtype == torch.float32, ids.dtype == torch.int32, unless_one,
+                            temperature, weight), _stream(logits))
+
+
+def _distill_results(logits, targets):
+    loss = torch.empty((), dtype=torch.float32, device=logits.device)
+    return loss, torch.empty((), dtype=torch.float32, device=logits.device) if targets is not None else None
 
 
 class _DistillFn(torch.autograd.Function):
@@ -539,9 +547,8 @@ class _DistillFn(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, logits, top, ids, targets, temperature, weight):
-        loss = torch.empty((), dtype=torch.float32, device=logits.device)
-        count = torch.empty((), dtype=torch.float32, device=logits.device) if targets is not None else None
-        ctx.dx = torch.empty_like(logits) if ctx.needs_input_grad[0] else None
+        loss, count = _distill_results(logits, targets)
+        ctx.dx = torch.empty_like(logits)
         _distill_call(logits, top, ids, targets, count, temperature, weight, loss=loss, dx=ctx.dx)
         ctx.rule = temperature, weight
         ctx.save_for_backward(logits, top, ids, targets, count)
@@ -601,5 +608,9 @@ def distill_loss(logits, top_logits, top_ids, targets=None, temperature=1.0, wei
         top, ids = (t.detach() if t.stride(1) == 1 else t.detach().contiguous() for t in (top_logits, top_ids))
         targets = targets if targets is None else targets.contiguous()
         if not (top_logits.requires_grad and torch.is_grad_enabled()) and _distill_usable(dense, top, ids, targets):
-            return _DistillFn.apply(dense, top, ids, targets, temperature, weight)
+            if _tracked(dense):
+                return _DistillFn.apply(dense, top, ids, targets, temperature, weight)
+            loss, count = _distill_results(dense, targets)
+            _distill_call(dense, top, ids, targets, count, temperature, weight, loss=loss)
+            return loss
     return _distill_torch(logits, top_logits, top_ids, targets, temperature, weight)

@@ -134,11 +134,13 @@ def test_attention_refuses_types():
 
 
 def test_attention_splits_rule():
-    assert F.attention_splits(16, 16, 16, 1, 4096, 1024, 4) == 8      # 256 rows of waves, 33 tiles
+    assert F.attention_splits(16, 16, 16, 1, 4096, 1024, 4) == 4      # 256 waves of rows, 33 tiles
     assert F.attention_splits(4, 32, 8, 1, 70000, F.NO_WINDOW, 0) == 64
     assert F.attention_splits(1, 1, 1, 1, 1, F.NO_WINDOW, 0) == 1
     assert F.attention_splits(4, 16, 16, 4096, 4096, 1024, 4) == 0    # enough rows
     assert F.attention_splits(1 << 16, 1, 1, 1, 4096, 1024, 4) == 0   # past a grid's third dimension
+    assert F.attention_splits(1, 16, 4, 1000, 20000, F.NO_WINDOW, 0) == 4  # 128 workgroups of rows
+    assert F.attention_splits(1, 16, 4, 1000, 1000, 64, 4) == 0       # too few keys to split
 
 
 # ----------------------------- distillation ---------------------------------

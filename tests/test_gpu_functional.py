@@ -193,14 +193,17 @@ def test_attention(monkeypatch, case):
     o = F.window_attention(q, k, v, window=window, sinks=sinks, lengths=n)
     grads = torch.autograd.grad(o, (q, k, v), do)
     _check((o, *grads), q, k, v, do, window, sinks, n, scale)
-    # the other form of the forward, and the same again: bitwise
+    # the same again: bitwise; and the other forms of the forward
     again = F.window_attention(q, k, v, window=window, sinks=sinks, lengths=n)
     assert torch.equal(o, again)
     for x, y in zip(grads, torch.autograd.grad(again, (q, k, v), do)):
         assert torch.equal(x, y)
     splits = F.attention_splits(b, heads, kv, lq, lk, F.NO_WINDOW if window is None else window, sinks)
-    monkeypatch.setattr(F, "attention_splits", lambda *a: 3 if splits == 0 else 0)
-    _check((F.window_attention(q, k, v, window=window, sinks=sinks, lengths=n),), q, k, v, do, window, sinks, n, scale, "o")
+    for other, few in ((3 if splits == 0 else 0, F.FEW_ROWS), (3, 0), (2, 1 << 30)):
+        monkeypatch.setattr(F, "attention_splits", lambda *a: other)
+        monkeypatch.setattr(F, "FEW_ROWS", few)
+        o = F.window_attention(q, k, v, window=window, sinks=sinks, lengths=n)
+        _check((o,), q, k, v, do, window, sinks, n, scale, "o")
 
 
 @pytest.mark.parametrize("scale", [0.01, 3.0])
@@ -244,7 +247,7 @@ def test_attention_strides():
 
 @pytest.mark.parametrize("hd", [64, 128])
 @pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
-def test_attention_of_what_is_not_seen(hd, value):
+def test_attention_of_what_is_not_seen(monkeypatch, hd, value):
     """Keys past a length, outside the window and ahead hold anything: the rows that do not
     see them, and those rows' gradients, are as if it were not there."""
     b, h, l = 2, 2, 200
@@ -252,7 +255,9 @@ def test_attention_of_what_is_not_seen(hd, value):
     lengths = torch.tensor([l, 150], device=dev())
     rule = dict(window=20, sinks=2, lengths=lengths)
     seen = F._visible(l, l, lengths, 20, 2, dev())
-    for lq in (l, 3):  # either form of the forward
+    for lq, splits, few in ((l, 0, 0), (l, 3, 0), (3, 2, 128)):  # the forms of the forward
+        monkeypatch.setattr(F, "attention_splits", lambda *a: splits)
+        monkeypatch.setattr(F, "FEW_ROWS", few)
         clean = F.window_attention(q[:, :, -lq:], k, v, **rule)
         bk, bv = k.clone(), v.clone()
         bk[:, :, 100], bv[:, :, 100] = value, value
