@@ -11,8 +11,9 @@
 //
 // Bound by HBM: a row is read once and its gradient written once, by one workgroup that
 // holds it in registers: the maximum, the sums of exponentials and the gradient are three
-// walks over registers.  The gradient is formed where the loss is, for dloss = 1; the
-// backward runs the same kernel again, which ends at once where dloss is 1 indeed.
+// walks over registers, and the next row's loads are issued chunk by chunk behind the
+// gradient's.  The gradient is formed where the loss is, for dloss = 1; the backward runs
+// the same kernel again, which ends at once where dloss is 1 indeed.
 #include <hip/hip_runtime.h>
 
 #include "common.hpp"
@@ -28,275 +29,325 @@ constexpr int kMaxK = 1024;
 // a x b for a factor a that may be zero: then nothing, whatever b is.
 __device__ __forceinline__ float part(float a, float b) { return a == 0.0f ? 0.0f : a * b; }
 
-template <int NW>
-__device__ __forceinline__ float block_max(float v, float* s) {
+__device__ __forceinline__ float wave_max(float v) {
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor(v, d, 64));
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = s[0];
-#pragma unroll
-  for (int w = 1; w < NW; ++w) v = fmaxf(v, s[w]);
   return v;
 }
 
-template <int NW>
-__device__ __forceinline__ float block_sum(float v, float* s) {
+// A value that every lane holds, as a scalar.
+__device__ __forceinline__ float uniform(float v) {
+  return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v)));
+}
+
+__device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d, 64);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = s[0];
-#pragma unroll
-  for (int w = 1; w < NW; ++w) v += s[w];
   return v;
 }
 
-// The 16-byte chunks of the whole buffer that hold a row: an odd V starts rows anywhere, so
-// the first and last chunk have elements of the neighbours.
+// A row as the whole 16-byte chunks of the buffer that lie inside it and, an odd V starting
+// rows anywhere, up to two ends of single elements, one to a thread.
 template <bool F32>
 struct Row {
-  static constexpr int kN = F32 ? 4 : 8;
-  const u32x4* x;
-  int64_t begin, end, total, first;
-  int chunks;
-  __device__ __forceinline__ Row(const void* p, int64_t row, int64_t V, int64_t rows) {
-    x = static_cast<const u32x4*>(p);
+  static constexpr int kN = F32 ? 4 : 8, kSize = F32 ? 4 : 2;
+  static constexpr uint32_t kNone = F32 ? 0xFF800000u : 0xFF80FF80u;  // -inf
+  int64_t begin;    // the row's first element
+  int head, chunks, tail;  // elements before the first whole chunk, whole chunks, elements after
+  __device__ __forceinline__ Row(int64_t row, int64_t V) {
     begin = row * V;
-    end = begin + V;
-    total = rows * V;
-    first = begin / kN;
-    chunks = static_cast<int>((end + kN - 1) / kN - first);
+    const int off = static_cast<int>(begin % kN), v = static_cast<int>(V);
+    head = off == 0 ? 0 : kN - off;
+    head = head < v ? head : v;
+    chunks = (v - head) / kN;
+    tail = v - head - chunks * kN;
   }
-  __device__ __forceinline__ u32x4 load(const void* p, int c) const {
-    const int64_t e0 = (first + c) * kN;
-    if (e0 + kN <= total) return x[first + c];
-    u32x4 w = {0u, 0u, 0u, 0u};  // past the buffer's last whole chunk
+  // the element of the ends that is thread t's, or -1
+  __device__ __forceinline__ int end_of(int t) const { return t < head ? t : t < head + tail ? chunks * kN + t : -1; }
+  // The whole chunks from `skip` on as a buffer: loads past the last give zeros, stores nothing.
+  // (`some`: else an empty one, whose loads cost nothing.  A buffer for each of a thread's
+  // chunks lets all of them use the same offset: scalars instead of a register each.)
+  __device__ __forceinline__ __amdgpu_buffer_rsrc_t from(const void* x, bool some, int skip) const {
+    char* at = const_cast<char*>(static_cast<const char*>(x)) + (begin + head) * kSize + skip * 16;
+    return __builtin_amdgcn_make_buffer_rsrc(at, static_cast<short>(0), some && skip < chunks ? (chunks - skip) * 16 : 0, 0x00020000);
+  }
+  __device__ __forceinline__ u32x4 load(const void* x, bool some, int skip, int tid) const {
+    return __builtin_amdgcn_raw_buffer_load_b128(from(x, some, skip), tid * 16, 0, 0);
+  }
+  // -inf for what is past the last chunk.  (Not in load: it would wait there.)
+  __device__ __forceinline__ void ends(u32x4& w, int c) const {
 #pragma unroll
-    for (int e = 0; e < kN; ++e) {
-      if (e0 + e >= total) continue;
-      if constexpr (F32) w[e] = static_cast<const uint32_t*>(p)[e0 + e];
-      else w[e / 2] |= static_cast<uint32_t>(static_cast<const uint16_t*>(p)[e0 + e]) << (16 * (e & 1));
-    }
-    return w;
+    for (int k = 0; k < 4; ++k) w[k] = c < chunks ? w[k] : kNone;
   }
-  // element e of chunk c is the row's
-  __device__ __forceinline__ bool in(int c, int e) const {
-    const int64_t at = (first + c) * kN + e;
-    return at >= begin && at < end;
-  }
-  __device__ __forceinline__ bool whole(int c) const {
-    const int64_t at = (first + c) * kN;
-    return at >= begin && at + kN <= end;
-  }
-  static __device__ __forceinline__ float value(const u32x4& w, int e) {
-    if constexpr (F32) return __uint_as_float(w[e]);
-    else return __uint_as_float(e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
-  }
-  static __device__ __forceinline__ u32x4 pack(const float (&v)[kN]) {
+  __device__ __forceinline__ void store(void* x, int skip, int tid, const float (&v)[kN]) const {
     u32x4 w;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       if constexpr (F32) w[k] = __float_as_uint(v[k]);
       else w[k] = pack_bf16x2(v[2 * k], v[2 * k + 1]);
     }
-    return w;
+    __builtin_amdgcn_raw_buffer_store_b128(w, from(x, true, skip), tid * 16, 0, 0);
   }
-  static __device__ __forceinline__ float one(const void* p, int64_t at) {
-    if constexpr (F32) return static_cast<const float*>(p)[at];
-    else return bf16_to_f32(static_cast<const uint16_t*>(p)[at]);
+  static __device__ __forceinline__ float value(const u32x4& w, int e) {
+    if constexpr (F32) return __uint_as_float(w[e]);
+    else return __uint_as_float(e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
   }
-  static __device__ __forceinline__ void put(void* p, int64_t at, float v) {
-    if constexpr (F32) static_cast<float*>(p)[at] = v;
-    else static_cast<uint16_t*>(p)[at] = f32_to_bf16(v);
+  __device__ __forceinline__ float one(const void* x, uint32_t v) const {
+    if constexpr (F32) return (static_cast<const float*>(x) + begin)[v];
+    else return bf16_to_f32((static_cast<const uint16_t*>(x) + begin)[v]);
+  }
+  __device__ __forceinline__ void put(void* x, uint32_t v, float g) const {
+    if constexpr (F32) (static_cast<float*>(x) + begin)[v] = g;
+    else (static_cast<uint16_t*>(x) + begin)[v] = f32_to_bf16(g);
   }
 };
 
+// The teacher's entries of a row as the main kernel wants them, by one wave: distinct ids, each
+// with the sum of its p, and behind them the target's, if it is not among them, with p = 0.
+// Workgroup 0 counts the rows whose target counts.
+__global__ __launch_bounds__(256) void k_distill_entries(DistillArgs a) {
+  extern __shared__ __attribute__((aligned(16))) int lds[];  // per wave: K ids and K values, K to a multiple of 4
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, K4 = (a.K + 3) / 4 * 4;
+  if (blockIdx.x == 0) {
+    if (a.target == nullptr) return;
+    int c = 0;
+#pragma unroll 8
+    for (int64_t r = threadIdx.x; r < a.rows; r += 256) c += a.target[r] != a.ignore_index ? 1 : 0;
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) c += __shfl_xor(c, d, 64);
+    if (lane == 0) lds[wave] = c;
+    __syncthreads();
+    if (threadIdx.x == 0) a.count[0] = static_cast<float>(lds[0] + lds[1] + lds[2] + lds[3]);
+    return;
+  }
+  int* sid = lds + wave * 2 * K4;
+  float* sp = reinterpret_cast<float*>(sid + K4);
+  const int64_t row = (static_cast<int64_t>(blockIdx.x) - 1) * 4 + wave;
+  if (row >= a.rows) return;
+  const int64_t target = a.target != nullptr ? a.target[row] : a.ignore_index - 1;
+  const bool hard = a.target != nullptr && a.weight != 1.0f, aim = hard && target >= 0 && target < a.V;
+  const char* ids = static_cast<const char*>(a.ids) + row * a.ids_ld * (a.ids32 ? 4 : 8);
+  const char* top = static_cast<const char*>(a.top) + row * a.top_ld * (a.top32 ? 4 : 2);
+  const float ninf = -__builtin_inff(), rT = 1.0f / a.temperature;
+  bool bad = hard && !aim, among = false;
+  float m = ninf;
+  for (int k = lane; k < K4; k += 64) {
+    int id = -1;
+    float t = ninf;
+    if (k < a.K) {
+      const int64_t given = a.ids32 ? reinterpret_cast<const int32_t*>(ids)[k] : reinterpret_cast<const int64_t*>(ids)[k];
+      t = a.top32 ? reinterpret_cast<const float*>(top)[k] : bf16_to_f32(reinterpret_cast<const uint16_t*>(top)[k]);
+      t = given < 0 ? ninf : t * rT;
+      bad |= given >= a.V;
+      id = given < 0 || given >= a.V ? -1 : static_cast<int>(given);
+      among |= aim && given == target;
+    }
+    sid[k] = id;
+    sp[k] = t;
+    m = fmaxf(m, t);
+  }
+  if (a.target != nullptr && target == a.ignore_index) return;
+  m = wave_max(m);
+  if (m == ninf) m = 0.0f;
+  float s = 0.0f;
+  for (int k = lane; k < K4; k += 64) s += expf(sp[k] - m);
+  s = wave_sum(s);
+  const float lse = m + logf(s);
+  const bool some = !(s == 0.0f);  // (a NaN is an entry)
+  float h = 0.0f;
+  for (int k = lane; k < K4; k += 64) {
+    const float lp = sp[k] - lse, p = some ? expf(lp) : 0.0f;
+    h += part(p, lp);
+    sp[k] = p;
+  }
+  h = wave_sum(h);
+  int2* out = reinterpret_cast<int2*>(a.entries) + row * (a.K + 1);
+  for (int k = lane; k < a.K; k += 64) {
+    const int id = sid[k];
+    float p = 0.0f;
+    int before = 0;  // equal ids before this one: the first has the sum of all
+#pragma unroll 4
+    for (int j = 0; j < K4; j += 4) {
+      const int4 v = *reinterpret_cast<const int4*>(sid + j);
+      const float4 q = *reinterpret_cast<const float4*>(sp + j);
+      p += (v.x == id ? q.x : 0.0f) + (v.y == id ? q.y : 0.0f) + (v.z == id ? q.z : 0.0f) + (v.w == id ? q.w : 0.0f);
+      before |= ((v.x == id) & (j < k)) | ((v.y == id) & (j + 1 < k)) | ((v.z == id) & (j + 2 < k)) | ((v.w == id) & (j + 3 < k));
+    }
+    const bool one = id >= 0 && !before;
+    out[k] = make_int2(one ? id : -1, __float_as_int(one ? p : 0.0f));
+  }
+  among = __any(among);
+  bad = __any(bad);
+  if (lane == 0) {
+    out[a.K] = make_int2(aim && !among ? static_cast<int>(target) : -1, 0);
+    a.stats[2 * row] = bad ? __builtin_nanf("") : h;
+    a.stats[2 * row + 1] = some ? 1.0f : 0.0f;
+  }
+}
+
 // One row per workgroup at a time; NC chunks per thread in registers, any more are read again
-// for each walk.
-template <bool F32, int THREADS, int NC>
-__global__ __launch_bounds__(THREADS) void k_distill(DistillArgs a) {
+// for each walk.  HARD: the targets have a part; TWO: at another temperature than the teacher.
+template <bool F32, int THREADS, int NC, bool HARD, bool TWO>
+__global__ __launch_bounds__(THREADS, 4) void k_distill(DistillArgs a) {
   using R = Row<F32>;
   constexpr int N = R::kN, NW = THREADS / 64;
-  __shared__ float red[NW];
-  __shared__ float sp[kMaxK];
-  __shared__ int sid[kMaxK];
-  const int tid = threadIdx.x;
-  const float ninf = -__builtin_inff();
+  __shared__ float smax[NW], ssum[NW][3];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const float ninf = -__builtin_inff(), nan = __builtin_nanf("");
   float scale = 1.0f;
   if (a.dloss != nullptr) {
     scale = a.dloss[0];
     if (a.unless_one && scale == 1.0f) return;
   }
-  scale /= a.target != nullptr ? a.count[0] : static_cast<float>(a.rows);
-  const float T = a.temperature, rT = 1.0f / T, w = a.weight;
-  const bool hard = a.target != nullptr && w != 1.0f;
-  // one sum serves both where the temperature is 1
-  const bool two = hard && T != 1.0f;
+  scale = uniform(scale / (a.target != nullptr ? a.count[0] : static_cast<float>(a.rows)));
+  const float T = a.temperature, rT = uniform(1.0f / T), w = a.weight, cT = uniform(kLog2e * rT);
+  const int entries = a.K + 1;
 
+  u32x4 x[NC];
+  float xe;   // this thread's single element
+  int2 entry; // this thread's entry (any more are read where they are used)
+  int64_t target;
+  bool live;  // else the row has no part: no loss, no gradient, and nothing is read
+  auto head_of = [&](int64_t row) {
+    target = a.target != nullptr && row < a.rows ? a.target[row] : 0;
+    live = row < a.rows && (a.target == nullptr || target != a.ignore_index);
+  };
+  auto load_ends = [&](const R& r, int64_t row) {
+    xe = live && r.end_of(tid) >= 0 ? r.one(a.x, r.end_of(tid)) : ninf;
+    entry = make_int2(-1, 0);
+    if (live && tid < entries) entry = reinterpret_cast<const int2*>(a.entries)[row * entries + tid];
+  };
+  head_of(blockIdx.x);
+  {
+    const R r(live ? blockIdx.x : 0, a.V);
+    load_ends(r, blockIdx.x);
+#pragma unroll
+    for (int i = 0; i < NC; ++i) x[i] = r.load(a.x, live, THREADS * i, tid);
+  }
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    const R r(a.x, row, a.V, a.rows);
-    const int64_t target = a.target != nullptr ? a.target[row] : 0;
-    if (a.target != nullptr && target == a.ignore_index) {  // the row has no part: no gradient
-      if (a.loss_row != nullptr && tid == 0) a.loss_row[row] = 0.0f;
-      if (a.dx != nullptr) {
-        for (int c = tid; c < r.chunks; c += THREADS) {
-          if (r.whole(c)) {
-            static_cast<u32x4*>(a.dx)[r.first + c] = u32x4{0u, 0u, 0u, 0u};
-          } else {
+    const R r(row, a.V);
+    const bool now = live;
+    const int64_t aim = target;
+    float m = xe, lT = 0.0f, l1 = 0.0f, gT = 0.0f, g1 = 0.0f, xv = 0.0f;
+    if (now) {
+      // logits that the entries and the target name, on their way while the row is walked
+      if (entry.x >= 0) xv = r.one(a.x, entry.x);
+      float xt = 0.0f;
+      if (HARD && tid == 0 && aim >= 0 && aim < a.V) xt = r.one(a.x, static_cast<uint32_t>(aim));
+      const float h = a.stats[2 * row];
+      const bool soft = a.stats[2 * row + 1] != 0.0f;
+      // f(chunk's words) over this thread's chunks.  (Each walk unpacks the words again: kept from
+      // one to the next, the values would take twice the registers.)
+      auto walk = [&](auto f) {
 #pragma unroll
-            for (int e = 0; e < N; ++e)
-              if (r.in(c, e)) R::put(a.dx, (r.first + c) * N + e, 0.0f);
-          }
+        for (int i = 0; i < NC; ++i) {
+          f(x[i]);
+          asm volatile("" : "+v"(x[i]));
+          __builtin_amdgcn_sched_barrier(0);
         }
-      }
-      continue;
-    }
-    u32x4 x[NC];
+#pragma unroll 1
+        for (int c = THREADS * NC; c + tid < r.chunks; c += THREADS) f(r.load(a.x, true, c, tid));
+      };
 #pragma unroll
-    for (int i = 0; i < NC; ++i) {
-      const int c = tid + THREADS * i;
-      if (c < r.chunks) x[i] = r.load(a.x, c);
-    }
-    // f(chunk's words, chunk) over this thread's chunks
-    auto walk = [&](auto f) {
-#pragma unroll
-      for (int i = 0; i < NC; ++i) {
-        const int c = tid + THREADS * i;
-        if (c < r.chunks) f(x[i], c);
-      }
-      for (int c = tid + THREADS * NC; c < r.chunks; c += THREADS) f(r.load(a.x, c), c);
-    };
-    // the teacher's entries
-    bool bad = hard && (target < 0 || target >= a.V);
-    __syncthreads();  // the last row's readers of sp, sid
-    float tm = ninf;
-    for (int k = tid; k < a.K; k += THREADS) {
-      const int64_t id = a.ids32 ? static_cast<const int32_t*>(a.ids)[row * a.ids_ld + k]
-                                 : static_cast<const int64_t*>(a.ids)[row * a.ids_ld + k];
-      float t = ninf;
-      if (id >= 0) t = rT * (a.top32 ? static_cast<const float*>(a.top)[row * a.top_ld + k]
-                                     : bf16_to_f32(static_cast<const uint16_t*>(a.top)[row * a.top_ld + k]));
-      bad |= id >= a.V;
-      sp[k] = t;
-      sid[k] = id < 0 || id >= a.V ? -1 : static_cast<int>(id);
-      tm = fmaxf(tm, t);
-    }
-    tm = block_max<NW>(tm, red);
-    const float tsh = tm == ninf ? 0.0f : tm;
-    float ts = 0.0f;
-    for (int k = tid; k < a.K; k += THREADS) ts += expf(sp[k] - tsh);
-    ts = block_sum<NW>(ts, red);
-    const float tlse = tsh + logf(ts);
-    const bool soft = !(ts == 0.0f);  // some entry (a NaN is one)
-
-    float m = ninf;
-    walk([&](const u32x4& c, int at) {
-      if (r.whole(at)) {
+      for (int i = 0; i < NC; ++i) r.ends(x[i], tid + THREADS * i);
+      walk([&](const u32x4& c) {
 #pragma unroll
         for (int e = 0; e < N; ++e) m = fmaxf(m, R::value(c, e));
-      } else {
+      });
+      m = wave_max(m);
+      if (lane == 0) smax[wave] = m;
+      __syncthreads();
+      m = wave_max(smax[lane & (NW - 1)]);
+      m = uniform(m == ninf ? 0.0f : m);
+      // sums of 2^(cT (x - m)), of the same at temperature 1, and of the entries' p (x - m) / T
+      float s1 = __builtin_amdgcn_exp2f((xe - m) * kLog2e), sT = __builtin_amdgcn_exp2f((xe - m) * cT), sx = 0.0f;
+      walk([&](const u32x4& c) {
 #pragma unroll
-        for (int e = 0; e < N; ++e)
-          if (r.in(at, e)) m = fmaxf(m, R::value(c, e));
+        for (int e = 0; e < N; ++e) {
+          const float d = R::value(c, e) - m;
+          sT += __builtin_amdgcn_exp2f(d * cT);
+          if constexpr (TWO) s1 += __builtin_amdgcn_exp2f(d * kLog2e);
+        }
+      });
+      if (a.loss_row != nullptr) {
+        // (p / T first: (x - m) / T may leave fp32's range where p brings it back)
+        sx = part(__int_as_float(entry.y) * rT, xv - m);
+#pragma unroll 1
+        for (int k = tid + THREADS; k < entries; k += THREADS) {
+          const int2 n = reinterpret_cast<const int2*>(a.entries)[row * entries + k];
+          if (n.x >= 0) sx += part(__int_as_float(n.y) * rT, r.one(a.x, n.x) - m);
+        }
+        sx = wave_sum(sx);
       }
-    });
-    m = block_max<NW>(m, red);
-    if (m == ninf) m = 0.0f;
-    // sums of 2^(c1 (x - m)), temperature 1, and 2^(cT (x - m))
-    const float c1 = kLog2e, cT = kLog2e * rT;
-    float s1 = 0.0f, sT = 0.0f;
-    walk([&](const u32x4& c, int at) {
-      const bool all = r.whole(at);
-#pragma unroll
-      for (int e = 0; e < N; ++e) {
-        if (!all && !r.in(at, e)) continue;
-        const float d = R::value(c, e) - m;
-        sT += __builtin_amdgcn_exp2f(d * cT);
-        if (two) s1 += __builtin_amdgcn_exp2f(d * c1);
+      sT = wave_sum(sT);
+      if constexpr (TWO) s1 = wave_sum(s1);
+      if (lane == 0) {
+        ssum[wave][0] = sT;
+        ssum[wave][1] = s1;
+        ssum[wave][2] = sx;
       }
-    });
-    sT = block_sum<NW>(sT, red);
-    s1 = two ? block_sum<NW>(s1, red) : sT;
-    // log q_v = (x_v - m) / T - lT
-    const float lT = logf(sT), l1 = logf(s1);
-    if (a.loss_row != nullptr) {
-      float kl = 0.0f;
-      for (int k = tid; k < a.K; k += THREADS) {
-        if (sid[k] < 0) continue;
-        const float lp = sp[k] - tlse, p = expf(lp);
-        // (x_v - m) / T may leave fp32's range where p brings it back
-        kl += part(p, lp + lT) - part(p * rT, R::one(a.x, r.begin + sid[k]) - m);
+      __syncthreads();
+      // (the waves' sums by lanes: as registers they would be too many beside the row)
+      sT = wave_sum(lane < NW ? ssum[lane & (NW - 1)][0] : 0.0f);
+      s1 = TWO ? wave_sum(lane < NW ? ssum[lane & (NW - 1)][1] : 0.0f) : sT;
+      sx = a.loss_row != nullptr ? wave_sum(lane < NW ? ssum[lane & (NW - 1)][2] : 0.0f) : 0.0f;
+      // log q_v = (x_v - m) / T - lT
+      lT = uniform(logf(sT));
+      l1 = TWO ? uniform(logf(s1)) : lT;
+      if (a.loss_row != nullptr && tid == 0) {
+        float loss = soft ? w * T * T * (h + lT - sx) : 0.0f;
+        if (HARD) loss += (1.0f - w) * (l1 - (xt - m));
+        a.loss_row[row] = h != h ? nan : loss;
       }
-      kl = block_sum<NW>(kl, red);
-      bad = __syncthreads_or(bad);
-      if (tid == 0) {
-        float loss = soft ? w * T * T * kl : 0.0f;
-        if (hard && !bad) loss += (1.0f - w) * (l1 - (R::one(a.x, r.begin + target) - m));
-        a.loss_row[row] = bad ? __builtin_nanf("") : loss;
-      }
-    } else {
-      bad = __syncthreads_or(bad);
+      gT = h != h ? nan : soft ? scale * w * T : 0.0f;
+      g1 = HARD ? scale * (1.0f - w) : 0.0f;
+    } else if (a.loss_row != nullptr && tid == 0) {
+      a.loss_row[row] = 0.0f;
     }
-    if (a.dx == nullptr) continue;
-    const float nan = __builtin_nanf("");
-    const float gT = bad ? nan : soft ? scale * w * T : 0.0f, g1 = hard ? scale * (1.0f - w) : 0.0f;
     // gradient of a logit without its teacher's or target's part
     const float oT = lT * kLog2e, o1 = l1 * kLog2e;
     auto base = [&](float v) {
       const float d = v - m;
-      float g = part(gT, __builtin_amdgcn_exp2f(__builtin_fmaf(d, cT, -oT)));
-      if (hard) g += g1 * __builtin_amdgcn_exp2f(__builtin_fmaf(d, c1, -o1));
-      return g;
+      if constexpr (!TWO) return part(gT + g1, __builtin_amdgcn_exp2f(__builtin_fmaf(d, cT, -oT)));
+      return part(gT, __builtin_amdgcn_exp2f(__builtin_fmaf(d, cT, -oT))) +
+             part(g1, __builtin_amdgcn_exp2f(__builtin_fmaf(d, kLog2e, -o1)));
     };
-    walk([&](const u32x4& c, int at) {
+    auto grad = [&](const u32x4& c, int skip) {
       float g[N];
 #pragma unroll
       for (int e = 0; e < N; ++e) g[e] = base(R::value(c, e));
-      if (r.whole(at)) {
-        static_cast<u32x4*>(a.dx)[r.first + at] = R::pack(g);
-      } else {
-#pragma unroll
-        for (int e = 0; e < N; ++e)
-          if (r.in(at, e)) R::put(a.dx, (r.first + at) * N + e, g[e]);
-      }
-    });
-    // the teacher's entries and the target, over what the walk wrote
-    __syncthreads();
-    for (int k = tid; k < a.K + 1; k += THREADS) {
-      const bool is_target = k == a.K;
-      if (is_target ? !hard || target < 0 || target >= a.V : sid[k] < 0) continue;
-      const int v = is_target ? static_cast<int>(target) : sid[k];
-      // the first of equal ids writes the sum of all
-      float p = 0.0f;
-      bool first = true;
-      for (int j = 0; j < a.K; ++j) {
-        if (sid[j] != v) continue;
-        first = first && j >= k;
-        p += expf(sp[j] - tlse);
-      }
-      if (!first) continue;
-      float g = base(R::one(a.x, r.begin + v)) - part(gT, p);
-      if (hard && v == target) g -= g1;
-      R::put(a.dx, r.begin + v, g);
+      r.store(a.dx, skip, tid, g);
+    };
+    const int2 named = entry;
+    if (a.dx != nullptr) {
+      if (r.end_of(tid) >= 0) r.put(a.dx, r.end_of(tid), base(xe));
+#pragma unroll 1
+      for (int c = THREADS * NC; c + tid < r.chunks; c += THREADS) grad(r.load(a.x, true, c, tid), c);
     }
-  }
-}
-
-// Rows whose target counts.
-__global__ __launch_bounds__(1024) void k_distill_count(DistillArgs a) {
-  __shared__ int s[16];
-  int c = 0;
-  for (int64_t r = threadIdx.x; r < a.rows; r += 1024) c += a.target[r] != a.ignore_index ? 1 : 0;
+    const int64_t next_row = row + gridDim.x;
+    head_of(next_row);
+    const R next(live ? next_row : row, a.V);
+    load_ends(next, next_row);
 #pragma unroll
-  for (int d = 32; d > 0; d >>= 1) c += __shfl_xor(c, d, 64);
-  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = c;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int w = 1; w < 16; ++w) c += s[w];
-    a.count[0] = static_cast<float>(c);
+    for (int i = 0; i < NC; ++i) {
+      if (a.dx != nullptr) grad(x[i], THREADS * i);
+      x[i] = next.load(a.x, live, THREADS * i, tid);
+      __builtin_amdgcn_sched_barrier(0);  // (all loads at once would want registers of their own)
+    }
+    if (a.dx == nullptr || !now) continue;
+    // the entries and the target, over what the walk wrote
+    __syncthreads();
+    auto fix = [&](const int2& n, float v) {
+      float g = base(v) - part(gT, __int_as_float(n.y));
+      if (HARD && n.x == aim) g -= g1;
+      r.put(a.dx, n.x, g);
+    };
+    if (named.x >= 0) fix(named, xv);
+#pragma unroll 1
+    for (int k = tid + THREADS; k < entries; k += THREADS) {
+      const int2 n = reinterpret_cast<const int2*>(a.entries)[row * entries + k];
+      if (n.x >= 0) fix(n, r.one(a.x, n.x));
+    }
   }
 }
 
@@ -317,15 +368,25 @@ __global__ __launch_bounds__(1024) void k_distill_mean(DistillArgs a) {
   }
 }
 
+template <bool F32, int THREADS, int NC>
+void launch_row(const DistillArgs& a, hipStream_t s) {
+  // as many workgroups as the card holds, each with its share of the rows
+  const int64_t most = 256 * ((NC > 4 ? 1024 : 1536) / THREADS);
+  const dim3 grid(static_cast<uint32_t>(a.rows < most ? a.rows : most)), block(THREADS);
+  const bool hard = a.target != nullptr && a.weight != 1.0f;
+  if (!hard) hipLaunchKernelGGL((k_distill<F32, THREADS, NC, false, false>), grid, block, 0, s, a);
+  else if (a.temperature == 1.0f) hipLaunchKernelGGL((k_distill<F32, THREADS, NC, true, false>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((k_distill<F32, THREADS, NC, true, true>), grid, block, 0, s, a);
+}
+
 template <bool F32>
 void launch(const DistillArgs& a, hipStream_t s) {
-  const int64_t chunks = ceil_div(a.V, F32 ? 4 : 8) + 1;
-  const int64_t most = a.unless_one ? 2048 : (int64_t(1) << 22) - 1;
-  const dim3 grid(static_cast<uint32_t>(a.rows < most ? a.rows : most));
-  if (chunks <= 256) hipLaunchKernelGGL((k_distill<F32, 256, 1>), grid, dim3(256), 0, s, a);
-  else if (chunks <= 1024) hipLaunchKernelGGL((k_distill<F32, 256, 4>), grid, dim3(256), 0, s, a);
-  else if (chunks <= 4096) hipLaunchKernelGGL((k_distill<F32, 256, 16>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((k_distill<F32, 1024, 16>), grid, dim3(1024), 0, s, a);
+  const int64_t chunks = a.V / (F32 ? 4 : 8);
+  if (chunks <= 256) launch_row<F32, 256, 1>(a, s);
+  else if (chunks <= 1024) launch_row<F32, 256, 4>(a, s);
+  else if (chunks <= 4096 + 128) launch_row<F32, 256, 16>(a, s);
+  else if (chunks <= 8192 + 256) launch_row<F32, 512, 16>(a, s);
+  else launch_row<F32, 1024, 16>(a, s);
 }
 
 }  // namespace
@@ -334,11 +395,13 @@ void launch(const DistillArgs& a, hipStream_t s) {
 using namespace compact;
 
 extern "C" int compact_distill(const DistillArgs* a, void* stream) {
-  if (a->rows < 1 || a->rows > 0x7FFFFFFF || a->V < 1 || a->V > int64_t(1) << 30 || a->K < 1 || a->K > kMaxK ||
+  if (a->rows < 1 || a->rows > 0x7FFFFFFF || a->V < 1 || a->V > int64_t(1) << 28 || a->K < 1 || a->K > kMaxK ||
       !(a->temperature > 0.0f))
     return -1;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (a->target != nullptr && a->loss_row != nullptr) hipLaunchKernelGGL(k_distill_count, dim3(1), dim3(1024), 0, s, *a);
+  if (!a->ready)
+    hipLaunchKernelGGL(k_distill_entries, dim3(static_cast<uint32_t>(ceil_div(a->rows, 4) + 1)), dim3(256),
+                       4 * 2 * sizeof(int) * ((a->K + 3) / 4 * 4), s, *a);
   if (a->f32) launch<true>(*a, s);
   else launch<false>(*a, s);
   if (a->loss_row != nullptr) hipLaunchKernelGGL(k_distill_mean, dim3(1), dim3(1024), 0, s, *a);

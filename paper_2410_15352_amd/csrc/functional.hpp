@@ -64,9 +64,12 @@ struct DistillArgs {
   float* loss;                   // their mean
   void* dx;                      // gradient of x, or NULL
   const float* dloss;            // NULL: 1
+  float* entries;                // [rows][K + 1] pairs of scratch
+  float* stats;                  // [rows] pairs of scratch
   int64_t rows, V, top_ld, ids_ld, ignore_index;
   int32_t K, f32, top32, ids32;
   int32_t unless_one;            // with dloss: nothing to do where that is 1
+  int32_t ready;                 // entries, stats and count are those of an earlier call
   float temperature, weight;
 };
 

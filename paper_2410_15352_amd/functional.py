@@ -34,7 +34,7 @@ _ROTARY = struct.Struct("@" + 3 * "2Q6q2i" + "2Q4q8if").pack
 _ATTN = "6Q12q8if2i2Q"
 _attn_pack = struct.Struct("@" + _ATTN).pack
 _attn_grad_pack = struct.Struct("@" + _ATTN + "5Q12qQ4i").pack
-_distill_pack = struct.Struct("@9Q5q5i2f").pack
+_distill_pack = struct.Struct("@11Q5q6i2f").pack
 _block = ctypes.c_char_p
 
 ops._SIGNATURES.update({
@@ -525,20 +525,24 @@ def _distill_torch(logits, top_logits, top_ids, targets, temperature, weight):
     return (torch.where(counts, loss, 0.0).sum() / counts.sum()).to(torch.float64 if wide == torch.float64 else torch.float32)
 
 
-def _distill_call(logits, top, ids, targets, count, temperature, weight, loss=None, dx=None, dloss=None, unless_one=False):
+def _distill_call(logits, top, ids, targets, scratch, temperature, weight, loss=None, dx=None, dloss=None, unless_one=False):
+    """`scratch`: the call's own, or an earlier call's on the same tensors, whose reading of the
+    teacher it holds."""
     rows, V = logits.shape
-    row = torch.empty(rows, dtype=torch.float32, device=logits.device) if loss is not None else None
+    K = top.shape[1]
+    ready = scratch is not None
+    if not ready:  # per row K + 1 pairs and a pair, and the loss; the count
+        scratch = torch.empty(rows * (2 * K + 5) + 1, dtype=torch.float32, device=logits.device)
+    entries = scratch.data_ptr()
+    stats = entries + 8 * rows * (K + 1)
     at = lambda x: 0 if x is None else x.data_ptr()
     ops._call("compact_distill",
-              _distill_pack(logits.data_ptr(), top.data_ptr(), ids.data_ptr(), at(targets), at(count), at(row), at(loss), at(dx),
-                            at(dloss), rows, V, top.stride(0), ids.stride(0), ops.IGNORE, top.shape[1],
-                            logits.dtype == torch.float32, top.dtype == torch.float32, ids.dtype == torch.int32, unless_one,
-                            temperature, weight), _stream(logits))
-
-
-def _distill_results(logits, targets):
-    loss = torch.empty((), dtype=torch.float32, device=logits.device)
-    return loss, torch.empty((), dtype=torch.float32, device=logits.device) if targets is not None else None
+              _distill_pack(logits.data_ptr(), top.data_ptr(), ids.data_ptr(), at(targets), stats + 12 * rows,
+                            0 if loss is None else stats + 8 * rows, at(loss), at(dx), at(dloss), entries, stats, rows, V,
+                            top.stride(0), ids.stride(0), ops.IGNORE, K, logits.dtype == torch.float32,
+                            top.dtype == torch.float32, ids.dtype == torch.int32, unless_one, ready, temperature, weight),
+              _stream(logits))
+    return scratch
 
 
 class _DistillFn(torch.autograd.Function):
@@ -547,16 +551,16 @@ class _DistillFn(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, logits, top, ids, targets, temperature, weight):
-        loss, count = _distill_results(logits, targets)
+        loss = torch.empty((), dtype=torch.float32, device=logits.device)
         ctx.dx = torch.empty_like(logits)
-        _distill_call(logits, top, ids, targets, count, temperature, weight, loss=loss, dx=ctx.dx)
+        ctx.scratch = _distill_call(logits, top, ids, targets, None, temperature, weight, loss=loss, dx=ctx.dx)
         ctx.rule = temperature, weight
-        ctx.save_for_backward(logits, top, ids, targets, count)
+        ctx.save_for_backward(logits, top, ids, targets)
         return loss
 
     @staticmethod
     def backward(ctx, dloss):
-        logits, top, ids, targets, count = ctx.saved_tensors
+        logits, top, ids, targets = ctx.saved_tensors
         rule = ctx.rule
         if torch.is_grad_enabled() or not _eager() or not _plain(dloss) or not _distill_usable(logits, top, ids, targets):
             return (ops._torch_grad(lambda t: _distill_torch(t, top, ids, targets, *rule), logits, dloss),
@@ -564,14 +568,14 @@ class _DistillFn(torch.autograd.Function):
         dx, ctx.dx = ctx.dx, None
         first = dx is not None  # a second backward over a retained graph forms its own
         dx = dx if first else torch.empty_like(logits)
-        _distill_call(logits, top, ids, targets, count, *rule, dx=dx, dloss=dloss.float(), unless_one=first)
+        _distill_call(logits, top, ids, targets, ctx.scratch, *rule, dx=dx, dloss=dloss.float(), unless_one=first)
         return dx, None, None, None, None, None
 
 
 def _distill_usable(logits, top, ids, targets):
     return (logits.dtype in (_bf16, torch.float32) and top.dtype in (_bf16, torch.float32)
             and all(_here(t) for t in (logits, top, ids)) and logits.is_contiguous() and logits.data_ptr() % 16 == 0
-            and 0 < logits.shape[0] < ops.MAX_ROWS and 0 < logits.shape[1] <= 1 << 30 and 1 <= top.shape[1] <= MAX_TOP
+            and 0 < logits.shape[0] < ops.MAX_ROWS and 0 < logits.shape[1] <= 1 << 28 and 1 <= top.shape[1] <= MAX_TOP
             and top.stride(1) == 1 and ids.stride(1) == 1 and (targets is None or _here(targets) and targets.is_contiguous()))
 
 
@@ -610,7 +614,7 @@ def distill_loss(logits, top_logits, top_ids, targets=None, temperature=1.0, wei
         if not (top_logits.requires_grad and torch.is_grad_enabled()) and _distill_usable(dense, top, ids, targets):
             if _tracked(dense):
                 return _DistillFn.apply(dense, top, ids, targets, temperature, weight)
-            loss, count = _distill_results(dense, targets)
-            _distill_call(dense, top, ids, targets, count, temperature, weight, loss=loss)
+            loss = torch.empty((), dtype=torch.float32, device=dense.device)
+            _distill_call(dense, top, ids, targets, None, temperature, weight, loss=loss)
             return loss
     return _distill_torch(logits, top_logits, top_ids, targets, temperature, weight)
