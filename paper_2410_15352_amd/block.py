@@ -15,7 +15,7 @@ The saved activations of one block are then exactly Table 7's list:
     (one storage), x_act | x7 or z_down
 and block_saved_bytes() gives that sum.  Rotary positions (rope=Rotary(...)) turn q and k
 where they stand and save nothing; a window with sinks takes the place of the library's
-attention and saves the same list without its two scalars.
+attention: it saves one byte more for each element of x3, and no dropout state.
 """
 from __future__ import annotations
 

@@ -29,6 +29,12 @@ typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
 typedef __attribute__((address_space(3))) void lds_void;
 
 constexpr float kLog2e = 1.44269504088896340736f;
+// Rows that see this many keys at most have dS in two bf16 parts in the gradients' products.
+// dS rounded to bf16 alone leaves dq and dk, rounded themselves, 1.42 times as far from the
+// exact gradients as their own rounding; with few keys to a row the error of o in D comes on
+// top (1.49 at windows of 16 and 20).  In two parts: 1.02 to 1.08.  Two more products of nine:
+// 8% of the backward's time with heads of 64, 17% with heads of 128, where windows are long.
+constexpr int kFineKeys = 512;
 constexpr int kBN = 64;  // keys (or queries) per staged tile
 
 // A tile of rows of HD bf16 in LDS, 16-byte chunk c of row r at chunk c ^ swz(r): the 16
@@ -206,6 +212,16 @@ __device__ __forceinline__ bool not_finite(const f32x16 (&acc)[N]) {
   return !(z == 0.0f);
 }
 
+// What pack_steps' rounding took off, as operands of their own.
+__device__ __forceinline__ void pack_rest(const f32x16& p, const u32x4 (&hi)[2], u32x4 (&out)[2]) {
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+      out[t][w] = pack_bf16x2(p[8 * t + 2 * w] - __uint_as_float(hi[t][w] << 16),
+                              p[8 * t + 2 * w + 1] - __uint_as_float(hi[t][w] & 0xFFFF0000u));
+}
+
 // The tiles of TN keys that rows at positions pmin .. pmax (of L keys) see: the sinks' tiles
 // before the window's, then the window's.
 template <int TN>
@@ -244,18 +260,40 @@ __device__ __forceinline__ int length_of(const AttnArgs& a, int b) {
   return L < 0 ? 0 : L > a.lk ? a.lk : L;
 }
 
+// What rounding to bf16 took off a value, as a byte: in 127ths of half a unit in the last place
+// of the rounded value (bits r; none for the smallest numbers, infinities and NaN).
+__device__ __forceinline__ float half_place(uint32_t r, int sign) {
+  const int e = static_cast<int>((r >> 7) & 0xFFu);
+  return e > 16 && e < 255 ? __uint_as_float(static_cast<uint32_t>(127 + sign * (e - 127 - 8)) << 23) : 0.0f;
+}
+__device__ __forceinline__ uint32_t low_byte(float v, uint32_t r) {
+  const float left = (v - __uint_as_float(r << 16)) * half_place(r, -1) * 127.0f;
+  return static_cast<uint32_t>(static_cast<int>(rintf(half_place(r, -1) == 0.0f ? 0.0f : left))) & 0xFFu;
+}
+__device__ __forceinline__ float low_value(uint32_t byte, uint32_t r) {
+  return static_cast<float>(static_cast<int8_t>(byte)) * half_place(r, 1) * (1.0f / 127.0f);
+}
+__device__ __forceinline__ uint32_t low_bytes(const float (&v)[4], const u32x2& w) {
+  uint32_t out = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) out |= low_byte(v[e], (w[e / 2] >> (16 * (e & 1))) & 0xFFFFu) << (8 * e);
+  return out;
+}
+
 // Columns of a transposed result (lane mod 32: the row of the output) as rows of bf16.
 template <int HD>
-__device__ __forceinline__ void store_rows(const f32x16 (&acc)[HD / 32], float f, uint16_t* row, int hd, int lane) {
+__device__ __forceinline__ void store_rows(const f32x16 (&acc)[HD / 32], float f, uint16_t* row, int hd, int lane,
+                                           int8_t* low = nullptr) {
 #pragma unroll
   for (int d = 0; d < HD / 32; ++d)
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       const int c = 32 * d + 8 * g + 4 * (lane >> 5);
       if (c < hd) {
-        u32x2 w = {pack_bf16x2(acc[d][4 * g] * f, acc[d][4 * g + 1] * f),
-                   pack_bf16x2(acc[d][4 * g + 2] * f, acc[d][4 * g + 3] * f)};
+        const float v[4] = {acc[d][4 * g] * f, acc[d][4 * g + 1] * f, acc[d][4 * g + 2] * f, acc[d][4 * g + 3] * f};
+        const u32x2 w = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
         *reinterpret_cast<u32x2*>(row + c) = w;
+        if (low != nullptr) *reinterpret_cast<uint32_t*>(low + c) = low_bytes(v, w);
       }
     }
 }
@@ -460,7 +498,7 @@ __device__ __forceinline__ bool attn_fwd(const AttnArgs& a, TilePair<HD>& even, 
       mark_rows<HD>(sm[n].o, mode, out, a.hd, lane);
       continue;
     }
-    store_rows<HD>(sm[n].o, f, out, a.hd, lane);
+    store_rows<HD>(sm[n].o, f, out, a.hd, lane, a.o_low == nullptr ? nullptr : a.o_low + (int64_t(bh) * a.lq + row) * a.hd);
     if (lane < 32) a.lse[int64_t(bh) * a.lq + row] = empty ? __builtin_inff() : sm[n].m + log2f(l);
   }
   return true;
@@ -640,17 +678,19 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
   const float f = empty ? 0.0f : 1.0f / l;
   const int bh = static_cast<int>(row / a.lq), i = static_cast<int>(row % a.lq);
   if (c < a.hd) {
-    const u32x2 w = {pack_bf16x2(o[0] * f, o[1] * f), pack_bf16x2(o[2] * f, o[3] * f)};
+    const float v[4] = {o[0] * f, o[1] * f, o[2] * f, o[3] * f};
+    const u32x2 w = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
     *reinterpret_cast<u32x2*>(a.o + (bh / a.heads) * a.os[0] + (bh % a.heads) * a.os[1] + i * a.os[2] + c) = w;
+    if (a.o_low != nullptr) *reinterpret_cast<uint32_t*>(a.o_low + row * a.hd + c) = low_bytes(v, w);
   }
   if (lane == 0) a.lse[row] = empty ? __builtin_inff() : m + log2f(l);
 }
 
 // ------------------------------ gradient of q --------------------------------
-// As the forward, with S^T and dP^T = V dO^T; D = sum(dO o) on the way (o as it was rounded),
+// As the forward, with S^T and dP^T = V dO^T; D = sum(dO o) on the way,
 // for the other kernel too.  Where the sums are not finite the work is done again with clean
 // values, and NaN in the rows that see a key that had others.
-template <int HD, int NQ>
+template <int HD, int NQ, bool FINE>
 __device__ __forceinline__ bool attn_dq(const AttnGradArgs& ga, TilePair<HD>& even, TilePair<HD>& odd, int* bad_key, int bh,
                                         int q0, int mode) {
   constexpr int KS = HD / 16;
@@ -681,14 +721,21 @@ __device__ __forceinline__ bool attn_dq(const AttnGradArgs& ga, TilePair<HD>& ev
     const int row = w0 + 32 * n + (lane & 31);
     load_frags<HD>(qf[n], a.o + b * a.os[0] + h * a.os[1], a.os[2], row, a.lq, a.hd, lane);
     load_frags<HD>(gf[n], ga.go + b * ga.gs[0] + h * ga.gs[1], ga.gs[2], row, a.lq, a.hd, lane);
+    // sum(do o), o with what its rounding took off: where a row sees few keys dS is a difference
+    // of near numbers, and a rounded o would cost it digits
     float s = 0.0f;
 #pragma unroll
-    for (int st = 0; st < KS; ++st)
+    for (int st = 0; st < KS; ++st) {
+      u32x2 low = {0u, 0u};
+      if (row < a.lq && 16 * st + 8 * (lane >> 5) < a.hd)
+        low = *reinterpret_cast<const u32x2*>(a.o_low + (int64_t(bh) * a.lq + row) * a.hd + 16 * st + 8 * (lane >> 5));
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        s = __builtin_fmaf(__uint_as_float(qf[n][st][w] << 16), __uint_as_float(gf[n][st][w] << 16), s);
-        s = __builtin_fmaf(__uint_as_float(qf[n][st][w] & 0xFFFF0000u), __uint_as_float(gf[n][st][w] & 0xFFFF0000u), s);
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t r = (qf[n][st][e / 2] >> (16 * (e & 1))) & 0xFFFFu, g = (gf[n][st][e / 2] >> (16 * (e & 1))) & 0xFFFFu;
+        const float o = __uint_as_float(r << 16) + low_value((low[e / 4] >> (8 * (e & 3))) & 0xFFu, r);
+        s = __builtin_fmaf(o, __uint_as_float(g << 16), s);
       }
+    }
     delta[n] = halves_sum(s);
     lse[n] = row < a.lq ? a.lse[int64_t(bh) * a.lq + row] : __builtin_inff();
     if (row < a.lq && lane < 32) ga.delta[int64_t(bh) * a.lq + row] = delta[n];
@@ -724,7 +771,7 @@ __device__ __forceinline__ bool attn_dq(const AttnGradArgs& ga, TilePair<HD>& ev
           dp[n] = mfma32x32x16(vf, gf[n][st], dp[n]);
         }
       }
-      u32x4 ds[NQ][2];
+      u32x4 ds[NQ][2], dr[NQ][2];
 #pragma unroll
       for (int n = 0; n < NQ; ++n) {
 #pragma unroll
@@ -739,6 +786,7 @@ __device__ __forceinline__ bool attn_dq(const AttnGradArgs& ga, TilePair<HD>& ev
           }
         }
         pack_steps(s[n], ds[n]);
+        if constexpr (FINE) pack_rest(s[n], ds[n], dr[n]);
       }
 #pragma unroll
       for (int st = 0; st < 2; ++st)
@@ -746,7 +794,10 @@ __device__ __forceinline__ bool attn_dq(const AttnGradArgs& ga, TilePair<HD>& ev
         for (int d = 0; d < HD / 32; ++d) {
           const u32x4 kf = Tile<HD>::col_frag(now.k, 32 * kb + 16 * st, d, lane);
 #pragma unroll
-          for (int n = 0; n < NQ; ++n) dq[n][d] = mfma32x32x16(kf, ds[n][st], dq[n][d]);
+          for (int n = 0; n < NQ; ++n) {
+            dq[n][d] = mfma32x32x16(kf, ds[n][st], dq[n][d]);
+            if constexpr (FINE) dq[n][d] = mfma32x32x16(kf, dr[n][st], dq[n][d]);
+          }
         }
     }
   };
@@ -769,7 +820,7 @@ __device__ __forceinline__ bool attn_dq(const AttnGradArgs& ga, TilePair<HD>& ev
   return true;
 }
 
-template <int HD, int NQ, int WAVES>
+template <int HD, int NQ, int WAVES, bool FINE>
 __global__ __launch_bounds__(256, WAVES) void k_attn_dq(AttnGradArgs ga) {
   constexpr int BM = 128 * NQ;
   __shared__ __attribute__((aligned(16))) TilePair<HD> even, odd;
@@ -779,7 +830,7 @@ __global__ __launch_bounds__(256, WAVES) void k_attn_dq(AttnGradArgs ga) {
   const int bh = static_cast<int>(id / nqb), q0 = (nqb - 1 - static_cast<int>(id % nqb)) * BM;
 #pragma unroll 1
   for (int mode = kPlain; mode <= kClean; ++mode) {
-    if (attn_dq<HD, NQ>(ga, even, odd, bad_key, bh, q0, mode)) break;
+    if (attn_dq<HD, NQ, FINE>(ga, even, odd, bad_key, bh, q0, mode)) break;
     __syncthreads();
   }
 }
@@ -798,11 +849,18 @@ struct RowPair {
   float lse[kBN], delta[kBN];
 };
 
+// Blocks per run: 32 where each XCD gets two such runs, else few enough for eight or so.
+__host__ __device__ inline int run_of(int nkb, int bk) {
+  const int64_t blocks = int64_t(nkb) * bk;
+  const int run = blocks >= 512 ? 32 : blocks < 64 ? 1 : static_cast<int>(blocks / 64);
+  return run < nkb ? run : nkb;
+}
+
 struct DkvJob {
   int bk, k0, slot, far;
 };
 
-template <int HD>
+template <int HD, bool FINE>
 __device__ __forceinline__ bool attn_dkv(const AttnGradArgs& ga, RowPair<HD>& even, RowPair<HD>& odd, int* bad_row,
                                          const DkvJob& job, int mode) {
   constexpr int KS = HD / 16;
@@ -892,12 +950,16 @@ __device__ __forceinline__ bool attn_dkv(const AttnGradArgs& ga, RowPair<HD>& ev
       u32x4 pf[2], df[2];
       pack_steps(s, pf);
       pack_steps(dp, df);
+      u32x4 dr[2];
+      if constexpr (FINE) pack_rest(dp, df, dr);
 #pragma unroll
       for (int st = 0; st < 2; ++st)
 #pragma unroll
         for (int d = 0; d < HD / 32; ++d) {
           dv[d] = mfma32x32x16(Tile<HD>::col_frag(now.g, 32 * qb + 16 * st, d, lane), pf[st], dv[d]);
-          dk[d] = mfma32x32x16(Tile<HD>::col_frag(now.q, 32 * qb + 16 * st, d, lane), df[st], dk[d]);
+          const u32x4 qt = Tile<HD>::col_frag(now.q, 32 * qb + 16 * st, d, lane);
+          dk[d] = mfma32x32x16(qt, df[st], dk[d]);
+          if constexpr (FINE) dk[d] = mfma32x32x16(qt, dr[st], dk[d]);
         }
     }
   };
@@ -921,18 +983,30 @@ __device__ __forceinline__ bool attn_dkv(const AttnGradArgs& ga, RowPair<HD>& ev
   return true;
 }
 
-template <int HD, int WAVES>
+template <int HD, int WAVES, bool FINE>
 __global__ __launch_bounds__(256, WAVES) void k_attn_dkv(AttnGradArgs ga) {
   __shared__ __attribute__((aligned(16))) RowPair<HD> even, odd;
   __shared__ int bad_row[kBN];
+  // The blocks of keys in runs, each run on one XCD: its workgroups walk the same
+  // rows within what an L2 holds.  Runs of the first keys, whose windows are whole, go first,
+  // and the far work, in shorter pieces, last: with a workgroup or two to a CU a long one that
+  // starts late is all that runs at the end.
   const int nkb = (ga.f.lk + 127) / 128, nfb = (ga.far_keys + 63) / 64, bk_all = ga.f.b * ga.f.kv;
-  const int far = bk_all * nfb * ga.chunks;
-  const int near_id = static_cast<int>(xcd_remap(blockIdx.x, gridDim.x)) - far, id = near_id < 0 ? near_id + far : near_id;
-  const int slots = near_id < 0 ? ga.chunks : ga.parts, blocks = near_id < 0 ? nfb : nkb;
-  const DkvJob job = {id / (slots * blocks), id / slots % blocks * (near_id < 0 ? 64 : 128), id % slots, near_id < 0};
+  const int run = run_of(nkb, bk_all), runs = (nkb + run - 1) / run * bk_all;
+  const int per_run = run * ga.parts, near = (runs + kNumXcd - 1) / kNumXcd * kNumXcd * per_run;
+  DkvJob job;
+  if (static_cast<int>(blockIdx.x) < near) {
+    const int xcd = blockIdx.x % kNumXcd, k = blockIdx.x / kNumXcd;
+    const int r = k / per_run * kNumXcd + xcd, in = k % per_run, kb = r / bk_all * run + in / ga.parts;
+    if (r >= runs || kb >= nkb) return;
+    job = {r % bk_all, kb * 128, in % ga.parts, 0};
+  } else {
+    const int id = blockIdx.x - near;
+    job = {id / (ga.chunks * nfb), id / ga.chunks % nfb * 64, id % ga.chunks, 1};
+  }
 #pragma unroll 1
   for (int mode = kPlain; mode <= kClean; ++mode) {
-    if (attn_dkv<HD>(ga, even, odd, bad_row, job, mode)) break;
+    if (attn_dkv<HD, FINE>(ga, even, odd, bad_row, job, mode)) break;
     __syncthreads();
   }
 }
@@ -963,7 +1037,7 @@ __global__ __launch_bounds__(256) void k_attn_dkv_sum(AttnGradArgs ga) {
 
 // How the gradients of k and v are split (AttnGradArgs), and the floats of `part`.
 // parts: 512 workgroups (two per CU) of at least 4 tiles where the blocks of keys are fewer.
-// chunks: a far workgroup walks as many tiles as a near one, at least 16.
+// chunks: a far workgroup walks a quarter of a near one's tiles, at least 16.
 int64_t plan_dkv(AttnGradArgs* g) {
   const AttnArgs& a = g->f;
   const int64_t bk = int64_t(a.b) * a.kv, G = a.heads / a.kv;
@@ -977,10 +1051,11 @@ int64_t plan_dkv(AttnGradArgs* g) {
   const bool far = a.sinks > 0 && a.window < a.lk;
   g->far_keys = far ? (a.sinks < a.lk ? a.sinks : a.lk) : 0;
   g->near_keys = parts > 1 ? a.lk : g->far_keys;
+  g->fine = (a.window < a.lk ? a.window + a.sinks : a.lk) <= kFineKeys;
   g->chunks = 0;
   if (far) {
     const int64_t far_rows = a.lk - a.window < a.lq ? a.lk - a.window : a.lq, far_tiles = G * ceil_div(far_rows, kBN);
-    const int64_t own = ceil_div(tiles, parts);
+    const int64_t own = ceil_div(tiles, 4 * parts);
     int64_t chunks = ceil_div(far_tiles, own < 16 ? 16 : own);
     g->chunks = static_cast<int>(chunks > 64 ? 64 : chunks);
   }
@@ -1019,18 +1094,27 @@ void launch_waves(const AttnArgs& a, hipStream_t s) {
   launch_join(a, s);
 }
 
-template <int HD, int NQ, int WQ, int WK>
-void launch_bwd(const AttnGradArgs& a, bool kv, hipStream_t s) {
+template <int HD, int NQ, int WQ, int WK, bool FINE>
+void launch_grads(const AttnGradArgs& a, bool kv, hipStream_t s) {
   const int grid = a.f.b * a.f.heads * static_cast<int>(ceil_div(a.f.lq, 128 * NQ));
-  hipLaunchKernelGGL((k_attn_dq<HD, NQ, WQ>), dim3(grid), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((k_attn_dq<HD, NQ, WQ, FINE>), dim3(grid), dim3(256), 0, s, a);
   if (!kv) return;
   const int bk = a.f.b * a.f.kv;
-  const int grid_kv = bk * (static_cast<int>(ceil_div(a.f.lk, 128)) * a.parts + static_cast<int>(ceil_div(a.far_keys, 64)) * a.chunks);
-  hipLaunchKernelGGL((k_attn_dkv<HD, WK>), dim3(grid_kv), dim3(256), 0, s, a);
+  const int nkb = static_cast<int>(ceil_div(a.f.lk, 128)), run = run_of(nkb, bk);
+  const int runs = static_cast<int>(ceil_div(nkb, run)) * bk;
+  const int grid_kv = static_cast<int>(ceil_div(runs, kNumXcd)) * kNumXcd * run * a.parts +
+                      bk * static_cast<int>(ceil_div(a.far_keys, 64)) * a.chunks;
+  hipLaunchKernelGGL((k_attn_dkv<HD, WK, FINE>), dim3(grid_kv), dim3(256), 0, s, a);
   if (a.near_keys > 0) {
     const int64_t threads = int64_t(bk) * a.near_keys * (a.f.hd / 2);
     hipLaunchKernelGGL(k_attn_dkv_sum, dim3(static_cast<uint32_t>(ceil_div(threads, 256))), dim3(256), 0, s, a);
   }
+}
+
+template <int HD, int NQ, int WQ, int WK>
+void launch_bwd(const AttnGradArgs& a, bool kv, hipStream_t s) {
+  if (a.fine) launch_grads<HD, NQ, WQ, WK, true>(a, kv, s);
+  else launch_grads<HD, NQ, WQ, WK, false>(a, kv, s);
 }
 
 int status() { return hipGetLastError() == hipSuccess ? 0 : -5; }
@@ -1069,12 +1153,12 @@ int64_t compact_attention_bwd_scratch(const AttnArgs* a) {
 int compact_attention_bwd(const AttnGradArgs* args, void* stream) {
   AttnGradArgs plan = *args;
   const AttnGradArgs* a = &plan;
-  if (!args_ok(a->f) || a->gs[2] < 0 || a->gs[2] > kMaxStride || (a->f.lq > 1 && a->gs[2] < a->f.hd)) return -1;
+  if (!args_ok(a->f) || a->f.o_low == nullptr || a->gs[2] < 0 || a->gs[2] > kMaxStride || (a->f.lq > 1 && a->gs[2] < a->f.hd)) return -1;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const bool kv = a->dk != nullptr;
   if (plan_dkv(&plan) > 0 && kv && a->part == nullptr) return -1;
   if (a->f.hd <= 64) launch_bwd<64, 1, 2, 2>(*a, kv, s);
-  else if (a->f.hd <= 96) launch_bwd<96, 1, 2, 1>(*a, kv, s);
+  else if (a->f.hd <= 96) launch_bwd<96, 1, 2, 2>(*a, kv, s);
   else launch_bwd<128, 1, 2, 1>(*a, kv, s);
   return status();
 }

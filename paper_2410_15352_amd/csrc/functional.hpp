@@ -33,6 +33,7 @@ struct AttnArgs {
   const uint16_t *q, *k, *v;     // (b, heads, lq, hd), (b, kv, lk, hd) twice
   uint16_t* o;
   float* lse;                    // [b heads][lq]: log2 of the sum of 2^(scale log2(e) q.k); +inf: no key
+  int8_t* o_low;                 // [b heads][lq][hd]: what o's rounding took off, in 127ths of half its last place; or NULL
   const int32_t* lengths;        // [b] keys of each sequence, or NULL: lk
   int64_t qs[3], ks[3], vs[3], os[3];  // strides: sequence, head, row
   int32_t b, heads, kv, lq, lk, hd;
@@ -51,7 +52,7 @@ struct AttnGradArgs {
   float* delta;                  // [b heads][lq] scratch
   int64_t gs[3], dqs[3], dks[3], dvs[3];
   float* part;                   // [compact_attention_bwd_scratch()]
-  int32_t parts, near_keys, chunks, far_keys;  // set by the entry point
+  int32_t parts, near_keys, chunks, far_keys, fine;  // set by the entry point
 };
 
 struct DistillArgs {

@@ -31,9 +31,9 @@ _bf16 = torch.bfloat16
 # The argument blocks of csrc/functional.hpp as native struct layouts (a ctypes.Structure
 # costs ten times as much to fill), passed by address.
 _ROTARY = struct.Struct("@" + 3 * "2Q6q2i" + "2Q4q8if").pack
-_ATTN = "6Q12q8if2i2Q"
+_ATTN = "7Q12q8if2i2Q"
 _attn_pack = struct.Struct("@" + _ATTN).pack
-_attn_grad_pack = struct.Struct("@" + _ATTN + "5Q12qQ4i").pack
+_attn_grad_pack = struct.Struct("@" + _ATTN + "5Q12qQ5i").pack
 _distill_pack = struct.Struct("@11Q5q6i2f").pack
 _block = ctypes.c_char_p
 
@@ -355,11 +355,11 @@ def attention_splits(b, heads, kv, lq, lk, window, sinks):
     return splits if splits > 1 else 0
 
 
-def _attn_fields(q, k, v, o, lse, lengths, window, sinks, scale, splits=0, waves=0, part=0, part_lse=0):
+def _attn_fields(q, k, v, o, lse, low, lengths, window, sinks, scale, splits=0, waves=0, part=0, part_lse=0):
     b, heads, lq, hd = q.shape
     _, kv, lk, _ = k.shape
     return (q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
-            0 if lengths is None else lengths.data_ptr(), *_strides(q), *_strides(k), *_strides(v), *_strides(o), b, heads,
+            0 if low is None else low.data_ptr(), 0 if lengths is None else lengths.data_ptr(), *_strides(q), *_strides(k), *_strides(v), *_strides(o), b, heads,
             kv, lq, lk, hd, NO_WINDOW if window is None or window > NO_WINDOW else window, min(sinks, NO_WINDOW), scale,
             splits, waves, part, part_lse)
 
@@ -390,40 +390,42 @@ def _attn_scratch(block):
 _fns = {}
 
 
-def _attention_apply(q, k, v, window, sinks, lengths, scale):
-    """(q, k, v as the kernels take them, o, lse)"""
+def _attention_apply(q, k, v, window, sinks, lengths, scale, tracked=False):
+    """(q, k, v as the kernels take them, o, lse, and for a backward what o's rounding took off)"""
     q, k, v = _attn_tensor(q), _attn_tensor(k), _attn_tensor(v)
     b, heads, lq, hd = q.shape
     _, kv, lk, _ = k.shape
     o = _empty_heads(q)
     lse = torch.empty(b, heads, lq, dtype=torch.float32, device=q.device)
+    low = torch.empty(b * heads * lq * hd, dtype=torch.int8, device=q.device) if tracked else None
     splits = attention_splits(b, heads, kv, lq, lk, NO_WINDOW if window is None else window, sinks)
     split = ()
     if splits > 0:
         rows = splits * b * heads * lq
         part = torch.empty(rows * (hd + 1), dtype=torch.float32, device=q.device)
         split = (splits, heads // kv * lq <= FEW_ROWS, part.data_ptr(), part.data_ptr() + 4 * rows * hd)
-    ops._call("compact_attention_fwd", _attn_pack(*_attn_fields(q, k, v, o, lse, lengths, window, sinks, scale, *split)),
+    ops._call("compact_attention_fwd", _attn_pack(*_attn_fields(q, k, v, o, lse, low, lengths, window, sinks, scale, *split)),
               _stream(q))
-    return q, k, v, o, lse
+    return q, k, v, o, lse, low
 
 
 class _AttentionFn(torch.autograd.Function):
-    """Keeps q, k, v, o and one fp32 number a row."""
+    """Keeps q, k, v, o, a byte beside each element of o and one fp32 number a row."""
 
     @staticmethod
     def forward(ctx, q, k, v, window, sinks, lengths, scale):
-        kept = _attention_apply(q, k, v, window, sinks, lengths, scale)
+        kept = _attention_apply(q, k, v, window, sinks, lengths, scale, tracked=True)
         ctx.rule = window, sinks, scale
         ctx.save_for_backward(*kept, lengths)
         return kept[3]
 
     @staticmethod
     def backward(ctx, do):
-        q, k, v, o, lse, lengths = ctx.saved_tensors
+        q, k, v, o, lse, low, lengths = ctx.saved_tensors
         window, sinks, scale = ctx.rule
         none = None, None, None, None
         if (torch.is_grad_enabled() or not _eager() or not _here(do) or not ops._companion(lse, torch.float32, q.shape[:3].numel())
+                or not ops._companion(low, torch.int8, q.numel())
                 or not all(_here(t) and t.dtype == _bf16 for t in (q, k, v, o))):
             recorded = torch.is_grad_enabled()
             with torch.enable_grad():
@@ -431,7 +433,7 @@ class _AttentionFn(torch.autograd.Function):
                 y = _attention_torch(*leaves, window, sinks, lengths, scale)
                 return (*torch.autograd.grad(y, leaves, do, create_graph=recorded), *none)
         q, k, v, o, do = (_attn_tensor(t) for t in (q, k, v, o, do.to(_bf16)))
-        fields = _attn_fields(q, k, v, o, lse, lengths, window, sinks, scale)
+        fields = _attn_fields(q, k, v, o, lse, low, lengths, window, sinks, scale)
         dq, delta = _empty_heads(q), torch.empty_like(lse)
         dk = dv = None
         outs, strides, part = (0, 0), (0,) * 6, None
@@ -443,7 +445,7 @@ class _AttentionFn(torch.autograd.Function):
                 part = torch.empty(floats, dtype=torch.float32, device=q.device)
         ops._call("compact_attention_bwd",
                   _attn_grad_pack(*fields, do.data_ptr(), dq.data_ptr(), *outs, delta.data_ptr(), *_strides(do), *_strides(dq),
-                                  *strides, 0 if part is None else part.data_ptr(), 0, 0, 0, 0), _stream(q))
+                                  *strides, 0 if part is None else part.data_ptr(), 0, 0, 0, 0, 0), _stream(q))
         return dq, dk, dv, *none
 
 
