@@ -45,9 +45,13 @@ ops._SIGNATURES.update({
 })
 
 
+_TYPES = ops._TYPES
+_device_now = torch._C._cuda_getDevice
+
+
 def _here(t):
     """A tensor of its own storage on the current GPU."""
-    return _plain(t) and t.get_device() >= 0 and t.get_device() == torch._C._cuda_getDevice()
+    return _plain(t) and t.is_cuda and t.get_device() == _device_now()
 
 
 def _strides(t):
@@ -59,12 +63,15 @@ def _strides(t):
 
 def _rows(t):
     """t (4-D), or a copy of it, whose last dimension is dense and whose every row is on a
-    16-byte boundary."""
-    x, y, z = _strides(t)
-    if t.stride(3) != 1 or (t.data_ptr() | (x | y | z) * t.element_size()) % 16 != 0:
+    16-byte boundary, and its strides."""
+    x, y, z, w = t.stride()
+    b, c, d, _ = t.shape
+    s = (x if b > 1 else 0, y if c > 1 else 0, z if d > 1 else 0)
+    if w != 1 or (t.data_ptr() | (s[0] | s[1] | s[2]) * t.element_size()) % 16 != 0:
         t = t.contiguous()
         t = t if t.data_ptr() % 16 == 0 else t.clone()
-    return t
+        s = _strides(t)
+    return t, s
 
 
 def _tracked(*tensors):
@@ -175,15 +182,10 @@ class Rotary(torch.nn.Module):
 _NO_TENSOR = (0,) * 10
 
 
-def _rotary_call(rope, positions, inverse, jobs):
-    """jobs: (source, destination, rotated) of (b, l, heads, hd) tensors whose rows are dense
-    and on 16-byte boundaries."""
-    x = jobs[0][0]
+def _rotary_call(rope, positions, inverse, x, fields, count):
+    """fields: of each of `count` tensors like x (b, l, heads, hd), its source and destination,
+    their strides, its heads and whether it is turned."""
     b, l, _, hd = x.shape
-    fields = []
-    for src, dst, rotate in jobs:
-        fields += (src.data_ptr(), dst.data_ptr(), *_strides(src), *_strides(dst), src.shape[2], rotate)
-    fields += _NO_TENSOR * (3 - len(jobs))
     at, pos_b, pos_l, offset, pos32 = 0, 0, 0, 0, 0
     if isinstance(positions, torch.Tensor):
         at, pos32 = positions.data_ptr(), positions.dtype == torch.int32
@@ -191,14 +193,24 @@ def _rotary_call(rope, positions, inverse, jobs):
     else:
         offset = positions or 0
     ops._call("compact_rotary",
-              _ROTARY(*fields, rope.turns(x.device).data_ptr(), at, pos_b, pos_l, offset, b * l, l, hd, rope.dims,
-                      len(jobs), rope.interleaved, inverse, pos32, x.dtype == torch.float32, rope.magnitude), _stream(x))
+              _ROTARY(*fields, *_NO_TENSOR * (3 - count), rope.turns(x.device).data_ptr(), at, pos_b, pos_l, offset, b * l, l,
+                      hd, rope.dims, count, rope.interleaved, inverse, pos32, x.dtype == torch.float32, rope.magnitude),
+              _stream(x))
 
 
 def _rotary_apply(rope, positions, inverse, *tensors):
-    jobs = [(_rows(t), torch.empty(t.shape, dtype=t.dtype, device=t.device), 1) for t in tensors if t is not None]
-    _rotary_call(rope, positions, inverse, jobs)
-    return [j[1] for j in jobs]
+    out, fields, kept = [], [], []
+    for t in tensors:
+        if t is None:
+            continue
+        src, strides = _rows(t)
+        _, l, heads, hd = src.shape
+        dst = torch.empty(src.shape, dtype=src.dtype, device=src.device)
+        fields += (src.data_ptr(), dst.data_ptr(), *strides, l * heads * hd, heads * hd, hd, heads, 1)
+        out.append(dst)
+        kept.append(src)
+    _rotary_call(rope, positions, inverse, kept[0], fields, len(out))
+    return out
 
 
 def _rotary_torch(rope, positions, inverse, *tensors):
@@ -259,7 +271,8 @@ class _RotaryQkvFn(torch.autograd.Function):
         ctx.rope, ctx.positions, ctx.shape = rope, positions, qkv.shape
         ctx.set_materialize_grads(False)
         q, k, v = qkv.unbind(2)
-        _rotary_call(rope, positions, 0, [(q, q, 1), (k, k, 1)])
+        _rotary_call(rope, positions, 0, q, [x for t in (q, k) for x in (t.data_ptr(), t.data_ptr(), *_strides(t), *_strides(t),
+                                                                        t.shape[2], 1)], 2)
         torch.autograd.graph.increment_version(qkv)  # whoever saved it is told
         return tuple(t.transpose(1, 2) for t in (q, k, v))
 
@@ -274,8 +287,10 @@ class _RotaryQkvFn(torch.autograd.Function):
             dq, dk = _rotary_torch(ctx.rope, ctx.positions, True, dq, dk)
             return None, None, torch.stack((dq, dk, dv), 2)
         out = torch.empty(ctx.shape, dtype=dq.dtype, device=dq.device)
-        _rotary_call(ctx.rope, ctx.positions, 1,
-                     [(_rows(g), to, rotate) for g, to, rotate in zip((dq, dk, dv), out.unbind(2), (1, 1, 0))])
+        rows = [_rows(g) for g in (dq, dk, dv)]
+        _rotary_call(ctx.rope, ctx.positions, 1, rows[0][0],
+                     [x for (g, s), to, rotate in zip(rows, out.unbind(2), (1, 1, 0))
+                      for x in (g.data_ptr(), to.data_ptr(), *s, *_strides(to), g.shape[2], rotate)], 3)
         return None, None, out
 
 
@@ -355,28 +370,40 @@ def attention_splits(b, heads, kv, lq, lk, window, sinks):
     return splits if splits > 1 else 0
 
 
-def _attn_fields(q, k, v, o, lse, low, lengths, window, sinks, scale, splits=0, waves=0, part=0, part_lse=0):
-    b, heads, lq, hd = q.shape
-    _, kv, lk, _ = k.shape
-    return (q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
-            0 if low is None else low.data_ptr(), 0 if lengths is None else lengths.data_ptr(), *_strides(q), *_strides(k), *_strides(v), *_strides(o), b, heads,
-            kv, lq, lk, hd, NO_WINDOW if window is None or window > NO_WINDOW else window, min(sinks, NO_WINDOW), scale,
-            splits, waves, part, part_lse)
-
-
 def _attn_tensor(t):
-    """A bf16 (b, heads, l, hd) tensor as the kernels take it: rows that lie on one another, or
-    so far apart that a tile of 64 passes 2^31 bytes, are copied too."""
-    _, _, l, hd = t.shape
+    """A bf16 (b, heads, l, hd) tensor as the kernels take it, and its strides: rows that lie on
+    one another, or so far apart that a tile of 64 passes 2^31 bytes, are copied too."""
+    l, hd = t.shape[2:]
     if l > 1 and not hd <= t.stride(2) <= MAX_ROW_STRIDE:
         t = t.contiguous()
     return _rows(t)
 
 
-def _empty_heads(like, l=None):
-    """(b, heads, l, hd) that lies as (b, l, heads, hd), the layout the projections take."""
-    b, heads, n, hd = like.shape
-    return torch.empty(b, n, heads, hd, dtype=_bf16, device=like.device).transpose(1, 2)
+def _attn_fields(q, k, v, o, stats, lengths, window, sinks, scale, splits=0, waves=0, part=0, part_lse=0):
+    """q, k, v, o: (tensor, strides); stats: the rows' log-sums, and with room for it what o's
+    rounding took off."""
+    b, heads, lq, hd = q[0].shape
+    _, kv, lk, _ = k[0].shape
+    rows, lse = b * heads * lq, stats.data_ptr()
+    return (q[0].data_ptr(), k[0].data_ptr(), v[0].data_ptr(), o[0].data_ptr(), lse,
+            lse + -(-rows // 4) * 16 if stats.numel() > rows else 0, 0 if lengths is None else lengths.data_ptr(), *q[1], *k[1], *v[1],
+            *o[1], b, heads, kv, lq, lk, hd, NO_WINDOW if window is None or window > NO_WINDOW else window,
+            min(sinks, NO_WINDOW), scale, splits, waves, part, part_lse)
+
+
+def _stats_count(shape, tracked):
+    """Floats of a call's statistics: one a row, and a byte for each element of o."""
+    b, heads, lq, hd = shape
+    rows = b * heads * lq
+    return -(-rows // 4) * 4 + rows * hd // 4 if tracked else rows
+
+
+def _empty_heads(shape, device):
+    """(b, heads, l, hd) that lies as (b, l, heads, hd), the layout the projections take, and
+    its strides."""
+    b, heads, l, hd = shape
+    strides = (l * heads * hd, hd, heads * hd)
+    return torch.empty_strided(shape, (*strides, 1), dtype=_bf16, device=device), strides
 
 
 def _attn_scratch(block):
@@ -391,26 +418,27 @@ _fns = {}
 
 
 def _attention_apply(q, k, v, window, sinks, lengths, scale, tracked=False):
-    """(q, k, v as the kernels take them, o, lse, and for a backward what o's rounding took off)"""
+    """(q, k, v as the kernels take them, o, the statistics that a backward wants)"""
     q, k, v = _attn_tensor(q), _attn_tensor(k), _attn_tensor(v)
-    b, heads, lq, hd = q.shape
-    _, kv, lk, _ = k.shape
-    o = _empty_heads(q)
-    lse = torch.empty(b, heads, lq, dtype=torch.float32, device=q.device)
-    low = torch.empty(b * heads * lq * hd, dtype=torch.int8, device=q.device) if tracked else None
+    shape, device = q[0].shape, q[0].device
+    b, heads, lq, hd = shape
+    _, kv, lk, _ = k[0].shape
+    o = _empty_heads(shape, device)
+    stats = torch.empty(_stats_count(shape, tracked), dtype=torch.float32, device=device)
     splits = attention_splits(b, heads, kv, lq, lk, NO_WINDOW if window is None else window, sinks)
     split = ()
     if splits > 0:
         rows = splits * b * heads * lq
-        part = torch.empty(rows * (hd + 1), dtype=torch.float32, device=q.device)
-        split = (splits, heads // kv * lq <= FEW_ROWS, part.data_ptr(), part.data_ptr() + 4 * rows * hd)
-    ops._call("compact_attention_fwd", _attn_pack(*_attn_fields(q, k, v, o, lse, low, lengths, window, sinks, scale, *split)),
-              _stream(q))
-    return q, k, v, o, lse, low
+        part = torch.empty(rows * (hd + 1), dtype=torch.float32, device=device)
+        at = part.data_ptr()
+        split = (splits, heads // kv * lq <= FEW_ROWS, at, at + 4 * rows * hd)
+    ops._call("compact_attention_fwd", _attn_pack(*_attn_fields(q, k, v, o, stats, lengths, window, sinks, scale, *split)),
+              _stream(stats))
+    return q[0], k[0], v[0], o[0], stats
 
 
 class _AttentionFn(torch.autograd.Function):
-    """Keeps q, k, v, o, a byte beside each element of o and one fp32 number a row."""
+    """Keeps q, k, v, o, and beside o one fp32 number a row and a byte an element."""
 
     @staticmethod
     def forward(ctx, q, k, v, window, sinks, lengths, scale):
@@ -421,31 +449,34 @@ class _AttentionFn(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, do):
-        q, k, v, o, lse, low, lengths = ctx.saved_tensors
+        q, k, v, o, stats, lengths = ctx.saved_tensors
         window, sinks, scale = ctx.rule
         none = None, None, None, None
-        if (torch.is_grad_enabled() or not _eager() or not _here(do) or not ops._companion(lse, torch.float32, q.shape[:3].numel())
-                or not ops._companion(low, torch.int8, q.numel())
-                or not all(_here(t) and t.dtype == _bf16 for t in (q, k, v, o))):
+        shape = q.shape
+        if (torch.is_grad_enabled() or not _eager() or not _here(do)
+                or not ops._companion(stats, torch.float32, _stats_count(shape, True))
+                or not all(t.dtype is _bf16 and _here(t) for t in (q, k, v, o))):
             recorded = torch.is_grad_enabled()
             with torch.enable_grad():
                 leaves = [x if recorded and x.requires_grad else x.detach().requires_grad_(True) for x in (q, k, v)]
                 y = _attention_torch(*leaves, window, sinks, lengths, scale)
                 return (*torch.autograd.grad(y, leaves, do, create_graph=recorded), *none)
-        q, k, v, o, do = (_attn_tensor(t) for t in (q, k, v, o, do.to(_bf16)))
-        fields = _attn_fields(q, k, v, o, lse, low, lengths, window, sinks, scale)
-        dq, delta = _empty_heads(q), torch.empty_like(lse)
+        do = _attn_tensor(do if do.dtype is _bf16 else do.to(_bf16))
+        fields = _attn_fields(_attn_tensor(q), _attn_tensor(k), _attn_tensor(v), _attn_tensor(o), stats, lengths, window, sinks,
+                              scale)
+        rows, device = shape[:3].numel(), q.device
+        dq, dq_strides = _empty_heads(shape, device)
         dk = dv = None
-        outs, strides, part = (0, 0), (0,) * 6, None
+        outs, strides, floats = (0, 0), (0,) * 6, 0
         if ctx.needs_input_grad[1] or ctx.needs_input_grad[2]:
-            dk, dv = _empty_heads(k), _empty_heads(v)
-            outs, strides = (dk.data_ptr(), dv.data_ptr()), _strides(dk) + _strides(dv)
+            (dk, dk_strides), (dv, _) = _empty_heads(k.shape, device), _empty_heads(k.shape, device)
+            outs, strides = (dk.data_ptr(), dv.data_ptr()), dk_strides * 2
             floats = _attn_scratch(_attn_pack(*fields))
-            if floats > 0:
-                part = torch.empty(floats, dtype=torch.float32, device=q.device)
+        scratch = torch.empty(-(-rows // 4) * 4 + floats, dtype=torch.float32, device=device)  # D, and sums in parts
+        delta = scratch.data_ptr()
         ops._call("compact_attention_bwd",
-                  _attn_grad_pack(*fields, do.data_ptr(), dq.data_ptr(), *outs, delta.data_ptr(), *_strides(do), *_strides(dq),
-                                  *strides, 0 if part is None else part.data_ptr(), 0, 0, 0, 0, 0), _stream(q))
+                  _attn_grad_pack(*fields, do[0].data_ptr(), dq.data_ptr(), *outs, delta, *do[1], *dq_strides, *strides,
+                                  delta + -(-rows // 4) * 16 if floats > 0 else 0, 0, 0, 0, 0, 0), _stream(q))
         return dq, dk, dv, *none
 
 
