@@ -170,10 +170,12 @@ __device__ __forceinline__ void both_halves(float v, float& lo, float& hi) {
   lo = __uint_as_float(r[0]);
   hi = __uint_as_float(r[1]);
 }
+// The maximum that keeps a NaN: one instruction for three values, where fmaxf has each quieted first.
+__device__ __forceinline__ float max_of(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 __device__ __forceinline__ float halves_max(float v) {
   float lo, hi;
   both_halves(v, lo, hi);
-  return fmaxf(lo, hi);
+  return max_of(lo, hi);
 }
 __device__ __forceinline__ float halves_sum(float v) {
   float lo, hi;
@@ -244,6 +246,19 @@ struct Walk {
 __device__ __forceinline__ bool seen(int j, int p, int window, int sinks) {
   // (no short cuts: element by element they would become branches)
   return (j <= p) & ((p - j < window) | (j < sinks));
+}
+
+// The elements of a result whose key (`first` the lane's first) is not seen; past the sinks one
+// difference decides.
+__device__ __forceinline__ void hide_unseen(f32x16& s, float hidden, int first, int p, bool sinks_here, int window, int sinks) {
+  if (!sinks_here) {
+    const int d = p - first;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[e] = static_cast<uint32_t>(d - (8 * (e >> 2) + (e & 3))) < static_cast<uint32_t>(window) ? s[e] : hidden;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[e] = seen(first + 8 * (e >> 2) + (e & 3), p, window, sinks) ? s[e] : hidden;
+  }
 }
 
 // No key of j0 .. j0 + n - 1 is seen from a position in pmin .. pmax / all are from all of them.
@@ -340,6 +355,7 @@ struct Softmax {
     l = 0.0f;
   }
   // A new maximum of scaled scores `top` (both halves' own): what was summed so far is scaled.
+  // (A NaN moves nothing: its row is NaN whatever the reference.)
   // The reference of a row moves only when a score lies more than 2^8 above it: P <= 256 costs
   // no accuracy in fp32 sums and bf16 factors, and most tiles leave O alone.
   __device__ __forceinline__ void raise(float top) {
@@ -359,21 +375,28 @@ struct Softmax {
 };
 
 // ------------------------------- forward ------------------------------------
-// A workgroup of four waves takes 128 NQ queries of one head, NQ columns of 32 per wave, and
-// walks the keys they see in tiles of 64, the next tile's copies in flight under the work on
-// one.  (Each of the two buffers is a variable of its own: so the compiler knows which reads
-// a copy in flight has nothing to do with.)  The work with V's values of `mode`; false: not
-// finite, to be done by modes.
+// A workgroup of four waves takes 128 queries of one head, 32 columns per wave, and walks the
+// keys they see in tiles of 64, the next tile's copies in flight under the work on one.  (Each
+// of the two buffers is a variable of its own: so the compiler knows which reads a copy in
+// flight has nothing to do with.)  The work with V's values of `mode`; false: not finite, to be
+// done by modes.
+//
+// Bound by the latency of a wave's own chain (scores, maximum, exponentials, P V) with two or
+// three waves on a SIMD: at heads of 64 the matrix units work 23 % of the time and the vector
+// units 65 %, at 128 the matrix units 40 %; LDS has no bank conflicts.  Tried and slower: the
+// next tile's scores among this one's exponentials (heads of 64: 125-145 us for 109 at
+// 4 x 4096, 16 heads, window 1024; heads of 128: 3-7 % faster, but its two tiles of scores do
+// not fit the registers), 64 columns per wave (no longer two workgroups per CU).
 template <int HD>
 struct TilePair {
   char k[Tile<HD>::kBytes], v[Tile<HD>::kBytes];
 };
 
-template <int HD, int NQ>
+template <int HD>
 __device__ __forceinline__ bool attn_fwd(const AttnArgs& a, TilePair<HD>& even, TilePair<HD>& odd, int bh, int q0, int split,
                                          int mode) {
   constexpr int KS = HD / 16;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), w0 = q0 + wave * 32 * NQ;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), w0 = q0 + wave * 32;
   const int b = bh / a.heads, h = bh % a.heads, hk = h / (a.heads / a.kv);
   const int L = length_of(a, b), off = L - a.lq;
   const uint16_t* q = a.q + b * a.qs[0] + h * a.qs[1];
@@ -381,9 +404,9 @@ __device__ __forceinline__ bool attn_fwd(const AttnArgs& a, TilePair<HD>& even, 
   const uint16_t* v = a.v + b * a.vs[0] + hk * a.vs[1];
   const float c = a.scale * kLog2e;
 
-  const int last = min(a.lq, q0 + 128 * NQ) - 1;
+  const int last = min(a.lq, q0 + 128) - 1;
   const Walk<kBN> walk(q0 + off, last + off, L, a.window, a.sinks);
-  const int pmin = w0 + off, pmax = min(w0 + 32 * NQ - 1, last) + off;
+  const int row = w0 + (lane & 31), p = row + off, pmin = w0 + off, pmax = min(w0 + 31, last) + off;
   Copy<HD> ck, cv;
   ck.init(a.ks[2], a.hd, tid);
   cv.init(a.vs[2], a.hd, tid);
@@ -395,13 +418,10 @@ __device__ __forceinline__ bool attn_fwd(const AttnArgs& a, TilePair<HD>& even, 
   const int per = a.splits > 0 ? (walk.count + a.splits - 1) / a.splits : walk.count;
   const int t0 = split * per, t1 = min(walk.count, t0 + per);
   if (t0 < t1) fetch(t0, even);
-  u32x4 qf[NQ][KS];
-  Softmax<HD> sm[NQ];
-#pragma unroll
-  for (int n = 0; n < NQ; ++n) {
-    load_frags<HD>(qf[n], q, a.qs[2], w0 + 32 * n + (lane & 31), a.lq, a.hd, lane);
-    sm[n].init();
-  }
+  u32x4 qf[KS];
+  Softmax<HD> sm;
+  load_frags<HD>(qf, q, a.qs[2], row, a.lq, a.hd, lane);
+  sm.init();
 
   auto step = [&](int t, TilePair<HD>& now, TilePair<HD>& next) {
     copies_done();
@@ -412,109 +432,83 @@ __device__ __forceinline__ bool attn_fwd(const AttnArgs& a, TilePair<HD>& even, 
     }
     const int j0 = walk.key(t);
     if (w0 > last || none_seen(j0, kBN, pmin, pmax, a.window, a.sinks)) return;
-    f32x16 s[NQ][2];
+    f32x16 s[2];
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
+      s[kb] = zero16();
 #pragma unroll
-      for (int n = 0; n < NQ; ++n) s[n][kb] = zero16();
-#pragma unroll
-      for (int st = 0; st < KS; ++st) {
-        const u32x4 kf = Tile<HD>::row_frag(now.k, 32 * kb, st, lane);
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) s[n][kb] = mfma32x32x16(kf, qf[n][st], s[n][kb]);
-      }
+      for (int st = 0; st < KS; ++st) s[kb] = mfma32x32x16(Tile<HD>::row_frag(now.k, 32 * kb, st, lane), qf[st], s[kb]);
     }
     if (!all_seen(j0, kBN, pmin, pmax, a.window, a.sinks)) {
 #pragma unroll
-      for (int n = 0; n < NQ; ++n)
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            s[n][kb][e] = seen(j0 + 32 * kb + acc_row(e, lane), w0 + 32 * n + (lane & 31) + off, a.window, a.sinks)
-                              ? s[n][kb][e] : -__builtin_inff();
-    }
-    u32x4 pf[NQ][4];
-#pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-      float top = s[n][0][0];
-#pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) top = fmaxf(top, s[n][kb][e]);
-      sm[n].raise(top * c);
-      const float sh = sm[n].shift();
+        for (int e = 0; e < 16; ++e)
+          s[kb][e] = seen(j0 + 32 * kb + acc_row(e, lane), p, a.window, a.sinks) ? s[kb][e] : -__builtin_inff();
+    }
+    float top = max_of(s[0][0], s[1][0]);
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
+    for (int e = 1; e < 16; ++e) top = max_of(max_of(top, s[0][e]), s[1][e]);
+    sm.raise(top * c);
+    const float sh = sm.shift();
+    u32x4 pf[4];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          s[n][kb][e] = exp2_fast(__builtin_fmaf(s[n][kb][e], c, -sh));
-          sm[n].l += s[n][kb][e];
-        }
-        u32x4 two[2];
-        pack_steps(s[n][kb], two);
-        pf[n][2 * kb] = two[0];
-        pf[n][2 * kb + 1] = two[1];
+    for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        s[kb][e] = exp2_fast(__builtin_fmaf(s[kb][e], c, -sh));
+        sm.l += s[kb][e];
       }
+      u32x4 two[2];
+      pack_steps(s[kb], two);
+      pf[2 * kb] = two[0];
+      pf[2 * kb + 1] = two[1];
     }
 #pragma unroll
     for (int st = 0; st < 4; ++st)
 #pragma unroll
-      for (int d = 0; d < HD / 32; ++d) {
-        const u32x4 vf = Tile<HD>::col_frag(now.v, 16 * st, d, lane);
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) sm[n].o[d] = mfma32x32x16(vf, pf[n][st], sm[n].o[d]);
-      }
+      for (int d = 0; d < HD / 32; ++d)
+        sm.o[d] = mfma32x32x16(Tile<HD>::col_frag(now.v, 16 * st, d, lane), pf[st], sm.o[d]);
   };
   for (int t = t0; t < t1; t += 2) {
     step(t, even, odd);
     if (t + 1 < t1) step(t + 1, odd, even);
   }
-  if (mode == kPlain) {
-    bool bad = false;
-#pragma unroll
-    for (int n = 0; n < NQ; ++n) bad |= not_finite(sm[n].o);
-    if (__syncthreads_or(bad)) return false;
-  }
-#pragma unroll
-  for (int n = 0; n < NQ; ++n) {
-    const int row = w0 + 32 * n + (lane & 31);
-    const float l = halves_sum(sm[n].l);
-    if (row >= a.lq) continue;
-    const bool empty = sm[n].m == -__builtin_inff() && l == 0.0f;
-    const float f = empty ? 0.0f : 1.0f / l;
-    if (a.splits > 0) {
-      const int64_t rows = int64_t(a.b) * a.heads * a.lq, at = split * rows + int64_t(bh) * a.lq + row;
-      if (mode >= kPos) {
-        mark_rows<HD>(sm[n].o, mode, a.part_o + at * a.hd, a.hd, lane);
-        continue;
-      }
-      store_row_values<HD>(sm[n].o, f, a.part_o + at * a.hd, a.hd, lane);
-      if (lane < 32) a.part_lse[at] = empty ? -__builtin_inff() : sm[n].m + log2f(l);
-      continue;
-    }
-    uint16_t* out = a.o + b * a.os[0] + h * a.os[1] + row * a.os[2];
+  if (mode == kPlain && __syncthreads_or(not_finite(sm.o))) return false;
+  const float l = halves_sum(sm.l);
+  if (row >= a.lq) return true;
+  const bool empty = sm.m == -__builtin_inff() && l == 0.0f;
+  const float f = empty ? 0.0f : 1.0f / l;
+  if (a.splits > 0) {
+    const int64_t rows = int64_t(a.b) * a.heads * a.lq, at = split * rows + int64_t(bh) * a.lq + row;
     if (mode >= kPos) {
-      mark_rows<HD>(sm[n].o, mode, out, a.hd, lane);
-      continue;
+      mark_rows<HD>(sm.o, mode, a.part_o + at * a.hd, a.hd, lane);
+      return true;
     }
-    store_rows<HD>(sm[n].o, f, out, a.hd, lane, a.o_low == nullptr ? nullptr : a.o_low + (int64_t(bh) * a.lq + row) * a.hd);
-    if (lane < 32) a.lse[int64_t(bh) * a.lq + row] = empty ? __builtin_inff() : sm[n].m + log2f(l);
+    store_row_values<HD>(sm.o, f, a.part_o + at * a.hd, a.hd, lane);
+    if (lane < 32) a.part_lse[at] = empty ? -__builtin_inff() : sm.m + log2f(l);
+    return true;
   }
+  uint16_t* out = a.o + b * a.os[0] + h * a.os[1] + row * a.os[2];
+  if (mode >= kPos) {
+    mark_rows<HD>(sm.o, mode, out, a.hd, lane);
+    return true;
+  }
+  store_rows<HD>(sm.o, f, out, a.hd, lane, a.o_low == nullptr ? nullptr : a.o_low + (int64_t(bh) * a.lq + row) * a.hd);
+  if (lane < 32) a.lse[int64_t(bh) * a.lq + row] = empty ? __builtin_inff() : sm.m + log2f(l);
   return true;
 }
 
-template <int HD, int NQ, int WAVES>
-__global__ __launch_bounds__(256, WAVES) void k_attn_fwd(AttnArgs a) {
-  constexpr int BM = 128 * NQ;
+template <int HD>
+__global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnArgs a) {
   __shared__ __attribute__((aligned(16))) TilePair<HD> even, odd;
-  const int nqb = (a.lq + BM - 1) / BM, splits = a.splits > 0 ? a.splits : 1;
+  const int nqb = (a.lq + 127) / 128, splits = a.splits > 0 ? a.splits : 1;
   const uint32_t id0 = xcd_remap(blockIdx.x, gridDim.x), id = id0 / splits;
   const int split = static_cast<int>(id0 % splits);
-  const int bh = static_cast<int>(id / nqb), q0 = (nqb - 1 - static_cast<int>(id % nqb)) * BM;
+  const int bh = static_cast<int>(id / nqb), q0 = (nqb - 1 - static_cast<int>(id % nqb)) * 128;
 #pragma unroll 1
   for (int mode = kPlain; mode <= kNeg; ++mode) {
-    if (attn_fwd<HD, NQ>(a, even, odd, bh, q0, split, mode) && mode == kPlain) break;
+    if (attn_fwd<HD>(a, even, odd, bh, q0, split, mode) && mode == kPlain) break;
     __syncthreads();
   }
 }
@@ -578,13 +572,11 @@ __device__ __forceinline__ bool attn_split(const AttnArgs& a, WaveTiles<HD>& eve
     for (int st = 0; st < KS; ++st) s = mfma32x32x16(kf[st], qf[st], s);
     fetch_k(t + 1);
     if (!all_seen(j0, TN, pmin, pmax, a.window, a.sinks)) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e)
-        s[e] = seen(j0 + acc_row(e, lane), p, a.window, a.sinks) ? s[e] : -__builtin_inff();
+      hide_unseen(s, -__builtin_inff(), j0 + 4 * (lane >> 5), p, j0 < a.sinks, a.window, a.sinks);
     }
     float top = s[0];
 #pragma unroll
-    for (int e = 1; e < 16; ++e) top = fmaxf(top, s[e]);
+    for (int e = 1; e < 16; ++e) top = max_of(top, s[e]);
     sm.raise(top * c);
     const float sh = sm.shift();
 #pragma unroll
@@ -690,21 +682,21 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
 // As the forward, with S^T and dP^T = V dO^T; D = sum(dO o) on the way,
 // for the other kernel too.  Where the sums are not finite the work is done again with clean
 // values, and NaN in the rows that see a key that had others.
-template <int HD, int NQ, bool FINE>
+template <int HD, bool FINE>
 __device__ __forceinline__ bool attn_dq(const AttnGradArgs& ga, TilePair<HD>& even, TilePair<HD>& odd, int* bad_key, int bh,
                                         int q0, int mode) {
   constexpr int KS = HD / 16;
   const AttnArgs& a = ga.f;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), w0 = q0 + wave * 32 * NQ;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), w0 = q0 + wave * 32;
   const int b = bh / a.heads, h = bh % a.heads, hk = h / (a.heads / a.kv);
   const int L = length_of(a, b), off = L - a.lq;
   const uint16_t* k = a.k + b * a.ks[0] + hk * a.ks[1];
   const uint16_t* v = a.v + b * a.vs[0] + hk * a.vs[1];
   const float c = a.scale * kLog2e;
 
-  const int last = min(a.lq, q0 + 128 * NQ) - 1;
+  const int last = min(a.lq, q0 + 128) - 1;
   const Walk<kBN> walk(q0 + off, last + off, L, a.window, a.sinks);
-  const int pmin = w0 + off, pmax = min(w0 + 32 * NQ - 1, last) + off;
+  const int row = w0 + (lane & 31), p = row + off, pmin = w0 + off, pmax = min(w0 + 31, last) + off;
   Copy<HD> ck, cv;
   ck.init(a.ks[2], a.hd, tid);
   cv.init(a.vs[2], a.hd, tid);
@@ -713,36 +705,31 @@ __device__ __forceinline__ bool attn_dq(const AttnGradArgs& ga, TilePair<HD>& ev
     cv.issue(v, a.vs[2], walk.key(t), L, a.hd, to.v, wave);
   };
   if (walk.count > 0) fetch(0, even);
-  u32x4 qf[NQ][KS], gf[NQ][KS];
-  f32x16 dq[NQ][HD / 32];
-  float lse[NQ], delta[NQ];
+  u32x4 qf[KS], gf[KS];
+  load_frags<HD>(qf, a.o + b * a.os[0] + h * a.os[1], a.os[2], row, a.lq, a.hd, lane);
+  load_frags<HD>(gf, ga.go + b * ga.gs[0] + h * ga.gs[1], ga.gs[2], row, a.lq, a.hd, lane);
+  // sum(do o), o with what its rounding took off: where a row sees few keys dS is a difference
+  // of near numbers, and a rounded o would cost it digits
+  float sum = 0.0f;
 #pragma unroll
-  for (int n = 0; n < NQ; ++n) {
-    const int row = w0 + 32 * n + (lane & 31);
-    load_frags<HD>(qf[n], a.o + b * a.os[0] + h * a.os[1], a.os[2], row, a.lq, a.hd, lane);
-    load_frags<HD>(gf[n], ga.go + b * ga.gs[0] + h * ga.gs[1], ga.gs[2], row, a.lq, a.hd, lane);
-    // sum(do o), o with what its rounding took off: where a row sees few keys dS is a difference
-    // of near numbers, and a rounded o would cost it digits
-    float s = 0.0f;
+  for (int st = 0; st < KS; ++st) {
+    u32x2 low = {0u, 0u};
+    if (row < a.lq && 16 * st + 8 * (lane >> 5) < a.hd)
+      low = *reinterpret_cast<const u32x2*>(a.o_low + (int64_t(bh) * a.lq + row) * a.hd + 16 * st + 8 * (lane >> 5));
 #pragma unroll
-    for (int st = 0; st < KS; ++st) {
-      u32x2 low = {0u, 0u};
-      if (row < a.lq && 16 * st + 8 * (lane >> 5) < a.hd)
-        low = *reinterpret_cast<const u32x2*>(a.o_low + (int64_t(bh) * a.lq + row) * a.hd + 16 * st + 8 * (lane >> 5));
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const uint32_t r = (qf[n][st][e / 2] >> (16 * (e & 1))) & 0xFFFFu, g = (gf[n][st][e / 2] >> (16 * (e & 1))) & 0xFFFFu;
-        const float o = __uint_as_float(r << 16) + low_value((low[e / 4] >> (8 * (e & 3))) & 0xFFu, r);
-        s = __builtin_fmaf(o, __uint_as_float(g << 16), s);
-      }
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t r = (qf[st][e / 2] >> (16 * (e & 1))) & 0xFFFFu, g = (gf[st][e / 2] >> (16 * (e & 1))) & 0xFFFFu;
+      const float o = __uint_as_float(r << 16) + low_value((low[e / 4] >> (8 * (e & 3))) & 0xFFu, r);
+      sum = __builtin_fmaf(o, __uint_as_float(g << 16), sum);
     }
-    delta[n] = halves_sum(s);
-    lse[n] = row < a.lq ? a.lse[int64_t(bh) * a.lq + row] : __builtin_inff();
-    if (row < a.lq && lane < 32) ga.delta[int64_t(bh) * a.lq + row] = delta[n];
-    load_frags<HD>(qf[n], a.q + b * a.qs[0] + h * a.qs[1], a.qs[2], row, a.lq, a.hd, lane);
-#pragma unroll
-    for (int d = 0; d < HD / 32; ++d) dq[n][d] = zero16();
   }
+  const float delta = halves_sum(sum);
+  const float lse = row < a.lq ? a.lse[int64_t(bh) * a.lq + row] : __builtin_inff();
+  if (row < a.lq && lane < 32) ga.delta[int64_t(bh) * a.lq + row] = delta;
+  load_frags<HD>(qf, a.q + b * a.qs[0] + h * a.qs[1], a.qs[2], row, a.lq, a.hd, lane);
+  f32x16 dq[HD / 32];
+#pragma unroll
+  for (int d = 0; d < HD / 32; ++d) dq[d] = zero16();
 
   auto step = [&](int t, TilePair<HD>& now, TilePair<HD>& next) {
     copies_done();
@@ -757,47 +744,34 @@ __device__ __forceinline__ bool attn_dq(const AttnGradArgs& ga, TilePair<HD>& ev
     const int j0 = walk.key(t);
     if (w0 > last || none_seen(j0, kBN, pmin, pmax, a.window, a.sinks)) return;
     const bool edge = mode != kPlain || !all_seen(j0, kBN, pmin, pmax, a.window, a.sinks);
-#pragma unroll (HD == 64 ? 2 : 1)
+    constexpr int kUnroll = HD == 64 ? 2 : 1;
+#pragma unroll kUnroll
     for (int kb = 0; kb < 2; ++kb) {
-      f32x16 s[NQ], dp[NQ];
-#pragma unroll
-      for (int n = 0; n < NQ; ++n) s[n] = dp[n] = zero16();
+      f32x16 s = zero16(), dp = zero16();
 #pragma unroll
       for (int st = 0; st < KS; ++st) {
-        const u32x4 kf = Tile<HD>::row_frag(now.k, 32 * kb, st, lane), vf = Tile<HD>::row_frag(now.v, 32 * kb, st, lane);
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) {
-          s[n] = mfma32x32x16(kf, qf[n][st], s[n]);
-          dp[n] = mfma32x32x16(vf, gf[n][st], dp[n]);
-        }
+        s = mfma32x32x16(Tile<HD>::row_frag(now.k, 32 * kb, st, lane), qf[st], s);
+        dp = mfma32x32x16(Tile<HD>::row_frag(now.v, 32 * kb, st, lane), gf[st], dp);
       }
-      u32x4 ds[NQ][2], dr[NQ][2];
 #pragma unroll
-      for (int n = 0; n < NQ; ++n) {
+      for (int e = 0; e < 16; ++e) s[e] = exp2_fast(__builtin_fmaf(s[e], c, -lse)) * (dp[e] - delta);
+      if (edge) {
+        if (mode != kPlain) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-          s[n][e] = exp2_fast(__builtin_fmaf(s[n][e], c, -lse[n])) * (dp[n][e] - delta[n]);
-        if (edge) {
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int j = 32 * kb + acc_row(e, lane);
-            const float v = mode != kPlain && bad_key[j] ? __builtin_nanf("") : s[n][e];
-            s[n][e] = seen(j0 + j, w0 + 32 * n + (lane & 31) + off, a.window, a.sinks) ? v : 0.0f;
-          }
+          for (int e = 0; e < 16; ++e) s[e] = bad_key[32 * kb + acc_row(e, lane)] ? __builtin_nanf("") : s[e];
         }
-        pack_steps(s[n], ds[n]);
-        if constexpr (FINE) pack_rest(s[n], ds[n], dr[n]);
+        hide_unseen(s, 0.0f, j0 + 32 * kb + 4 * (lane >> 5), p, j0 < a.sinks, a.window, a.sinks);
       }
+      u32x4 ds[2], dr[2];
+      pack_steps(s, ds);
+      if constexpr (FINE) pack_rest(s, ds, dr);
 #pragma unroll
       for (int st = 0; st < 2; ++st)
 #pragma unroll
         for (int d = 0; d < HD / 32; ++d) {
           const u32x4 kf = Tile<HD>::col_frag(now.k, 32 * kb + 16 * st, d, lane);
-#pragma unroll
-          for (int n = 0; n < NQ; ++n) {
-            dq[n][d] = mfma32x32x16(kf, ds[n][st], dq[n][d]);
-            if constexpr (FINE) dq[n][d] = mfma32x32x16(kf, dr[n][st], dq[n][d]);
-          }
+          dq[d] = mfma32x32x16(kf, ds[st], dq[d]);
+          if constexpr (FINE) dq[d] = mfma32x32x16(kf, dr[st], dq[d]);
         }
     }
   };
@@ -805,32 +779,22 @@ __device__ __forceinline__ bool attn_dq(const AttnGradArgs& ga, TilePair<HD>& ev
     step(t, even, odd);
     if (t + 1 < walk.count) step(t + 1, odd, even);
   }
-  if (mode == kPlain) {
-    bool bad = false;
-#pragma unroll
-    for (int n = 0; n < NQ; ++n) bad |= not_finite(dq[n]);
-    if (__syncthreads_or(bad)) return false;
-  }
-#pragma unroll
-  for (int n = 0; n < NQ; ++n) {
-    const int row = w0 + 32 * n + (lane & 31);
-    if (row < a.lq)
-      store_rows<HD>(dq[n], a.scale, ga.dq + b * ga.dqs[0] + h * ga.dqs[1] + row * ga.dqs[2], a.hd, lane);
-  }
+  if (mode == kPlain && __syncthreads_or(not_finite(dq))) return false;
+  if (row < a.lq)
+    store_rows<HD>(dq, a.scale, ga.dq + b * ga.dqs[0] + h * ga.dqs[1] + row * ga.dqs[2], a.hd, lane);
   return true;
 }
 
-template <int HD, int NQ, int WAVES, bool FINE>
-__global__ __launch_bounds__(256, WAVES) void k_attn_dq(AttnGradArgs ga) {
-  constexpr int BM = 128 * NQ;
+template <int HD, bool FINE>
+__global__ __launch_bounds__(256, 2) void k_attn_dq(AttnGradArgs ga) {
   __shared__ __attribute__((aligned(16))) TilePair<HD> even, odd;
   __shared__ int bad_key[kBN];
-  const int nqb = (ga.f.lq + BM - 1) / BM;
+  const int nqb = (ga.f.lq + 127) / 128;
   const uint32_t id = xcd_remap(blockIdx.x, gridDim.x);
-  const int bh = static_cast<int>(id / nqb), q0 = (nqb - 1 - static_cast<int>(id % nqb)) * BM;
+  const int bh = static_cast<int>(id / nqb), q0 = (nqb - 1 - static_cast<int>(id % nqb)) * 128;
 #pragma unroll 1
   for (int mode = kPlain; mode <= kClean; ++mode) {
-    if (attn_dq<HD, NQ, FINE>(ga, even, odd, bad_key, bh, q0, mode)) break;
+    if (attn_dq<HD, FINE>(ga, even, odd, bad_key, bh, q0, mode)) break;
     __syncthreads();
   }
 }
@@ -914,7 +878,8 @@ __device__ __forceinline__ bool attn_dkv(const AttnGradArgs& ga, RowPair<HD>& ev
       __syncthreads();
     }
     const int r0 = (i0 + (first + t) % tiles) * kBN;
-#pragma unroll (HD == 64 ? 2 : 1)
+    constexpr int kUnroll = HD == 64 ? 2 : 1;
+#pragma unroll kUnroll
     for (int qb = 0; qb < 2; ++qb) {
       const int i1st = r0 + 32 * qb, pmin = i1st + off, pmax = pmin + 31;
       if (w0 > kl || i1st >= a.lq) continue;
@@ -1079,10 +1044,10 @@ void launch_join(const AttnArgs& a, hipStream_t s) {
   hipLaunchKernelGGL(k_attn_join, dim3(static_cast<uint32_t>(int64_t(a.b) * a.heads * a.lq)), dim3(256), 0, s, a);
 }
 
-template <int HD, int NQ, int WAVES>
+template <int HD>
 void launch_fwd(const AttnArgs& a, hipStream_t s) {
-  const int grid = a.b * a.heads * static_cast<int>(ceil_div(a.lq, 128 * NQ)) * (a.splits > 0 ? a.splits : 1);
-  hipLaunchKernelGGL((k_attn_fwd<HD, NQ, WAVES>), dim3(grid), dim3(256), 0, s, a);
+  const int grid = a.b * a.heads * static_cast<int>(ceil_div(a.lq, 128)) * (a.splits > 0 ? a.splits : 1);
+  hipLaunchKernelGGL((k_attn_fwd<HD>), dim3(grid), dim3(256), 0, s, a);
   if (a.splits > 0) launch_join(a, s);
 }
 
@@ -1094,10 +1059,10 @@ void launch_waves(const AttnArgs& a, hipStream_t s) {
   launch_join(a, s);
 }
 
-template <int HD, int NQ, int WQ, int WK, bool FINE>
+template <int HD, int WK, bool FINE>
 void launch_grads(const AttnGradArgs& a, bool kv, hipStream_t s) {
-  const int grid = a.f.b * a.f.heads * static_cast<int>(ceil_div(a.f.lq, 128 * NQ));
-  hipLaunchKernelGGL((k_attn_dq<HD, NQ, WQ, FINE>), dim3(grid), dim3(256), 0, s, a);
+  const int grid = a.f.b * a.f.heads * static_cast<int>(ceil_div(a.f.lq, 128));
+  hipLaunchKernelGGL((k_attn_dq<HD, FINE>), dim3(grid), dim3(256), 0, s, a);
   if (!kv) return;
   const int bk = a.f.b * a.f.kv;
   const int nkb = static_cast<int>(ceil_div(a.f.lk, 128)), run = run_of(nkb, bk);
@@ -1111,10 +1076,10 @@ void launch_grads(const AttnGradArgs& a, bool kv, hipStream_t s) {
   }
 }
 
-template <int HD, int NQ, int WQ, int WK>
+template <int HD, int WK>
 void launch_bwd(const AttnGradArgs& a, bool kv, hipStream_t s) {
-  if (a.fine) launch_grads<HD, NQ, WQ, WK, true>(a, kv, s);
-  else launch_grads<HD, NQ, WQ, WK, false>(a, kv, s);
+  if (a.fine) launch_grads<HD, WK, true>(a, kv, s);
+  else launch_grads<HD, WK, false>(a, kv, s);
 }
 
 int status() { return hipGetLastError() == hipSuccess ? 0 : -5; }
@@ -1129,15 +1094,18 @@ extern "C" {
 int compact_attention_fwd(const AttnArgs* a, void* stream) {
   if (!args_ok(*a)) return -1;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (a->splits > 0 && (int64_t(a->b) * a->heads * a->lq >= int64_t(1) << 24 || a->part_o == nullptr)) return -1;
+  if (a->splits > 0 &&
+      (a->splits > 4096 || int64_t(a->b) * a->heads * a->lq >= int64_t(1) << 24 || a->part_o == nullptr ||
+       int64_t(a->b) * a->heads * ceil_div(a->lq, 128) * a->splits >= int64_t(1) << 31))
+    return -1;
   if (a->splits > 0 && a->waves) {
     if (int64_t(a->b) * a->kv > 65535 || ceil_div(int64_t(a->heads / a->kv) * a->lq, 32) > 65535) return -1;
     if (a->hd <= 64) launch_waves<64>(*a, s);
     else if (a->hd <= 96) launch_waves<96>(*a, s);
     else launch_waves<128>(*a, s);
-  } else if (a->hd <= 64) launch_fwd<64, 1, 2>(*a, s);
-  else if (a->hd <= 96) launch_fwd<96, 1, 2>(*a, s);
-  else launch_fwd<128, 1, 2>(*a, s);
+  } else if (a->hd <= 64) launch_fwd<64>(*a, s);
+  else if (a->hd <= 96) launch_fwd<96>(*a, s);
+  else launch_fwd<128>(*a, s);
   return status();
 }
 
@@ -1157,9 +1125,9 @@ int compact_attention_bwd(const AttnGradArgs* args, void* stream) {
   hipStream_t s = static_cast<hipStream_t>(stream);
   const bool kv = a->dk != nullptr;
   if (plan_dkv(&plan) > 0 && kv && a->part == nullptr) return -1;
-  if (a->f.hd <= 64) launch_bwd<64, 1, 2, 2>(*a, kv, s);
-  else if (a->f.hd <= 96) launch_bwd<96, 1, 2, 2>(*a, kv, s);
-  else launch_bwd<128, 1, 2, 1>(*a, kv, s);
+  if (a->f.hd <= 64) launch_bwd<64, 2>(*a, kv, s);
+  else if (a->f.hd <= 96) launch_bwd<96, 2>(*a, kv, s);
+  else launch_bwd<128, 1>(*a, kv, s);
   return status();
 }
 
