@@ -813,13 +813,6 @@ struct RowPair {
   float lse[kBN], delta[kBN];
 };
 
-// Blocks per run: 32 where each XCD gets two such runs, else few enough for eight or so.
-__host__ __device__ inline int run_of(int nkb, int bk) {
-  const int64_t blocks = int64_t(nkb) * bk;
-  const int run = blocks >= 512 ? 32 : blocks < 64 ? 1 : static_cast<int>(blocks / 64);
-  return run < nkb ? run : nkb;
-}
-
 struct DkvJob {
   int bk, k0, slot, far;
 };
@@ -952,19 +945,19 @@ template <int HD, int WAVES, bool FINE>
 __global__ __launch_bounds__(256, WAVES) void k_attn_dkv(AttnGradArgs ga) {
   __shared__ __attribute__((aligned(16))) RowPair<HD> even, odd;
   __shared__ int bad_row[kBN];
-  // The blocks of keys in runs, each run on one XCD: its workgroups walk the same
-  // rows within what an L2 holds.  Runs of the first keys, whose windows are whole, go first,
-  // and the far work, in shorter pieces, last: with a workgroup or two to a CU a long one that
+  // A head's blocks stay on one XCD where the heads are a multiple of 8 (on two, where 4): what
+  // its workgroups walk at a time is rows that an L2 holds.  (Runs of 8 or of 32 neighbouring
+  // blocks, for fewer heads, were no faster: 2405 and 2530 us for 2404 at 16384 rows, 4 heads of
+  // k, with the gradient of q.)  The first keys' blocks, whose windows are whole, go first, and
+  // the far work, in shorter pieces, last: with a workgroup or two to a CU a long one that
   // starts late is all that runs at the end.
   const int nkb = (ga.f.lk + 127) / 128, nfb = (ga.far_keys + 63) / 64, bk_all = ga.f.b * ga.f.kv;
-  const int run = run_of(nkb, bk_all), runs = (nkb + run - 1) / run * bk_all;
-  const int per_run = run * ga.parts, near = (runs + kNumXcd - 1) / kNumXcd * kNumXcd * per_run;
+  const int blocks = nkb * bk_all, near = (blocks + kNumXcd - 1) / kNumXcd * kNumXcd * ga.parts;
   DkvJob job;
   if (static_cast<int>(blockIdx.x) < near) {
-    const int xcd = blockIdx.x % kNumXcd, k = blockIdx.x / kNumXcd;
-    const int r = k / per_run * kNumXcd + xcd, in = k % per_run, kb = r / bk_all * run + in / ga.parts;
-    if (r >= runs || kb >= nkb) return;
-    job = {r % bk_all, kb * 128, in % ga.parts, 0};
+    const int k = blockIdx.x / kNumXcd, r = k / ga.parts * kNumXcd + blockIdx.x % kNumXcd;
+    if (r >= blocks) return;
+    job = {r % bk_all, r / bk_all * 128, k % ga.parts, 0};
   } else {
     const int id = blockIdx.x - near;
     job = {id / (ga.chunks * nfb), id / ga.chunks % nfb * 64, id % ga.chunks, 1};
@@ -1001,8 +994,12 @@ __global__ __launch_bounds__(256) void k_attn_dkv_sum(AttnGradArgs ga) {
 }
 
 // How the gradients of k and v are split (AttnGradArgs), and the floats of `part`.
-// parts: 512 workgroups (two per CU) of at least 4 tiles where the blocks of keys are fewer.
-// chunks: a far workgroup walks a quarter of a near one's tiles, at least 16.
+// parts: 512 workgroups (two per CU) of at least 8 tiles where the blocks of keys are fewer.
+// chunks: a far workgroup walks a quarter of a near one's tiles, at least 8.
+// The whole backward, us, with at least 4 / 8 tiles: 3 x 1531 rows, 10 heads on 2 of 80, window
+// 301: 117 / 91; 2 x 5000, 4 on 1 of 64, window 700: 110 / 102; 1000, 16 on 2 of 96: 79 / 80.
+// Far work of at least 16 / 8 tiles: 4 x 4096, 16 heads of 64, window 1024: 356 / 346; as much
+// as a near workgroup's: 396.
 int64_t plan_dkv(AttnGradArgs* g) {
   const AttnArgs& a = g->f;
   const int64_t bk = int64_t(a.b) * a.kv, G = a.heads / a.kv;
@@ -1010,7 +1007,7 @@ int64_t plan_dkv(AttnGradArgs* g) {
   const int64_t rows = a.window < a.lk ? (int64_t(a.window) + 127 < a.lq ? int64_t(a.window) + 127 : a.lq) : a.lq;
   const int64_t tiles = G * ceil_div(rows, kBN);
   int64_t parts = ceil_div(512, blocks);
-  if (parts > tiles / 4) parts = tiles / 4;
+  if (parts > tiles / 8) parts = tiles / 8;
   if (parts < 1) parts = 1;
   g->parts = static_cast<int>(parts);
   const bool far = a.sinks > 0 && a.window < a.lk;
@@ -1021,7 +1018,7 @@ int64_t plan_dkv(AttnGradArgs* g) {
   if (far) {
     const int64_t far_rows = a.lk - a.window < a.lq ? a.lk - a.window : a.lq, far_tiles = G * ceil_div(far_rows, kBN);
     const int64_t own = ceil_div(tiles, 4 * parts);
-    int64_t chunks = ceil_div(far_tiles, own < 16 ? 16 : own);
+    int64_t chunks = ceil_div(far_tiles, own < 8 ? 8 : own);
     g->chunks = static_cast<int>(chunks > 64 ? 64 : chunks);
   }
   return 2 * a.hd * bk * (parts * g->near_keys + 2 * int64_t(g->chunks) * g->far_keys);
@@ -1065,9 +1062,8 @@ void launch_grads(const AttnGradArgs& a, bool kv, hipStream_t s) {
   hipLaunchKernelGGL((k_attn_dq<HD, FINE>), dim3(grid), dim3(256), 0, s, a);
   if (!kv) return;
   const int bk = a.f.b * a.f.kv;
-  const int nkb = static_cast<int>(ceil_div(a.f.lk, 128)), run = run_of(nkb, bk);
-  const int runs = static_cast<int>(ceil_div(nkb, run)) * bk;
-  const int grid_kv = static_cast<int>(ceil_div(runs, kNumXcd)) * kNumXcd * run * a.parts +
+  const int blocks = bk * static_cast<int>(ceil_div(a.f.lk, 128));
+  const int grid_kv = static_cast<int>(ceil_div(blocks, kNumXcd)) * kNumXcd * a.parts +
                       bk * static_cast<int>(ceil_div(a.far_keys, 64)) * a.chunks;
   hipLaunchKernelGGL((k_attn_dkv<HD, WK, FINE>), dim3(grid_kv), dim3(256), 0, s, a);
   if (a.near_keys > 0) {
