@@ -806,7 +806,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnGradArgs ga) {
 // beyond the window ("far") are a work of their own: 64 of the sinks, 32 to a pair of waves
 // that share a tile's rows, in `chunks` of the tiles.  What several workgroups form lies in
 // fp32 in slots of `part`, and k_attn_dkv_sum adds the slots in order:
-//   near [parts][b kv][near_keys][2][hd], then far [2 chunks][b kv][far_keys][2][hd].
+//   near [parts][b kv][near_keys][2][hd], then far [chunks, each far_slots times][b kv][far_keys][2][hd].
 template <int HD>
 struct RowPair {
   char q[Tile<HD>::kBytes], g[Tile<HD>::kBytes];
@@ -817,20 +817,39 @@ struct DkvJob {
   int bk, k0, slot, far;
 };
 
+// Heads over 96: eight waves, of which two share 32 keys, each with half of a tile's rows; the
+// block's k and v lie in LDS, and at the end the one half's sums are added to the other's.
+// Else four waves with both halves, k and v in registers.  With 128 columns of dk and dv the
+// latter is one wave to a SIMD, with nothing to run while it waits; 64 columns leave room for
+// two anyway, and the reads of k and v cost them more.  The whole backward, us, with eight / four
+// waves: 16384 rows, 16 heads on 4 of 128, window 4096: 1917 / 2411; 2 x 4096, 16 of 128, all
+// keys: 608 / 722; 4 x 4096, 16 of 64, window 1024: 431 / 364; 1000, 16 on 2 of 96: 96 / 95.
+__host__ __device__ constexpr bool shared_keys(int hd) { return hd > 96; }
+__host__ __device__ constexpr int far_block(int hd) { return shared_keys(hd) ? 128 : 64; }
+__host__ __device__ constexpr int far_slots(int hd) { return shared_keys(hd) ? 1 : 2; }
+
+template <int HD, bool SHARED>
+struct KeyBlock {
+  char k[2][Tile<HD>::kBytes], v[2][Tile<HD>::kBytes];
+};
+template <int HD>
+struct KeyBlock<HD, false> {};
+
 template <int HD, bool FINE>
-__device__ __forceinline__ bool attn_dkv(const AttnGradArgs& ga, RowPair<HD>& even, RowPair<HD>& odd, int* bad_row,
-                                         const DkvJob& job, int mode) {
+__device__ __forceinline__ bool attn_dkv(const AttnGradArgs& ga, KeyBlock<HD, shared_keys(HD)>& keys, RowPair<HD>& even,
+                                         RowPair<HD>& odd, int* bad_row, const DkvJob& job, int mode) {
   constexpr int KS = HD / 16;
+  constexpr bool SHARED = shared_keys(HD);
   const AttnArgs& a = ga.f;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), G = a.heads / a.kv;
   const int b = job.bk / a.kv, hk = job.bk % a.kv;
   const int L = length_of(a, b), off = L - a.lq;
-  const bool far = job.far != 0;
-  const int w0 = job.k0 + 32 * (far ? wave >> 1 : wave), j = w0 + (lane & 31);
+  const bool far = job.far != 0, halves = SHARED || far;  // a wave has one half of each tile's rows
+  const int kw = halves ? wave >> 1 : wave, w0 = job.k0 + 32 * kw, j = w0 + (lane & 31);
   const float c = a.scale * kLog2e;
 
   // the rows that see some key of the block
-  const int kl = min(job.k0 + (far ? 64 : 128), far ? min(L, a.sinks) : L) - 1;
+  const int kl = min(job.k0 + (far ? far_block(HD) : 128), far ? min(L, a.sinks) : L) - 1;
   int i0 = max(0, job.k0 + (far ? a.window : 0) - off), i1 = a.lq;
   if (!far && int64_t(kl) + a.window - off < i1) i1 = kl + a.window - off;
   i0 = i0 / kBN;
@@ -841,21 +860,43 @@ __device__ __forceinline__ bool attn_dkv(const AttnGradArgs& ga, RowPair<HD>& ev
   const int per = (tiles * G + (far ? ga.chunks : ga.parts) - 1) / (far ? ga.chunks : ga.parts);
   const int first = job.slot * per, steps = max(0, min(tiles * G, first + per) - first);
 
-  Copy<HD> cq, cg;
-  cq.init(a.qs[2], a.hd, tid);
-  cg.init(ga.gs[2], a.hd, tid);
+  const uint16_t* k = a.k + b * a.ks[0] + hk * a.ks[1];
+  const uint16_t* v = a.v + b * a.vs[0] + hk * a.vs[1];
+  Copy<HD> cq, cg;  // SHARED: the first four waves copy q and k, the others do and v, all with cq
+  const bool of_g = SHARED && wave >= 4;
+  u32x4 kf[KS], vf[KS];
+  if constexpr (SHARED) {
+    if (steps > 0) {
+      const int64_t stride = of_g ? a.vs[2] : a.ks[2];
+      cq.init(stride, a.hd, tid & 255);
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        cq.issue(of_g ? v : k, stride, job.k0 + i * kBN, L, a.hd, of_g ? keys.v[i] : keys.k[i], wave & 3);
+    }
+    cq.init(of_g ? ga.gs[2] : a.qs[2], a.hd, tid & 255);
+  } else {
+    cq.init(a.qs[2], a.hd, tid);
+    cg.init(ga.gs[2], a.hd, tid);
+  }
   auto fetch = [&](int t, RowPair<HD>& to) {
     const int h = hk * G + (first + t) / tiles, r0 = (i0 + (first + t) % tiles) * kBN;
-    cq.issue(a.q + b * a.qs[0] + h * a.qs[1], a.qs[2], r0, a.lq, a.hd, to.q, wave);
-    cg.issue(ga.go + b * ga.gs[0] + h * ga.gs[1], ga.gs[2], r0, a.lq, a.hd, to.g, wave);
+    const uint16_t* q = a.q + b * a.qs[0] + h * a.qs[1];
+    const uint16_t* g = ga.go + b * ga.gs[0] + h * ga.gs[1];
+    if constexpr (SHARED) {
+      cq.issue(of_g ? g : q, of_g ? ga.gs[2] : a.qs[2], r0, a.lq, a.hd, of_g ? to.g : to.q, wave & 3);
+    } else {
+      cq.issue(q, a.qs[2], r0, a.lq, a.hd, to.q, wave);
+      cg.issue(g, ga.gs[2], r0, a.lq, a.hd, to.g, wave);
+    }
     const int64_t row = (int64_t(b) * a.heads + h) * a.lq;
     if (wave == 0) copy_row_values(a.lse + row, r0, a.lq, reinterpret_cast<char*>(to.lse), lane);
     if (wave == 1) copy_row_values(ga.delta + row, r0, a.lq, reinterpret_cast<char*>(to.delta), lane);
   };
   if (steps > 0) fetch(0, even);
-  u32x4 kf[KS], vf[KS];
-  load_frags<HD>(kf, a.k + b * a.ks[0] + hk * a.ks[1], a.ks[2], j, L, a.hd, lane);
-  load_frags<HD>(vf, a.v + b * a.vs[0] + hk * a.vs[1], a.vs[2], j, L, a.hd, lane);
+  if constexpr (!SHARED) {
+    load_frags<HD>(kf, k, a.ks[2], j, L, a.hd, lane);
+    load_frags<HD>(vf, v, a.vs[2], j, L, a.hd, lane);
+  }
   f32x16 dk[HD / 32], dv[HD / 32];
 #pragma unroll
   for (int d = 0; d < HD / 32; ++d) dk[d] = dv[d] = zero16();
@@ -866,15 +907,18 @@ __device__ __forceinline__ bool attn_dkv(const AttnGradArgs& ga, RowPair<HD>& ev
     if (mode != kPlain) {
       if (tid < kBN) bad_row[tid] = 0;
       __syncthreads();
-      convert_tile<HD>(now.q, mode, bad_row, tid);
-      convert_tile<HD>(now.g, mode, bad_row, tid);
+      convert_tile<HD, kBN, SHARED ? 512 : 256>(now.q, mode, bad_row, tid);
+      convert_tile<HD, kBN, SHARED ? 512 : 256>(now.g, mode, bad_row, tid);
       __syncthreads();
     }
     const int r0 = (i0 + (first + t) % tiles) * kBN;
+    // (Where registers are short most places in LDS are formed anew for each tile: kept, they spill.)
+    int ln = lane;
+    if constexpr (SHARED) asm volatile("" : "+v"(ln));
     constexpr int kUnroll = HD == 64 ? 2 : 1;
 #pragma unroll kUnroll
-    for (int qb = 0; qb < 2; ++qb) {
-      const int i1st = r0 + 32 * qb, pmin = i1st + off, pmax = pmin + 31;
+    for (int n = 0; n < (SHARED ? 1 : 2); ++n) {
+      const int qb = SHARED ? wave & 1 : n, i1st = r0 + 32 * qb, pmin = i1st + off, pmax = pmin + 31;
       if (w0 > kl || i1st >= a.lq) continue;
       if (far ? (wave & 1) != qb || pmax - w0 < a.window : w0 > pmax || pmin - (w0 + 31) >= a.window) continue;
       const bool all = far ? w0 + 31 < a.sinks && pmin - (w0 + 31) >= a.window : w0 + 31 <= pmin && pmax - w0 < a.window;
@@ -882,13 +926,21 @@ __device__ __forceinline__ bool attn_dkv(const AttnGradArgs& ga, RowPair<HD>& ev
       f32x16 s = zero16(), dp = zero16();
 #pragma unroll
       for (int st = 0; st < KS; ++st) {
-        s = mfma32x32x16(Tile<HD>::row_frag(now.q, 32 * qb, st, lane), kf[st], s);
-        dp = mfma32x32x16(Tile<HD>::row_frag(now.g, 32 * qb, st, lane), vf[st], dp);
+        u32x4 k1, v1;
+        if constexpr (SHARED) {
+          k1 = Tile<HD>::row_frag(keys.k[kw >> 1], 32 * (kw & 1), st, lane);
+          v1 = Tile<HD>::row_frag(keys.v[kw >> 1], 32 * (kw & 1), st, lane);
+        } else {
+          k1 = kf[st];
+          v1 = vf[st];
+        }
+        s = mfma32x32x16(Tile<HD>::row_frag(now.q, 32 * qb, st, ln), k1, s);
+        dp = mfma32x32x16(Tile<HD>::row_frag(now.g, 32 * qb, st, ln), v1, dp);
       }
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        const f32x4 l4 = *reinterpret_cast<const f32x4*>(now.lse + 32 * qb + 8 * g + 4 * (lane >> 5));
-        const f32x4 d4 = *reinterpret_cast<const f32x4*>(now.delta + 32 * qb + 8 * g + 4 * (lane >> 5));
+        const f32x4 l4 = *reinterpret_cast<const f32x4*>(now.lse + 32 * qb + 8 * g + 4 * (ln >> 5));
+        const f32x4 d4 = *reinterpret_cast<const f32x4*>(now.delta + 32 * qb + 8 * g + 4 * (ln >> 5));
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float pr = exp2_fast(__builtin_fmaf(s[4 * g + e], c, -l4[e]));
@@ -899,7 +951,7 @@ __device__ __forceinline__ bool attn_dkv(const AttnGradArgs& ga, RowPair<HD>& ev
       if (edge) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          const int r = 32 * qb + acc_row(e, lane), p = r0 + r + off;
+          const int r = 32 * qb + acc_row(e, ln), p = r0 + r + off;
           const bool in = (static_cast<uint32_t>(p - jj - apart) < span) & (p < L), nan = mode != kPlain && bad_row[r];
           s[e] = in ? (nan ? __builtin_nanf("") : s[e]) : 0.0f;
           dp[e] = in ? (nan ? __builtin_nanf("") : dp[e]) : 0.0f;
@@ -914,8 +966,8 @@ __device__ __forceinline__ bool attn_dkv(const AttnGradArgs& ga, RowPair<HD>& ev
       for (int st = 0; st < 2; ++st)
 #pragma unroll
         for (int d = 0; d < HD / 32; ++d) {
-          dv[d] = mfma32x32x16(Tile<HD>::col_frag(now.g, 32 * qb + 16 * st, d, lane), pf[st], dv[d]);
-          const u32x4 qt = Tile<HD>::col_frag(now.q, 32 * qb + 16 * st, d, lane);
+          dv[d] = mfma32x32x16(Tile<HD>::col_frag(now.g, 32 * qb + 16 * st, d, ln), pf[st], dv[d]);
+          const u32x4 qt = Tile<HD>::col_frag(now.q, 32 * qb + 16 * st, d, ln);
           dk[d] = mfma32x32x16(qt, df[st], dk[d]);
           if constexpr (FINE) dk[d] = mfma32x32x16(qt, dr[st], dk[d]);
         }
@@ -925,13 +977,44 @@ __device__ __forceinline__ bool attn_dkv(const AttnGradArgs& ga, RowPair<HD>& ev
     step(t, even, odd);
     if (t + 1 < steps) step(t + 1, odd, even);
   }
-  if (mode == kPlain && __syncthreads_or(not_finite(dk) || not_finite(dv))) return false;
+  if (mode == kPlain) {
+    if (__syncthreads_or(not_finite(dk) || not_finite(dv))) return false;
+  } else if (SHARED) {
+    __syncthreads();
+  }
+  if constexpr (SHARED) {
+    // (128 columns of four waves: in fp32 as much as the block's k and v in bf16)
+    f32x4* at = reinterpret_cast<f32x4*>(&keys) + kw * (HD / 8) * 64 + lane;
+    auto join = [&](f32x16 (&x)[HD / 32]) {
+      if (wave & 1) {
+#pragma unroll
+        for (int i = 0; i < HD / 8; ++i) {
+          const f32x16& y = x[i / 4];
+          at[i * 64] = f32x4{y[4 * (i % 4)], y[4 * (i % 4) + 1], y[4 * (i % 4) + 2], y[4 * (i % 4) + 3]};
+        }
+      }
+      __syncthreads();
+      if (!(wave & 1)) {
+#pragma unroll
+        for (int i = 0; i < HD / 8; ++i) {
+          const f32x4 y = at[i * 64];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[i / 4][4 * (i % 4) + e] += y[e];
+        }
+      }
+      __syncthreads();
+    };
+    join(dk);
+    join(dv);
+    if (wave & 1) return true;
+  }
   const int64_t bk_all = int64_t(a.b) * a.kv;
   if (far || j < ga.near_keys) {
     if (j >= (far ? ga.far_keys : ga.near_keys)) return true;
+    const int slot = far ? far_slots(HD) * job.slot + (SHARED ? 0 : wave & 1) : job.slot;
     float* out = ga.part;
-    if (far) out += (ga.parts * bk_all * ga.near_keys + ((2 * job.slot + (wave & 1)) * bk_all + job.bk) * ga.far_keys + j) * 2 * a.hd;
-    else out += ((job.slot * bk_all + job.bk) * ga.near_keys + j) * 2 * a.hd;
+    if (far) out += (ga.parts * bk_all * ga.near_keys + (slot * bk_all + job.bk) * ga.far_keys + j) * 2 * a.hd;
+    else out += ((slot * bk_all + job.bk) * ga.near_keys + j) * 2 * a.hd;
     store_row_values<HD>(dk, a.scale, out, a.hd, lane);
     store_row_values<HD>(dv, 1.0f, out + a.hd, a.hd, lane);
   } else if (j < a.lk) {
@@ -941,8 +1024,9 @@ __device__ __forceinline__ bool attn_dkv(const AttnGradArgs& ga, RowPair<HD>& ev
   return true;
 }
 
-template <int HD, int WAVES, bool FINE>
-__global__ __launch_bounds__(256, WAVES) void k_attn_dkv(AttnGradArgs ga) {
+template <int HD, bool FINE>
+__global__ __launch_bounds__(shared_keys(HD) ? 512 : 256, 2) void k_attn_dkv(AttnGradArgs ga) {
+  __shared__ __attribute__((aligned(16))) KeyBlock<HD, shared_keys(HD)> keys;
   __shared__ __attribute__((aligned(16))) RowPair<HD> even, odd;
   __shared__ int bad_row[kBN];
   // A head's blocks stay on one XCD where the heads are a multiple of 8 (on two, where 4): what
@@ -951,7 +1035,7 @@ __global__ __launch_bounds__(256, WAVES) void k_attn_dkv(AttnGradArgs ga) {
   // k, with the gradient of q.)  The first keys' blocks, whose windows are whole, go first, and
   // the far work, in shorter pieces, last: with a workgroup or two to a CU a long one that
   // starts late is all that runs at the end.
-  const int nkb = (ga.f.lk + 127) / 128, nfb = (ga.far_keys + 63) / 64, bk_all = ga.f.b * ga.f.kv;
+  const int nkb = (ga.f.lk + 127) / 128, nfb = (ga.far_keys + far_block(HD) - 1) / far_block(HD), bk_all = ga.f.b * ga.f.kv;
   const int blocks = nkb * bk_all, near = (blocks + kNumXcd - 1) / kNumXcd * kNumXcd * ga.parts;
   DkvJob job;
   if (static_cast<int>(blockIdx.x) < near) {
@@ -960,11 +1044,11 @@ __global__ __launch_bounds__(256, WAVES) void k_attn_dkv(AttnGradArgs ga) {
     job = {r % bk_all, r / bk_all * 128, k % ga.parts, 0};
   } else {
     const int id = blockIdx.x - near;
-    job = {id / (ga.chunks * nfb), id / ga.chunks % nfb * 64, id % ga.chunks, 1};
+    job = {id / (ga.chunks * nfb), id / ga.chunks % nfb * far_block(HD), id % ga.chunks, 1};
   }
 #pragma unroll 1
   for (int mode = kPlain; mode <= kClean; ++mode) {
-    if (attn_dkv<HD, FINE>(ga, even, odd, bad_row, job, mode)) break;
+    if (attn_dkv<HD, FINE>(ga, keys, even, odd, bad_row, job, mode)) break;
     __syncthreads();
   }
 }
@@ -983,7 +1067,7 @@ __global__ __launch_bounds__(256) void k_attn_dkv_sum(AttnGradArgs ga) {
     s += *reinterpret_cast<const f32x4*>(ga.part + ((p * bk_all + bk) * ga.near_keys + j) * 2 * a.hd + col);
   if (j < ga.far_keys) {
     const float* far = ga.part + ga.parts * bk_all * ga.near_keys * 2 * a.hd;
-    for (int p = 0; p < 2 * ga.chunks; ++p)
+    for (int p = 0; p < far_slots(a.hd) * ga.chunks; ++p)
       s += *reinterpret_cast<const f32x4*>(far + ((p * bk_all + bk) * ga.far_keys + j) * 2 * a.hd + col);
   }
   const int b = static_cast<int>(bk / a.kv), hk = static_cast<int>(bk % a.kv);
@@ -1021,7 +1105,7 @@ int64_t plan_dkv(AttnGradArgs* g) {
     int64_t chunks = ceil_div(far_tiles, own < 8 ? 8 : own);
     g->chunks = static_cast<int>(chunks > 64 ? 64 : chunks);
   }
-  return 2 * a.hd * bk * (parts * g->near_keys + 2 * int64_t(g->chunks) * g->far_keys);
+  return 2 * a.hd * bk * (parts * g->near_keys + far_slots(a.hd) * int64_t(g->chunks) * g->far_keys);
 }
 
 bool args_ok(const AttnArgs& a) {
@@ -1056,7 +1140,7 @@ void launch_waves(const AttnArgs& a, hipStream_t s) {
   launch_join(a, s);
 }
 
-template <int HD, int WK, bool FINE>
+template <int HD, bool FINE>
 void launch_grads(const AttnGradArgs& a, bool kv, hipStream_t s) {
   const int grid = a.f.b * a.f.heads * static_cast<int>(ceil_div(a.f.lq, 128));
   hipLaunchKernelGGL((k_attn_dq<HD, FINE>), dim3(grid), dim3(256), 0, s, a);
@@ -1064,18 +1148,18 @@ void launch_grads(const AttnGradArgs& a, bool kv, hipStream_t s) {
   const int bk = a.f.b * a.f.kv;
   const int blocks = bk * static_cast<int>(ceil_div(a.f.lk, 128));
   const int grid_kv = static_cast<int>(ceil_div(blocks, kNumXcd)) * kNumXcd * a.parts +
-                      bk * static_cast<int>(ceil_div(a.far_keys, 64)) * a.chunks;
-  hipLaunchKernelGGL((k_attn_dkv<HD, WK, FINE>), dim3(grid_kv), dim3(256), 0, s, a);
+                      bk * static_cast<int>(ceil_div(a.far_keys, far_block(HD))) * a.chunks;
+  hipLaunchKernelGGL((k_attn_dkv<HD, FINE>), dim3(grid_kv), dim3(shared_keys(HD) ? 512 : 256), 0, s, a);
   if (a.near_keys > 0) {
     const int64_t threads = int64_t(bk) * a.near_keys * (a.f.hd / 2);
     hipLaunchKernelGGL(k_attn_dkv_sum, dim3(static_cast<uint32_t>(ceil_div(threads, 256))), dim3(256), 0, s, a);
   }
 }
 
-template <int HD, int WK>
+template <int HD>
 void launch_bwd(const AttnGradArgs& a, bool kv, hipStream_t s) {
-  if (a.fine) launch_grads<HD, WK, true>(a, kv, s);
-  else launch_grads<HD, WK, false>(a, kv, s);
+  if (a.fine) launch_grads<HD, true>(a, kv, s);
+  else launch_grads<HD, false>(a, kv, s);
 }
 
 int status() { return hipGetLastError() == hipSuccess ? 0 : -5; }
@@ -1121,9 +1205,9 @@ int compact_attention_bwd(const AttnGradArgs* args, void* stream) {
   hipStream_t s = static_cast<hipStream_t>(stream);
   const bool kv = a->dk != nullptr;
   if (plan_dkv(&plan) > 0 && kv && a->part == nullptr) return -1;
-  if (a->f.hd <= 64) launch_bwd<64, 2>(*a, kv, s);
-  else if (a->f.hd <= 96) launch_bwd<96, 2>(*a, kv, s);
-  else launch_bwd<128, 1>(*a, kv, s);
+  if (a->f.hd <= 64) launch_bwd<64>(*a, kv, s);
+  else if (a->f.hd <= 96) launch_bwd<96>(*a, kv, s);
+  else launch_bwd<128>(*a, kv, s);
   return status();
 }
 
