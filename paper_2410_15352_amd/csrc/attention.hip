@@ -33,7 +33,8 @@ constexpr float kLog2e = 1.44269504088896340736f;
 // dS rounded to bf16 alone leaves dq and dk, rounded themselves, 1.42 times as far from the
 // exact gradients as their own rounding; with few keys to a row the error of o in D comes on
 // top (1.49 at windows of 16 and 20).  In two parts: 1.02 to 1.08.  Two more products of nine:
-// 8% of the backward's time with heads of 64, 17% with heads of 128, where windows are long.
+// where windows are long 10% of the backward's time with heads of 64 (355 to 390 us at 4 x 4096
+// rows, window 1024) and 18% with heads of 128 (1885 to 2230 us at 16384, window 4096).
 constexpr int kFineKeys = 512;
 constexpr int kBN = 64;  // keys (or queries) per staged tile
 
@@ -384,9 +385,12 @@ struct Softmax {
 // Bound by the latency of a wave's own chain (scores, maximum, exponentials, P V) with two or
 // three waves on a SIMD: at heads of 64 the matrix units work 23 % of the time and the vector
 // units 65 %, at 128 the matrix units 40 %; LDS has no bank conflicts.  Tried and slower: the
-// next tile's scores among this one's exponentials (heads of 64: 125-145 us for 109 at
+// next tile's scores among this one's exponentials (heads of 64: 125-145 us for 105 at
 // 4 x 4096, 16 heads, window 1024; heads of 128: 3-7 % faster, but its two tiles of scores do
 // not fit the registers), 64 columns per wave (no longer two workgroups per CU).
+// Measured: that 105 us, 574 TFLOP/s over the pairs that are seen; 557 us, 865 TFLOP/s, at
+// 16384 rows, 16 heads on 4 of 128, window 4096; 26 us at 3 x 1531 rows, 10 on 2 of 80, window
+// 301; 19 us at 32 x 256 rows, 8 heads, window 128.  A large matrix product: 1223 TFLOP/s.
 template <int HD>
 struct TilePair {
   char k[Tile<HD>::kBytes], v[Tile<HD>::kBytes];
@@ -517,7 +521,10 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnArgs a) {
 // Few rows over many keys: the rows of the heads that share keys (32 of the G lq at a time)
 // are the columns of one wave, and each wave takes a range of the keys on its own: K straight
 // from memory as the A operand, V by copies into its own part of LDS, both a tile of 32 keys
-// ahead.
+// ahead.  Bound by HBM where there are keys enough: 165 us, 5.2 TB/s, for one token of 4
+// sequences of up to 70000 keys, 32 heads on 8 of 128 (with the join 175 us), as a large copy;
+// 16 us and the join's 4 for 16 sequences, 16 heads of 64, 1028 keys seen (4.3 TB/s over both
+// would be 13 us), where each wave's few tiles in a row are what counts.
 template <int HD>
 struct WaveTiles {
   char v[4][32 * HD * 2];
@@ -679,9 +686,14 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
 }
 
 // ------------------------------ gradient of q --------------------------------
-// As the forward, with S^T and dP^T = V dO^T; D = sum(dO o) on the way,
-// for the other kernel too.  Where the sums are not finite the work is done again with clean
-// values, and NaN in the rows that see a key that had others.
+// As the forward, with S^T and dP^T = V dO^T; D = sum(dO o) on the way, for the other kernel
+// too.  Where the sums are not finite the work is done again with clean values, and NaN in the
+// rows that see a key that had others.
+//
+// Bound as the forward.  Measured: 160 us at 4 x 4096 rows, 16 heads of 64, window 1024; 742 us,
+// 970 TFLOP/s of its three products, at 16384 rows, 16 heads on 4 of 128, window 4096; 24 us at
+// 32 x 256 rows, 8 heads of 64, window 128.  (Three waves to a SIMD at heads of 64, with places
+// in LDS formed for each tile: 352 us with the other gradients for 344.)
 template <int HD, bool FINE>
 __device__ __forceinline__ bool attn_dq(const AttnGradArgs& ga, TilePair<HD>& even, TilePair<HD>& odd, int* bad_key, int bh,
                                         int q0, int mode) {
@@ -800,13 +812,21 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnGradArgs ga) {
 }
 
 // --------------------------- gradients of k and v ----------------------------
-// A workgroup takes 128 keys, 32 per wave, and walks the query tiles of the heads that share
-// them in order.  Two things would leave the card to a few long workgroups: few keys and heads
-// (then `parts` workgroups share a block's tiles), and the sinks, which every row sees.  Pairs
-// beyond the window ("far") are a work of their own: 64 of the sinks, 32 to a pair of waves
-// that share a tile's rows, in `chunks` of the tiles.  What several workgroups form lies in
-// fp32 in slots of `part`, and k_attn_dkv_sum adds the slots in order:
+// A workgroup takes 128 keys and walks the query tiles of the heads that share them in order: no
+// atomics, the same sums every time.  Two things would leave the card to a few long workgroups:
+// few keys and heads (then `parts` workgroups share a block's tiles), and the sinks, which every
+// row sees.  Pairs beyond the window ("far") are a work of their own: 64 (128) of the sinks, 32
+// to a pair of waves that share a tile's rows, in `chunks` of the tiles.  What several workgroups
+// form lies in fp32 in slots of `part`, and k_attn_dkv_sum adds the slots in order:
 //   near [parts][b kv][near_keys][2][hd], then far [chunks, each far_slots times][b kv][far_keys][2][hd].
+//
+// Bound by the chain of one wave (products, exponentials, products) with two to a SIMD, and with
+// 128 columns by LDS too: a step's fragments take 1.5 times as long to read as its products.
+// Measured: 209 us at 4 x 4096 rows, 16 heads of 64, window 1024; 1213 us, 790 TFLOP/s of its four
+// products, at 16384 rows, 16 heads on 4 of 128, window 4096; 27 us at 32 x 256 rows, 8 heads of
+// 64, window 128.  Both halves of a tile in one stretch of code were slower (2702 us with the
+// gradient of q for 2580, spilled or at one wave to a SIMD), and so were three waves at heads of
+// 64 (369 for 344).
 template <int HD>
 struct RowPair {
   char q[Tile<HD>::kBytes], g[Tile<HD>::kBytes];

@@ -14,6 +14,12 @@
 // walks over registers, and the next row's loads are issued chunk by chunk behind the
 // gradient's.  The gradient is formed where the loss is, for dloss = 1; the backward runs
 // the same kernel again, which ends at once where dloss is 1 indeed.
+//
+// Measured, loss and gradient in bf16: 8192 rows of 32000 logits 286 us, 3.7 TB/s, at T = 2 with
+// targets (two exponentials per logit and walk), 243 us, 4.3 TB/s, at T = 1; 4096 rows of 131072
+// without targets 508 us, 4.2 TB/s; a large copy reaches 5.2 TB/s.  Of it 12 us are the entries'
+// kernel and 5 the mean's.  Rows of a thousand logits are bound by a row's chain of walks and
+// barriers: 16384 of them 83 us, 0.8 TB/s.
 #include <hip/hip_runtime.h>
 
 #include "common.hpp"
@@ -370,7 +376,8 @@ __global__ __launch_bounds__(1024) void k_distill_mean(DistillArgs a) {
 
 template <bool F32, int THREADS, int NC>
 void launch_row(const DistillArgs& a, hipStream_t s) {
-  // as many workgroups as the card holds, each with its share of the rows
+  // as many workgroups as the card holds, each with its share of the rows.  (Twice as many are
+  // as fast, within 3%; but the loss alone of 4096 fp32 rows of 32000 takes 122 us for 109.)
   const int64_t most = 256 * ((NC > 4 ? 1024 : 1536) / THREADS);
   const dim3 grid(static_cast<uint32_t>(a.rows < most ? a.rows : most)), block(THREADS);
   const bool hard = a.target != nullptr && a.weight != 1.0f;
@@ -381,6 +388,14 @@ void launch_row(const DistillArgs& a, hipStream_t s) {
 
 template <bool F32>
 void launch(const DistillArgs& a, hipStream_t s) {
+  // The smallest workgroup whose registers hold a row, or all but the last 3% of it.  us by
+  // threads x chunks, loss and gradient in bf16 at T = 2 (the rule's *):
+  //             256 x 1  256 x 4  256 x 16  512 x 16  1024 x 16
+  //   16384 x   1000  83*     146      429       838      1656
+  //    8192 x   8000 104       90*     224       425       838
+  //    8192 x  32001 344      330      282*      441       839
+  //    2048 x  65536 200      194      182       151*      233
+  //    1024 x 200000 365      361      337       290       260*
   const int64_t chunks = a.V / (F32 ? 4 : 8);
   if (chunks <= 256) launch_row<F32, 256, 1>(a, s);
   else if (chunks <= 1024) launch_row<F32, 256, 4>(a, s);

@@ -9,6 +9,10 @@
 // product of the position and the frequency, of which the nearest whole number is taken off:
 // exact for any position, where an fp32 product is off by 2^-24 of the angle), and so are the
 // tokens' places in the up to three tensors of a call; then they serve every head.
+//
+// Measured: 12.7 us, 5.3 TB/s, for q and k of 32 x 256 tokens, 16 heads of 64 in bf16; 207 us,
+// 4.75 TB/s, for 2 x 12001 tokens, 32 and 8 heads of 128 in fp32, the first half turned; 3.3 us,
+// a launch, for one token of 8 sequences.  (A large copy reaches 5.2 TB/s.)
 #include <hip/hip_runtime.h>
 
 #include "common.hpp"
@@ -180,6 +184,8 @@ __global__ __launch_bounds__(256) void k_rotary(RotaryArgs a, RotaryPlan pl) {
 
 template <bool F32, int N, bool PAIRS>
 void launch(const RotaryArgs& a, const RotaryPlan& p, dim3 grid, hipStream_t s) {
+  // (one, two or four items in flight: 215, 207 and 204 us for the fp32 tensors above, 42.8, 43.6
+  // and 46.2 for 8 x 4096 tokens, 20 heads of 96 in bf16)
   hipLaunchKernelGGL((k_rotary<F32, N, PAIRS, 2>), grid, dim3(256), 0, s, a, p);
 }
 
@@ -201,6 +207,7 @@ extern "C" int compact_rotary(const RotaryArgs* a, void* stream) {
     heads += a->t[i].heads;
   }
   // elements moved in one piece: halves start where the widest piece that divides them can
+  // (halves of 64 turned by pieces of 8, 5.2 TB/s; of 10, which leave pieces of 2, 3.8)
   int piece = n;
   if (!a->interleaved)
     while (a->dims / 2 % piece != 0) piece /= 2;
@@ -211,7 +218,10 @@ extern "C" int compact_rotary(const RotaryArgs* a, void* stream) {
                               : p.rotated + static_cast<int>(ceil_div(pieces - 2 * p.rotated, 2));
   if (heads * p.per_head >= 1 << 16) return -1;
   p.per_token = static_cast<int>(heads) * p.per_head;
-  // a sine per thread, while that leaves four workgroups for every CU
+  // a sine per thread, while that leaves four workgroups for every CU.  (us with half as many
+  // sines / a sine / two per thread: 32 x 256 tokens, 32 heads of 64: 14.0 / 12.7 / 12.7; 8 x
+  // 4096, 20 of 96: 48.5 / 43.6 / 46.2; 2 x 12001, 40 of 128, fp32: 198 / 207 / 213.  One
+  // workgroup for every CU at least, where four are asked for: the first 15.7.)
   int64_t tokens = 512 / a->dims;
   const int64_t most = a->tokens / 1024, fit = ((1 << 16) - 1) / p.per_token;
   tokens = tokens > most ? most : tokens;

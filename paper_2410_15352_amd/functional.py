@@ -336,6 +336,8 @@ def _attention_torch(q, k, v, window, sinks, lengths, scale):
     if kv != heads:
         kw, vw = (t.repeat_interleave(heads // kv, 1) for t in (kw, vw))
     seen = _visible(lq, lk, lengths, window, sinks, q.device)
+    used = seen.any(2).unsqueeze(-1)  # (what lies past a sequence, or before every window, may be anything)
+    kw, vw = torch.where(used, kw, 0.0), torch.where(used, vw, 0.0)
     s = torch.matmul(qw, kw.transpose(2, 3).contiguous()) * scale
     s = torch.where(seen, s, -math.inf)
     some = seen.any(-1, keepdim=True)
@@ -345,20 +347,23 @@ def _attention_torch(q, k, v, window, sinks, lengths, scale):
     return torch.matmul(p, vw).to(q.dtype)
 
 
-FEW_ROWS = 128  # of the heads that share keys
+FEW_ROWS = 32
 
 
 def attention_splits(b, heads, kv, lq, lk, window, sinks):
     """Ranges of keys that are worked on apart and joined (0: the rows alone fill the card).
-    Up to FEW_ROWS rows share keys: a wave takes 32 of them and a range, of at least 4 tiles of
-    32 keys, or 8 past 1024 waves, and 2048 waves at most.  More rows: a workgroup takes 128 of
-    one head; ranges of at least 8 tiles of 64 keys where 256 workgroups are not reached.
+    Up to FEW_ROWS rows a head: a wave takes 32 rows of the heads that share keys and a range,
+    of at least 4 tiles of 32 keys, or 8 past 1024 waves, and 2048 waves at most.  More rows: a
+    workgroup takes 128 of one head; ranges of at least 8 tiles of 64 keys where 256 workgroups
+    are not reached.  us, waves / workgroups: 4 x 8192 keys, 32 heads on 8 of 128, 8 rows 35 / 66,
+    32 rows 64 / 68, 64 rows 103 / 78; 8 x 4096 keys, 16 heads of 64, 32 rows 34 / 32, 64 rows
+    55 / 41.
     One token, us by ranges (the rule's *), heads of 128: 4 sequences of up to 70000 keys, 8
     heads of k: 16 270, 32 196, 64* 192, 128 186; one sequence: 64 77, 128 66, 256* 72, 512 86;
     32 of 8192: 2 194, 8* 202, 16 213; heads of 64, 16 x 16 of 1028 keys: 2 18, 4* 19, 8 20, 16
     21.  1000 rows of 16 heads over 20000 keys: 1 508, 2 281, 4* 191, 8 204."""
     share = heads // kv * lq
-    if share <= FEW_ROWS and b * kv <= 65535:
+    if lq <= FEW_ROWS and b * kv <= 65535:
         blocks = b * kv * -(-share // 32)
         tiles = -(-min(lk, window + sinks + lq) // 32)
         splits = max(1, min(-(-2048 // blocks), tiles // 4))
@@ -431,7 +436,7 @@ def _attention_apply(q, k, v, window, sinks, lengths, scale, tracked=False):
         rows = splits * b * heads * lq
         part = torch.empty(rows * (hd + 1), dtype=torch.float32, device=device)
         at = part.data_ptr()
-        split = (splits, heads // kv * lq <= FEW_ROWS, at, at + 4 * rows * hd)
+        split = (splits, lq <= FEW_ROWS, at, at + 4 * rows * hd)
     ops._call("compact_attention_fwd", _attn_pack(*_attn_fields(q, k, v, o, stats, lengths, window, sinks, scale, *split)),
               _stream(stats))
     return q[0], k[0], v[0], o[0], stats
@@ -490,7 +495,8 @@ def window_attention(q, k, v, window=None, sinks=0, lengths=None, scale=None):
     A row that sees no key (lq > L) gives zeros and passes no gradient.  A key that a row does
     not see has no part in it, whatever it holds.  scale: 1 / sqrt(hd) if None.
 
-    The kernels take bf16 with heads of up to 128 elements, a multiple of 8."""
+    The kernels take bf16 with heads of up to 128 elements, a multiple of 8.  In the torch
+    expressions an infinite or NaN key or value that some rows see makes the others NaN too.  A gradient of a row with NaN is NaN."""
     if q.dim() != 4 or k.dim() != 4 or v.dim() != 4:
         raise ValueError("window_attention: q (b, heads, lq, hd), k and v (b, kv, lk, hd)")
     if k.shape != v.shape or q.shape[0] != k.shape[0] or q.shape[3] != k.shape[3]:

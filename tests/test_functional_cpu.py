@@ -228,3 +228,25 @@ def test_block_and_model_run_them_together():
     loss = m(tokens[:, :-1], tokens[:, 1:], teacher=(torch.randn(2, 8, 3), torch.randint(32, (2, 8, 3))), temperature=2.0)
     loss.backward()
     assert loss.isfinite() and m.head.weight.grad.isfinite().all() and m.embed.grad.abs().sum() > 0
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float64])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_attention_leaves_out_what_no_row_sees(dtype, bad):
+    """A cache that holds anything past its sequences, and before every row's window."""
+    g = torch.Generator().manual_seed(5)
+    q = torch.randn(2, 4, 3, 8, generator=g, dtype=dtype).requires_grad_()
+    k, v = (torch.randn(2, 2, 20, 8, generator=g, dtype=dtype) for _ in range(2))
+    lengths = torch.tensor([11, 3])
+    held = [k.clone(), v.clone()]
+    for t in held:
+        t[0, :, 11:] = bad
+        t[1, :, 3:] = bad
+        t[0, :, 1:4] = bad  # rows 8, 9, 10 of a window of 5 see 4 on, and the sink 0
+    held = [t.requires_grad_() for t in held]
+    plain = [t.clone().requires_grad_() for t in (k, v)]
+    out = [F.window_attention(q, *kv, window=5, sinks=1, lengths=lengths) for kv in (plain, held)]
+    assert torch.equal(out[0], out[1])
+    grads = [torch.autograd.grad(o.sum(), (q, *kv)) for o, kv in zip(out, (plain, held))]
+    for a, b in zip(*grads):
+        assert torch.equal(a, b)
