@@ -15,7 +15,7 @@
 // gradient's.  The gradient is formed where the loss is, for dloss = 1; the backward runs
 // the same kernel again, which ends at once where dloss is 1 indeed.
 //
-// Measured, loss and gradient in bf16: 8192 rows of 32000 logits 286 us, 3.7 TB/s, at T = 2 with
+// Measured, loss and gradient in bf16: 8192 rows of 32000 logits 275 us, 3.8 TB/s, at T = 2 with
 // targets (two exponentials per logit and walk), 243 us, 4.3 TB/s, at T = 1; 4096 rows of 131072
 // without targets 508 us, 4.2 TB/s; a large copy reaches 5.2 TB/s.  Of it 12 us are the entries'
 // kernel and 5 the mean's.  Rows of a thousand logits are bound by a row's chain of walks and
@@ -234,7 +234,8 @@ __global__ __launch_bounds__(THREADS, 4) void k_distill(DistillArgs a) {
     const R r(row, a.V);
     const bool now = live;
     const int64_t aim = target;
-    float m = xe, lT = 0.0f, l1 = 0.0f, gT = 0.0f, g1 = 0.0f, xv = 0.0f;
+    // gT, g1: the factors of the two softmaxes' gradients, gT / sT and g1 / s1 their exponentials'
+    float m = now ? xe : 0.0f, gT = 0.0f, g1 = 0.0f, eT = 0.0f, e1 = 0.0f, xv = 0.0f;
     if (now) {
       // logits that the entries and the target name, on their way while the row is walked
       if (entry.x >= 0) xv = r.one(a.x, entry.x);
@@ -266,7 +267,7 @@ __global__ __launch_bounds__(THREADS, 4) void k_distill(DistillArgs a) {
       m = wave_max(smax[lane & (NW - 1)]);
       m = uniform(m == ninf ? 0.0f : m);
       // sums of 2^(cT (x - m)), of the same at temperature 1, and of the entries' p (x - m) / T
-      float s1 = __builtin_amdgcn_exp2f((xe - m) * kLog2e), sT = __builtin_amdgcn_exp2f((xe - m) * cT), sx = 0.0f;
+      float sT = __builtin_amdgcn_exp2f((xe - m) * cT), s1 = __builtin_amdgcn_exp2f((xe - m) * kLog2e), sx = 0.0f;
       walk([&](const u32x4& c) {
 #pragma unroll
         for (int e = 0; e < N; ++e) {
@@ -297,36 +298,38 @@ __global__ __launch_bounds__(THREADS, 4) void k_distill(DistillArgs a) {
       sT = wave_sum(lane < NW ? ssum[lane & (NW - 1)][0] : 0.0f);
       s1 = TWO ? wave_sum(lane < NW ? ssum[lane & (NW - 1)][1] : 0.0f) : sT;
       sx = a.loss_row != nullptr ? wave_sum(lane < NW ? ssum[lane & (NW - 1)][2] : 0.0f) : 0.0f;
-      // log q_v = (x_v - m) / T - lT
-      lT = uniform(logf(sT));
-      l1 = TWO ? uniform(logf(s1)) : lT;
-      if (a.loss_row != nullptr && tid == 0) {
-        float loss = soft ? w * T * T * (h + lT - sx) : 0.0f;
-        if (HARD) loss += (1.0f - w) * (l1 - (xt - m));
+      if (a.loss_row != nullptr && tid == 0) {  // log q_v = (x_v - m) / T - log sT
+        float loss = soft ? w * T * T * (h + logf(sT) - sx) : 0.0f;
+        if (HARD) loss += (1.0f - w) * (logf(TWO ? s1 : sT) - (xt - m));
         a.loss_row[row] = h != h ? nan : loss;
       }
       gT = h != h ? nan : soft ? scale * w * T : 0.0f;
       g1 = HARD ? scale * (1.0f - w) : 0.0f;
+      // (not in the exponents: an addition and a selection less for each logit, 275 us for 286)
+      eT = uniform(gT == 0.0f ? 0.0f : gT / sT);
+      e1 = uniform(g1 == 0.0f ? 0.0f : g1 / (TWO ? s1 : sT));
     } else if (a.loss_row != nullptr && tid == 0) {
       a.loss_row[row] = 0.0f;
     }
-    // gradient of a logit without its teacher's or target's part
-    const float oT = lT * kLog2e, o1 = l1 * kLog2e;
+    // gradient of a logit without its teacher's or target's part (a row without any part has
+    // none, whatever its logits are)
+    const bool none = gT == 0.0f && g1 == 0.0f;
     auto base = [&](float v) {
-      const float d = v - m;
-      if constexpr (!TWO) return part(gT + g1, __builtin_amdgcn_exp2f(__builtin_fmaf(d, cT, -oT)));
-      return part(gT, __builtin_amdgcn_exp2f(__builtin_fmaf(d, cT, -oT))) +
-             part(g1, __builtin_amdgcn_exp2f(__builtin_fmaf(d, kLog2e, -o1)));
+      const float d = v - m, u = __builtin_amdgcn_exp2f(d * cT);
+      if constexpr (TWO) return __builtin_fmaf(eT, u, e1 * __builtin_amdgcn_exp2f(d * kLog2e));
+      else return u * (eT + e1);
     };
     auto grad = [&](const u32x4& c, int skip) {
-      float g[N];
+      float g[N] = {};
+      if (!none) {
 #pragma unroll
-      for (int e = 0; e < N; ++e) g[e] = base(R::value(c, e));
+        for (int e = 0; e < N; ++e) g[e] = base(R::value(c, e));
+      }
       r.store(a.dx, skip, tid, g);
     };
     const int2 named = entry;
     if (a.dx != nullptr) {
-      if (r.end_of(tid) >= 0) r.put(a.dx, r.end_of(tid), base(xe));
+      if (r.end_of(tid) >= 0) r.put(a.dx, r.end_of(tid), none ? 0.0f : base(xe));
 #pragma unroll 1
       for (int c = THREADS * NC; c + tid < r.chunks; c += THREADS) grad(r.load(a.x, true, c, tid), c);
     }
@@ -344,7 +347,7 @@ __global__ __launch_bounds__(THREADS, 4) void k_distill(DistillArgs a) {
     // the entries and the target, over what the walk wrote
     __syncthreads();
     auto fix = [&](const int2& n, float v) {
-      float g = base(v) - part(gT, __int_as_float(n.y));
+      float g = (none ? 0.0f : base(v)) - part(gT, __int_as_float(n.y));
       if (HARD && n.x == aim) g -= g1;
       r.put(a.dx, n.x, g);
     };
@@ -391,11 +394,11 @@ void launch(const DistillArgs& a, hipStream_t s) {
   // The smallest workgroup whose registers hold a row, or all but the last 3% of it.  us by
   // threads x chunks, loss and gradient in bf16 at T = 2 (the rule's *):
   //             256 x 1  256 x 4  256 x 16  512 x 16  1024 x 16
-  //   16384 x   1000  83*     146      429       838      1656
-  //    8192 x   8000 104       90*     224       425       838
-  //    8192 x  32001 344      330      282*      441       839
-  //    2048 x  65536 200      194      182       151*      233
-  //    1024 x 200000 365      361      337       290       260*
+  //   16384 x   1000  84*     140      402       784      1540
+  //    8192 x   8000 103       89*     211       399       782
+  //    8192 x  32001 345      328      275*      419       786
+  //    2048 x  65536 197      189      179       150*      224
+  //    1024 x 200000 357      352      329       286       260*
   const int64_t chunks = a.V / (F32 ? 4 : 8);
   if (chunks <= 256) launch_row<F32, 256, 1>(a, s);
   else if (chunks <= 1024) launch_row<F32, 256, 4>(a, s);

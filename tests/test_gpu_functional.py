@@ -570,3 +570,28 @@ def test_other_streams_and_graphs():
         for a, r in zip(out, ref):
             assert torch.equal(a, r)
         step()
+
+
+@pytest.mark.parametrize("rows,V,K,dtype", [(9, 1001, 64, torch.bfloat16), (20, 32000, 64, torch.bfloat16),
+                                            (8, 20001, 9, torch.float32), (6, 70001, 16, torch.bfloat16)])
+@pytest.mark.parametrize("T", [2.0, 4.0, 5.0])
+@pytest.mark.parametrize("w", [0.0, 0.75, 1.0])
+def test_distill_temperatures(rows, V, K, dtype, T, w):
+    x, top, ids, t = _distill_inputs(rows, V, K, dtype)
+    x.requires_grad_(True)
+    loss = F.distill_loss(x, top, ids, targets=t, temperature=T, weight=w)
+    (g,) = torch.autograd.grad(loss, x)
+    _distill_check(x, top, ids, t, T, w, loss, g)
+
+
+@pytest.mark.parametrize("T", [1.0, 2.0, 4.0, 5.0])
+def test_distill_rows_without_a_part(T):
+    """No entry and no weight on the targets: no gradient, whatever the logits are."""
+    x, top, ids, t = _distill_inputs(9, 1001, 8, torch.bfloat16)
+    with torch.no_grad():
+        x[2, :3] = torch.tensor([math.nan, math.inf, -math.inf], device=dev())  # (row 2 has no entry)
+    x.requires_grad_(True)
+    for targets in (None, t):
+        loss = F.distill_loss(x, top, ids, targets=targets, temperature=T, weight=1.0)
+        (g,) = torch.autograd.grad(loss, x)
+        assert loss.isfinite() and g.isfinite().all() and torch.equal(g[2], torch.zeros_like(g[2]))
