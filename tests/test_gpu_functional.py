@@ -595,3 +595,30 @@ def test_distill_rows_without_a_part(T):
         loss = F.distill_loss(x, top, ids, targets=targets, temperature=T, weight=1.0)
         (g,) = torch.autograd.grad(loss, x)
         assert loss.isfinite() and g.isfinite().all() and torch.equal(g[2], torch.zeros_like(g[2]))
+
+
+@pytest.mark.parametrize("case", [
+    # b, heads, kv, l, hd, window, sinks: rows that see more than 512 keys, several blocks of sinks, shared heads
+    (1, 4, 2, 1500, 128, 700, 140), (1, 2, 2, 1400, 64, 600, 70), (2, 5, 1, 1289, 88, 640, 129),
+    (1, 3, 3, 700, 104, None, 0), (3, 4, 1, 515, 120, 513, 1), (1, 16, 16, 2047, 112, 31, 260)], ids=str)
+def test_attention_gradients_of_long_windows(case):
+    b, heads, kv, l, hd, window, sinks = case
+    q = _rand(b, heads, l, hd, seed=1).requires_grad_(True)
+    k, v = (_rand(b, kv, l, hd, seed=s).requires_grad_(True) for s in (2, 3))
+    do = _rand(b, heads, l, hd, seed=4)
+    o = F.window_attention(q, k, v, window=window, sinks=sinks)
+    grads = torch.autograd.grad(o, (q, k, v), do, retain_graph=True)
+    _check((o, *grads), q, k, v, do, window, sinks, None, hd ** -0.5)
+    for x, y in zip(grads, torch.autograd.grad(o, (q, k, v), do)):
+        assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("lq", [31, 32, 33, 64])
+def test_attention_between_the_forms(lq):
+    """Rows of a head on both sides of the limit between waves and workgroups, many heads to a key head."""
+    q, do = _rand(2, 12, lq, 64, seed=1), _rand(2, 12, lq, 64, seed=4)
+    k, v = (_rand(2, 2, 900, 64, seed=s) for s in (2, 3))
+    lengths = torch.tensor([900, 20], device=dev())
+    for rule in (dict(), dict(window=100, sinks=5)):
+        o = F.window_attention(q, k, v, lengths=lengths, **rule)
+        _check((o,), q, k, v, do, rule.get("window"), rule.get("sinks", 0), lengths, 64 ** -0.5, "o")
