@@ -449,6 +449,7 @@ class _AttentionFn(torch.autograd.Function):
     def forward(ctx, q, k, v, window, sinks, lengths, scale):
         kept = _attention_apply(q, k, v, window, sinks, lengths, scale, tracked=True)
         ctx.rule = window, sinks, scale
+        ctx.shapes = kept[0].shape, kept[1].shape
         ctx.save_for_backward(*kept, lengths)
         return kept[3]
 
@@ -457,11 +458,14 @@ class _AttentionFn(torch.autograd.Function):
         q, k, v, o, stats, lengths = ctx.saved_tensors
         window, sinks, scale = ctx.rule
         none = None, None, None, None
-        shape = q.shape
+        shape, kv_shape = ctx.shapes
         if (torch.is_grad_enabled() or not _eager() or not _here(do)
                 or not ops._companion(stats, torch.float32, _stats_count(shape, True))
-                or not all(t.dtype is _bf16 and _here(t) for t in (q, k, v, o))):
+                or lengths is not None and not ops._companion(lengths, torch.int32, shape[0])
+                or not all(t.dtype is _bf16 and t.shape == s and _here(t)
+                           for t, s in ((q, shape), (k, kv_shape), (v, kv_shape), (o, shape)))):
             recorded = torch.is_grad_enabled()
+            lengths = lengths if lengths is None else lengths.to(q.device)
             with torch.enable_grad():
                 leaves = [x if recorded and x.requires_grad else x.detach().requires_grad_(True) for x in (q, k, v)]
                 y = _attention_torch(*leaves, window, sinks, lengths, scale)
@@ -594,6 +598,7 @@ class _DistillFn(torch.autograd.Function):
         ctx.dx = torch.empty_like(logits)
         ctx.scratch = _distill_call(logits, top, ids, targets, None, temperature, weight, loss=loss, dx=ctx.dx)
         ctx.rule = temperature, weight
+        ctx.size = logits.dtype, logits.shape, top.shape
         ctx.save_for_backward(logits, top, ids, targets)
         return loss
 
@@ -601,7 +606,11 @@ class _DistillFn(torch.autograd.Function):
     def backward(ctx, dloss):
         logits, top, ids, targets = ctx.saved_tensors
         rule = ctx.rule
-        if torch.is_grad_enabled() or not _eager() or not _plain(dloss) or not _distill_usable(logits, top, ids, targets):
+        # (the gradient's buffer and the scratch are of the forward's types and sizes)
+        if (torch.is_grad_enabled() or not _eager() or not _plain(dloss) or not _distill_usable(logits, top, ids, targets)
+                or (logits.dtype, logits.shape, top.shape) != ctx.size
+                or targets is not None and not ops._companion(targets, torch.int64, len(logits))):
+            targets = targets if targets is None else targets.to(torch.int64)
             return (ops._torch_grad(lambda t: _distill_torch(t, top, ids, targets, *rule), logits, dloss),
                     None, None, None, None, None)
         dx, ctx.dx = ctx.dx, None

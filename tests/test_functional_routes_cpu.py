@@ -1,0 +1,88 @@
+"""Which form of rotary positions, attention and distillation answers, and what its backward
+keeps, without a GPU: the kernels' routes run on CPU tensors with launches that are noted
+instead of made, so a kernel's results are unwritten memory and only the rest is looked at."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+F = pytest.importorskip("paper_2410_15352_amd.functional")
+
+bf16, f32, f64 = torch.bfloat16, torch.float32, torch.float64
+
+
+def _rand(*shape, seed=0, dtype=bf16):
+    return torch.randn(*shape, generator=torch.Generator().manual_seed(seed + sum(shape))).to(dtype)
+
+
+@pytest.fixture
+def launches(monkeypatch):
+    """Entry points called, in order."""
+    names = []
+    monkeypatch.setattr(F, "_here", F._plain)
+    monkeypatch.setattr(F, "_stream", lambda t: 0)
+    monkeypatch.setattr(F.ops, "_call", lambda name, *args: names.append(name))
+    monkeypatch.setattr(F.ops, "_companion", lambda t, dtype, count: (
+        t.dtype == dtype and t.numel() == count and F._plain(t) and t.is_contiguous()))
+    monkeypatch.setattr(F, "_attn_scratch", lambda block: 0)
+    return names
+
+
+# --------------------- saved tensors from a hook -----------------------------
+
+def _attention_with_hook(unpack):
+    q, k, v = (_rand(2, 2, 5, 8, seed=s).requires_grad_() for s in (1, 2, 3))
+    do = _rand(2, 2, 5, 8, seed=4)
+    lengths = torch.tensor([5, 3], dtype=torch.int32)
+    rule = dict(window=3, sinks=1, lengths=lengths)
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: t, unpack):
+        o = F.window_attention(q, k, v, **rule)
+    grads = torch.autograd.grad(o, (q, k, v), do)
+    wide = [t.detach().to(f64).requires_grad_() for t in (q, k, v)]
+    expect = torch.autograd.grad(F.window_attention(*wide, **rule), wide, do.to(f64))
+    return grads, expect
+
+
+def test_attention_saved_tensors_as_they_were(launches):
+    _attention_with_hook(lambda t: t)
+    assert launches == ["compact_attention_fwd", "compact_attention_bwd"]
+
+
+@pytest.mark.parametrize("unpack", [
+    lambda t: t.long() if t.dtype == torch.int32 else t,           # lengths of another type
+    lambda t: torch.stack((t, t), 1)[:, 0] if t.dtype == torch.int32 else t,  # not dense
+    lambda t: t.float() if t.dtype == bf16 else t])
+def test_attention_saved_tensors_changed_by_a_hook(launches, unpack):
+    """The kernel would read lengths as int32 from a pointer of the GPU's: it must not run on others."""
+    grads, expect = _attention_with_hook(unpack)
+    assert launches == ["compact_attention_fwd"]
+    for g, e in zip(grads, expect):
+        assert g.dtype == bf16 and (g.double() - e).abs().max() <= 2.0 ** -7 * e.abs().max()
+
+
+def _distill_with_hook(unpack, dtype=bf16):
+    x, top = _rand(4, 24, seed=1, dtype=dtype).requires_grad_(), _rand(4, 3, seed=2)
+    ids, targets = torch.arange(12).view(4, 3), torch.tensor([0, -100, 5, 23])
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: t, unpack):
+        loss = F._DistillFn.apply(x, top, ids, targets, 2.0, 0.5)
+    (g,) = torch.autograd.grad(loss, x, torch.tensor(3.0))
+    wide = x.detach().double().requires_grad_()
+    (e,) = torch.autograd.grad(F.distill_loss(wide, top.double(), ids, targets=targets, temperature=2.0, weight=0.5), wide,
+                               torch.tensor(3.0, dtype=f64))
+    return g, e
+
+
+def test_distill_saved_tensors_as_they_were(launches):
+    _distill_with_hook(lambda t: t)
+    assert launches == ["compact_distill"] * 2
+
+
+@pytest.mark.parametrize("unpack", [
+    lambda t: t.float() if t.shape == (4, 24) else t,               # logits of a wider type than the gradient's buffer
+    lambda t: t.int() if t.shape == (4,) else t,                    # targets read as int64
+    lambda t: torch.stack((t, t), -1)[..., 0] if t.shape == (4,) else t])
+def test_distill_saved_tensors_changed_by_a_hook(launches, unpack):
+    """The gradient's buffer is of the forward's type and size: no kernel writes it for others."""
+    g, e = _distill_with_hook(unpack)
+    assert launches == ["compact_distill"]
+    assert g.dtype in (bf16, f32) and (g.double() - e).abs().max() <= 2.0 ** -7 * e.abs().max()
