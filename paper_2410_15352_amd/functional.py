@@ -14,6 +14,7 @@ function, and so does a backward that is itself recorded or batched.  Arguments 
 takes are refused with ValueError or TypeError."""
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 import struct
@@ -325,8 +326,20 @@ def _visible(lq, lk, lengths, window, sinks, device):
     return seen.unsqueeze(1)
 
 
+def _as_typed(t):
+    """Outside autocast: products in the types that they are given."""
+    kind = t.device.type
+    return torch.autocast(kind, enabled=False) if kind in ("cuda", "cpu") else contextlib.nullcontext()
+
+
 def _attention_torch(q, k, v, window, sinks, lengths, scale):
-    """The attention as torch expressions, in fp32 (fp64 for fp64)."""
+    """The attention as torch expressions, in fp32 (fp64 for fp64).  (Autocast would make its
+    products bf16 ones, of batches with a transposed operand in the backward.)"""
+    with _as_typed(q):
+        return _attention_expressions(q, k, v, window, sinks, lengths, scale)
+
+
+def _attention_expressions(q, k, v, window, sinks, lengths, scale):
     b, heads, lq, hd = q.shape
     kv, lk = k.shape[1:3]
     wide = torch.float64 if q.dtype == torch.float64 else torch.float32

@@ -86,3 +86,22 @@ def test_distill_saved_tensors_changed_by_a_hook(launches, unpack):
     g, e = _distill_with_hook(unpack)
     assert launches == ["compact_distill"]
     assert g.dtype in (bf16, f32) and (g.double() - e).abs().max() <= 2.0 ** -7 * e.abs().max()
+
+
+# ------------------------------- autocast ------------------------------------
+
+def test_attention_under_autocast_stays_in_32_bits():
+    """The torch expressions' products are fp32 ones, forward and backward, whatever autocast makes of products."""
+    t = [_rand(2, 4, 9, 8, seed=s, dtype=f32).requires_grad_() for s in (1, 2, 3)]
+    do = _rand(2, 4, 9, 8, seed=4, dtype=f32)
+    plain = F.window_attention(*t, window=4, sinks=1)
+    with torch.autocast("cpu", dtype=bf16):
+        o = F.window_attention(*t, window=4, sinks=1)
+    assert o.dtype == f32 and torch.equal(o, plain)
+    for a, b in zip(torch.autograd.grad(o, t, do), torch.autograd.grad(plain, t, do)):
+        assert torch.equal(a, b)
+
+
+def test_attention_of_tensors_without_storage():
+    q = torch.empty(1, 2, 5, 8, device="meta")
+    assert F.window_attention(q, q, q, window=3).shape == q.shape
