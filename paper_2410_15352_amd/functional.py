@@ -113,7 +113,8 @@ class Rotary(torch.nn.Module):
                 values are multiplied by 0.1 ln(factor) + 1 (in q and in k)
 
     rope(q, k, positions=...) rotates q (b, l, heads, hd) and, if given, k (b, l, kv, hd);
-    positions: None (0, 1, ...), an int (the first one's), or integers of shape (l,) or (b, l).
+    positions: None (0, 1, ...), an int (the first one's), or integers of shape (l,) or (b, l),
+    which the backward reads again: written in between, autograd refuses it.
     No parameters; the angles are exact for any position (fp64)."""
 
     def __init__(self, dims, base=10000.0, layout="half", scaling="none", factor=1.0, original_length=2048, low=1.0,
@@ -240,12 +241,30 @@ def _rotary_torch(rope, positions, inverse, *tensors):
     return tuple(out)
 
 
+def _save_positions(ctx, positions):
+    """A tensor as autograd keeps them: written again before the backward, it is refused there."""
+    if isinstance(positions, torch.Tensor):
+        ctx.positions = positions.dtype, positions.shape
+        ctx.save_for_backward(positions)
+    else:
+        ctx.positions = positions
+
+
+def _saved_positions(ctx, x):
+    """(a saved-tensor hook may have given them another type, place or shape)"""
+    if not isinstance(ctx.positions, tuple):
+        return ctx.positions
+    (positions,), (dtype, shape) = ctx.saved_tensors, ctx.positions
+    return positions.to(x.device, dtype).reshape(shape)
+
+
 class _RotaryFn(torch.autograd.Function):
     """q and k turned; nothing is kept but the positions."""
 
     @staticmethod
     def forward(ctx, rope, positions, q, k):
-        ctx.rope, ctx.positions, ctx.pair = rope, positions, k is not None
+        ctx.rope, ctx.pair = rope, k is not None
+        _save_positions(ctx, positions)
         ctx.set_materialize_grads(False)
         out = _rotary_apply(rope, positions, 0, q, k)
         return tuple(out) if ctx.pair else (out[0], None)
@@ -255,10 +274,11 @@ class _RotaryFn(torch.autograd.Function):
         given = [t for t in (dq, dk) if t is not None]
         if not given:
             return None, None, None, None
-        if torch.is_grad_enabled() or not ctx.rope._usable(given[0], given[-1], ctx.positions):
-            out = iter(_rotary_torch(ctx.rope, ctx.positions, True, *given))
+        positions = _saved_positions(ctx, given[0])
+        if torch.is_grad_enabled() or not ctx.rope._usable(given[0], given[-1], positions):
+            out = iter(_rotary_torch(ctx.rope, positions, True, *given))
         else:
-            out = iter(_rotary_apply(ctx.rope, ctx.positions, 1, *given))
+            out = iter(_rotary_apply(ctx.rope, positions, 1, *given))
         dq, dk = (None if t is None else next(out) for t in (dq, dk))
         return None, None, dq, dk
 
@@ -269,7 +289,8 @@ class _RotaryQkvFn(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, rope, positions, qkv):
-        ctx.rope, ctx.positions, ctx.shape = rope, positions, qkv.shape
+        ctx.rope, ctx.shape = rope, qkv.shape
+        _save_positions(ctx, positions)
         ctx.set_materialize_grads(False)
         q, k, v = qkv.unbind(2)
         _rotary_call(rope, positions, 0, q, [x for t in (q, k) for x in (t.data_ptr(), t.data_ptr(), *_strides(t), *_strides(t),
@@ -284,12 +305,13 @@ class _RotaryQkvFn(torch.autograd.Function):
             return None, None, None
         grads = [torch.zeros_like(some) if g is None else g for g in grads]
         dq, dk, dv = (g.transpose(1, 2) for g in grads)
-        if torch.is_grad_enabled() or not _here(dv) or not ctx.rope._usable(dq, dk, ctx.positions):
-            dq, dk = _rotary_torch(ctx.rope, ctx.positions, True, dq, dk)
+        positions = _saved_positions(ctx, dv)
+        if torch.is_grad_enabled() or not _here(dv) or not ctx.rope._usable(dq, dk, positions):
+            dq, dk = _rotary_torch(ctx.rope, positions, True, dq, dk)
             return None, None, torch.stack((dq, dk, dv), 2)
         out = torch.empty(ctx.shape, dtype=dq.dtype, device=dq.device)
         rows = [_rows(g) for g in (dq, dk, dv)]
-        _rotary_call(ctx.rope, ctx.positions, 1, rows[0][0],
+        _rotary_call(ctx.rope, positions, 1, rows[0][0],
                      [x for (g, s), to, rotate in zip(rows, out.unbind(2), (1, 1, 0))
                       for x in (g.data_ptr(), to.data_ptr(), *s, *_strides(to), g.shape[2], rotate)], 3)
         return None, None, out

@@ -105,3 +105,63 @@ def test_attention_under_autocast_stays_in_32_bits():
 def test_attention_of_tensors_without_storage():
     q = torch.empty(1, 2, 5, 8, device="meta")
     assert F.window_attention(q, q, q, window=3).shape == q.shape
+
+
+# ------------------------------- rotary --------------------------------------
+
+@pytest.fixture
+def turned_by_kernels(monkeypatch):
+    """Rotary's kernel route, its launches made by the torch expressions."""
+    monkeypatch.setattr(F, "_here", F._plain)
+    monkeypatch.setattr(F, "_rotary_apply", lambda rope, positions, inverse, *t: [
+        y for y in F._rotary_torch(rope, positions, bool(inverse), *t) if y is not None])
+
+    def call(rope, positions, inverse, x, fields, count):  # in place, of qkv's q and k
+        calls.append((positions, inverse))
+    calls = []
+    monkeypatch.setattr(F, "_rotary_call", call)
+    return calls
+
+
+def _rotary_step(kind, positions):
+    """(gradient, its inputs) of one rotation with the given positions, as a function that runs the backward."""
+    rope = F.Rotary(8)
+    if kind == "in place":
+        qkv = _rand(2, 4, 3, 2, 8, seed=1, dtype=f32).requires_grad_()
+        out = F.rotary_split_qkv(qkv * 1, rope, positions=positions)
+        return lambda: torch.autograd.grad(sum(t.sum() for t in out), qkv)
+    q, k = (_rand(2, 4, 2, 8, seed=s, dtype=f32).requires_grad_() for s in (1, 2))
+    if kind == "q":
+        y = rope(q, positions=positions)
+        return lambda: torch.autograd.grad(y, q, torch.ones_like(y))
+    y = rope(q, k, positions=positions)
+    return lambda: torch.autograd.grad(y, (q, k), [torch.ones_like(x) for x in y])
+
+
+@pytest.mark.parametrize("kind", ["q", "q and k", "in place"])
+def test_rotary_positions_written_before_the_backward(turned_by_kernels, kind):
+    """A buffer of positions that moved on: the angles of the forward are gone, and autograd says so."""
+    positions = torch.arange(4)
+    back = _rotary_step(kind, positions)
+    back()
+    back = _rotary_step(kind, positions)
+    positions += 4
+    with pytest.raises(RuntimeError, match="inplace operation"):
+        back()
+
+
+@pytest.mark.parametrize("kind", ["q", "q and k", "in place"])
+def test_rotary_positions_through_saved_tensor_hooks(turned_by_kernels, kind):
+    """Positions that come back in another type turn back by the same angles."""
+    positions = torch.tensor([[3, 1, 4, 1], [5, 9, 2, 6]])
+    plain = _rotary_step(kind, positions)()
+    if kind == "in place":
+        assert torch.equal(turned_by_kernels[-1][0], positions)
+    packed = []
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: packed.append(t) or t.to(torch.int16), lambda t: t):
+        back = _rotary_step(kind, positions)
+    assert any(t is positions or torch.equal(t, positions) for t in packed)
+    for a, b in zip(back(), plain):
+        assert kind == "in place" or torch.equal(a, b)
+    if kind == "in place":
+        assert turned_by_kernels[-1][0].dtype == positions.dtype and torch.equal(turned_by_kernels[-1][0], positions)
