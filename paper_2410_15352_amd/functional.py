@@ -502,7 +502,8 @@ class _AttentionFn(torch.autograd.Function):
             recorded = torch.is_grad_enabled()
             lengths = lengths if lengths is None else lengths.to(q.device)
             with torch.enable_grad():
-                leaves = [x if recorded and x.requires_grad else x.detach().requires_grad_(True) for x in (q, k, v)]
+                # (aliases: of v = f(k), k's own gradient must not hold what reaches k through v)
+                leaves = [x.view_as(x) if recorded and x.requires_grad else x.detach().requires_grad_(True) for x in (q, k, v)]
                 y = _attention_torch(*leaves, window, sinks, lengths, scale)
                 return (*torch.autograd.grad(y, leaves, do, create_graph=recorded), *none)
         do = _attn_tensor(do if do.dtype is _bf16 else do.to(_bf16))

@@ -165,3 +165,38 @@ def test_rotary_positions_through_saved_tensor_hooks(turned_by_kernels, kind):
         assert kind == "in place" or torch.equal(a, b)
     if kind == "in place":
         assert turned_by_kernels[-1][0].dtype == positions.dtype and torch.equal(turned_by_kernels[-1][0], positions)
+
+
+# --------------------- recorded backwards of attention -----------------------
+
+RULE = dict(window=3, sinks=1)
+
+
+def _recorded(make, dtype):
+    """First and second derivatives by x of attention whose q, k and v are make(x); bf16 takes the kernels' route."""
+    x = _rand(3, 1, 2, 6, 8, seed=5).to(dtype).requires_grad_()
+    do = _rand(1, 2, 6, 8, seed=6).to(dtype)
+    q, k, v = make(x)
+    o = F.window_attention(q, k, v, **RULE)
+    leaves = [x, *(t for t in (q, k, v) if t is not x)]
+    first = torch.autograd.grad(o, leaves, do, create_graph=True)
+    (second,) = torch.autograd.grad(first[0].double().square().sum(), x)
+    return [*first, second]
+
+
+DEPENDENT = {
+    "separate": lambda x: (x[0], x[1], x[2]),
+    "v is k": lambda x: (lambda k: (x[0], k, k))(x[1] * 1),
+    "v from k": lambda x: (lambda k: (x[0], k, 2 * k))(x[1] * 1),
+    "q, k and v are one": lambda x: (lambda t: (t, t, t))(x[0] * 1),
+    "q from v from k": lambda x: (lambda k: (lambda v: (v + x[0], k, v))(k * x[2]))(x[1] * 1),
+}
+
+
+@pytest.mark.parametrize("name", list(DEPENDENT))
+def test_recorded_backward_of_inputs_that_depend_on_one_another(launches, name):
+    got, ref = _recorded(DEPENDENT[name], bf16), _recorded(DEPENDENT[name], f64)
+    assert launches == ["compact_attention_fwd"]
+    for a, b in zip(got, ref):
+        # bf16 results of a few roundings each
+        assert (a.double() - b).norm() <= 2.0 ** -5 * b.norm()
