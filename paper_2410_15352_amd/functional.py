@@ -458,8 +458,7 @@ _fns = {}
 
 
 def _attention_apply(q, k, v, window, sinks, lengths, scale, tracked=False):
-    """(q, k, v as the kernels take them, o, the statistics that a backward wants)"""
-    q, k, v = _attn_tensor(q), _attn_tensor(k), _attn_tensor(v)
+    """q, k, v: as _attn_tensor gives them; (o, the statistics that a backward wants)"""
     shape, device = q[0].shape, q[0].device
     b, heads, lq, hd = shape
     _, kv, lk, _ = k[0].shape
@@ -474,25 +473,26 @@ def _attention_apply(q, k, v, window, sinks, lengths, scale, tracked=False):
         split = (splits, lq <= FEW_ROWS, at, at + 4 * rows * hd)
     ops._call("compact_attention_fwd", _attn_pack(*_attn_fields(q, k, v, o, stats, lengths, window, sinks, scale, *split)),
               _stream(stats))
-    return q[0], k[0], v[0], o[0], stats
+    return o[0], stats
 
 
 class _AttentionFn(torch.autograd.Function):
-    """Keeps q, k, v, o, and beside o one fp32 number a row and a byte an element."""
+    """Keeps q, k, v, o, and beside o one fp32 number a row and a byte an element.  Its q, k and v
+    lie as the kernels take them: a copy made in here would have no history for a recorded backward."""
 
     @staticmethod
-    def forward(ctx, q, k, v, window, sinks, lengths, scale):
-        kept = _attention_apply(q, k, v, window, sinks, lengths, scale, tracked=True)
+    def forward(ctx, q, k, v, strides, window, sinks, lengths, scale):
+        o, stats = _attention_apply(*zip((q, k, v), strides), window, sinks, lengths, scale, tracked=True)
         ctx.rule = window, sinks, scale
-        ctx.shapes = kept[0].shape, kept[1].shape
-        ctx.save_for_backward(*kept, lengths)
-        return kept[3]
+        ctx.shapes = q.shape, k.shape
+        ctx.save_for_backward(q, k, v, o, stats, lengths)
+        return o
 
     @staticmethod
     def backward(ctx, do):
         q, k, v, o, stats, lengths = ctx.saved_tensors
         window, sinks, scale = ctx.rule
-        none = None, None, None, None
+        none = (None,) * 5
         shape, kv_shape = ctx.shapes
         if (torch.is_grad_enabled() or not _eager() or not _here(do)
                 or not ops._companion(stats, torch.float32, _stats_count(shape, True))
@@ -556,9 +556,10 @@ def window_attention(q, k, v, window=None, sinks=0, lengths=None, scale=None):
     if _eager() and _attention_usable(q, k, v):
         if lengths is not None:
             lengths = lengths.to(torch.int32).contiguous()
-        if _tracked(q, k, v):
-            return _AttentionFn.apply(q, k, v, window, sinks, lengths, scale)
-        return _attention_apply(q, k, v, window, sinks, lengths, scale)[3]
+        q, k, v = _attn_tensor(q), _attn_tensor(k), _attn_tensor(v)
+        if _tracked(q[0], k[0], v[0]):
+            return _AttentionFn.apply(q[0], k[0], v[0], (q[1], k[1], v[1]), window, sinks, lengths, scale)
+        return _attention_apply(q, k, v, window, sinks, lengths, scale)[0]
     return _attention_torch(q, k, v, window, sinks, lengths, scale)
 
 

@@ -200,3 +200,21 @@ def test_recorded_backward_of_inputs_that_depend_on_one_another(launches, name):
     for a, b in zip(got, ref):
         # bf16 results of a few roundings each
         assert (a.double() - b).norm() <= 2.0 ** -5 * b.norm()
+
+
+COPIED = {
+    "q off the 16-byte boundary": lambda x: (torch.nn.functional.pad(x[0].reshape(-1), (1, 0))[1:].view(x[0].shape), x[1], x[2]),
+    "q's rows 12 apart": lambda x: (torch.nn.functional.pad(x[0], (0, 4))[..., :8], x[1], x[2]),
+    "k's last dimension strided": lambda x: (x[0], x[1].transpose(2, 3).contiguous().transpose(2, 3), x[2]),
+    "v's rows on one another": lambda x: (x[0], x[1], x[2].reshape(-1).as_strided((1, 2, 6, 8), (96, 48, 4, 1))),
+}
+
+
+@pytest.mark.parametrize("name", list(COPIED))
+def test_recorded_backward_of_inputs_that_are_copied(launches, name):
+    """The kernels read a dense, aligned copy: its history reaches the second derivatives."""
+    assert any(F._attn_tensor(t)[0] is not t for t in COPIED[name](_rand(3, 1, 2, 6, 8)))
+    got, ref = _recorded(COPIED[name], bf16), _recorded(COPIED[name], f64)
+    assert launches == ["compact_attention_fwd"]
+    for a, b in zip(got, ref):
+        assert (a.double() - b).norm() <= 2.0 ** -5 * b.norm()
