@@ -48,6 +48,7 @@ ops._SIGNATURES.update({
 
 _TYPES = ops._TYPES
 _device_now = torch._C._cuda_getDevice
+_is_compiling = torch.compiler.is_compiling
 
 
 def _here(t):
@@ -131,13 +132,25 @@ class Rotary(torch.nn.Module):
         self.dims, self.interleaved = dims, layout == "interleaved"
         f, self.magnitude = _rotary_frequencies(dims, float(base), scaling, float(factor), original_length, low, high)
         # (not a buffer: module.to(dtype) must not round it)
-        self._turns = {torch.device("cpu"): torch.tensor([x / (2 * math.pi) for x in f], dtype=torch.float64)}
+        self._revolutions = [x / (2 * math.pi) for x in f]
+        self._turns = {}  # by device
 
     def turns(self, device):
-        """Revolutions per position of each pair, fp64."""
-        t = self._turns.get(device)
-        if t is None:
-            t = self._turns[device] = self._turns[torch.device("cpu")].to(device)
+        """Revolutions per position of each pair, fp64; kept for the device, but for what a
+        transform or a tracer makes of them."""
+        t = self._turns.get(device) if _eager() else None
+        if t is not None:
+            return t
+        if device.type == "cuda" and not _is_compiling() and torch.cuda.is_current_stream_capturing():
+            # a copy from the host is not captured; these are part of the graph and hold nothing before its replay
+            t = torch.empty(len(self._revolutions), dtype=torch.float64, device=device)
+            for i, x in enumerate(self._revolutions):
+                t[i].fill_(x)
+            return t
+        with torch.inference_mode(False) if torch.is_inference_mode_enabled() else contextlib.nullcontext():
+            t = torch.tensor(self._revolutions, dtype=torch.float64, device=device)
+        if _eager() and _plain(t):
+            self._turns[device] = t
         return t
 
     def forward(self, q, k=None, positions=None):
@@ -194,8 +207,10 @@ def _rotary_call(rope, positions, inverse, x, fields, count):
         pos_b, pos_l = (0, *positions.stride()) if positions.dim() == 1 else positions.stride()
     else:
         offset = positions or 0
+    turns = rope._turns.get(x.device)
+    turns = rope.turns(x.device) if turns is None else turns
     ops._call("compact_rotary",
-              _ROTARY(*fields, *_NO_TENSOR * (3 - count), rope.turns(x.device).data_ptr(), at, pos_b, pos_l, offset, b * l, l,
+              _ROTARY(*fields, *_NO_TENSOR * (3 - count), turns.data_ptr(), at, pos_b, pos_l, offset, b * l, l,
                       hd, rope.dims, count, rope.interleaved, inverse, pos32, x.dtype == torch.float32, rope.magnitude),
               _stream(x))
 

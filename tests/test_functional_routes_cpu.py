@@ -218,3 +218,57 @@ def test_recorded_backward_of_inputs_that_are_copied(launches, name):
     assert launches == ["compact_attention_fwd"]
     for a, b in zip(got, ref):
         assert (a.double() - b).norm() <= 2.0 ** -5 * b.norm()
+
+
+# ------------------------- a Rotary's frequencies -----------------------------
+
+def _fake_rotation(rope):
+    from torch._subclasses.fake_tensor import FakeTensorMode
+    with FakeTensorMode():
+        assert rope(torch.zeros(1, 2, 1, 8)).shape == (1, 2, 1, 8)
+
+
+def _traced_rotation(rope):
+    from torch.fx.experimental.proxy_tensor import make_fx
+    x = _rand(1, 2, 1, 8, dtype=f32)
+    assert torch.equal(make_fx(rope, tracing_mode="fake")(x)(x), F.Rotary(8)(x))
+
+
+FIRST_USES = {
+    "func.grad": lambda rope: torch.func.grad(lambda q: rope(q).sum())(_rand(1, 2, 1, 8, dtype=f32)),
+    "vmap": lambda rope: torch.func.vmap(rope)(_rand(3, 1, 2, 1, 8, dtype=f32)),
+    "fake tensors": _fake_rotation,
+    "make_fx": _traced_rotation,
+    "inference": lambda rope: torch.inference_mode()(rope)(_rand(1, 2, 1, 8, dtype=f32)),
+    "meta": lambda rope: rope(torch.zeros(1, 2, 1, 8, device="meta")),
+}
+
+
+@pytest.mark.parametrize("name", list(FIRST_USES))
+def test_rotary_first_used_under_a_transform(name):
+    """What a transform makes of the frequencies is not kept for later calls."""
+    rope = F.Rotary(8)
+    # (a device's copy as on a GPU: none yet)
+    rope._turns.clear()
+    FIRST_USES[name](rope)
+    turns = rope.turns(torch.device("cpu"))
+    assert type(turns) is torch.Tensor and turns.data_ptr() != 0 and not turns.is_inference()
+    assert torch.equal(turns, F.Rotary(8).turns(torch.device("cpu")))
+    x = _rand(1, 2, 1, 8, dtype=f32)
+    assert torch.equal(rope(x), F.Rotary(8)(x))
+
+
+def test_rotary_made_under_another_device():
+    with torch.device("meta"):
+        rope = F.Rotary(8)
+    x = _rand(1, 2, 1, 8, dtype=f32)
+    assert torch.equal(rope(x), F.Rotary(8)(x))
+
+
+def test_rotary_copied_and_saved():
+    import copy
+    import pickle
+    rope = F.Rotary(8, scaling="linear", factor=2.0)
+    x = _rand(1, 2, 1, 8, dtype=f32)
+    for other in (copy.deepcopy(rope), pickle.loads(pickle.dumps(rope))):
+        assert torch.equal(other(x), rope(x))
