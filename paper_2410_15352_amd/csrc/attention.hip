@@ -1097,6 +1097,13 @@ __global__ __launch_bounds__(256) void k_attn_dkv_sum(AttnGradArgs ga) {
   *reinterpret_cast<u32x2*>(out) = w;
 }
 
+// Far workgroups are 1024 at most, or one to a block of sinks: a chunk costs a slot in fp32 for each
+// sink.  us (MB of scratch beside the gradients) without a limit / 2048 / 1024 / 512: 4 x 16384 rows, 16
+// heads of 64, window 1024, 4 sinks 1493 (6) / 1483 (6) / 1477 (2) / 1465; 1024 sinks 3146 (2046) /
+// 2443 (167) / 2470 (100) / 2472; 16384 rows, window 128, 4096 sinks 1996 (2183) / 1200 (168) / 1244
+// (101) / 1245; 16 heads on 4 of 128, window 4096, 4096 sinks 3219 (220) / 3223 / 3156 (153) / 3227.
+constexpr int64_t kFarWork = 1024;
+
 // How the gradients of k and v are split (AttnGradArgs), and the floats of `part`.
 // parts: 512 workgroups (two per CU) of at least 8 tiles where the blocks of keys are fewer.
 // chunks: a far workgroup walks a quarter of a near one's tiles, at least 8.
@@ -1121,9 +1128,10 @@ int64_t plan_dkv(AttnGradArgs* g) {
   g->chunks = 0;
   if (far) {
     const int64_t far_rows = a.lk - a.window < a.lq ? a.lk - a.window : a.lq, far_tiles = G * ceil_div(far_rows, kBN);
-    const int64_t own = ceil_div(tiles, 4 * parts);
+    const int64_t own = ceil_div(tiles, 4 * parts), most = ceil_div(kFarWork, bk * ceil_div(g->far_keys, far_block(a.hd)));
     int64_t chunks = ceil_div(far_tiles, own < 8 ? 8 : own);
-    g->chunks = static_cast<int>(chunks > 64 ? 64 : chunks);
+    chunks = chunks > 64 ? 64 : chunks;
+    g->chunks = static_cast<int>(chunks > most ? most : chunks);
   }
   return 2 * a.hd * bk * (parts * g->near_keys + far_slots(a.hd) * int64_t(g->chunks) * g->far_keys);
 }

@@ -571,6 +571,8 @@ def window_attention(q, k, v, window=None, sinks=0, lengths=None, scale=None):
     if _eager() and _attention_usable(q, k, v):
         if lengths is not None:
             lengths = lengths.to(torch.int32).contiguous()
+        if window is not None and window + sinks >= k.shape[2]:
+            window, sinks = None, 0  # every earlier key is one or the other
         q, k, v = _attn_tensor(q), _attn_tensor(k), _attn_tensor(v)
         if _tracked(q[0], k[0], v[0]):
             return _AttentionFn.apply(q[0], k[0], v[0], (q[1], k[1], v[1]), window, sinks, lengths, scale)

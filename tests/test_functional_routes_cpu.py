@@ -2,6 +2,7 @@
 keeps, without a GPU: the kernels' routes run on CPU tensors with launches that are noted
 instead of made, so a kernel's results are unwritten memory and only the rest is looked at."""
 import math
+import struct
 
 import pytest
 
@@ -272,3 +273,38 @@ def test_rotary_copied_and_saved():
     x = _rand(1, 2, 1, 8, dtype=f32)
     for other in (copy.deepcopy(rope), pickle.loads(pickle.dumps(rope))):
         assert torch.equal(other(x), rope(x))
+
+
+# --------------------------- sizes of a call's plan ---------------------------
+
+def _scratch_bytes(b, heads, kv, l, hd, window, sinks):
+    """The backward's scratch for sums in parts, as the library plans it (no launch)."""
+    lib = pytest.importorskip("paper_2410_15352_amd._lib").load()
+    fn = lib.compact_attention_bwd_scratch
+    fn.restype, fn.argtypes = F._i64, [F._block]
+    rows = (l * hd, hd, hd)
+    floats = fn(F._attn_pack(*(0,) * 7, *rows, *rows, *rows, *rows, b, heads, kv, l, l, hd,
+                             F.NO_WINDOW if window is None else window, sinks, 1.0, 0, 0, 0, 0))
+    return 4 * floats
+
+
+@pytest.mark.parametrize("b,heads,kv,l,hd", [(4, 16, 16, 16384, 64), (1, 16, 16, 16384, 64), (1, 16, 4, 16384, 128),
+                                             (1, 1, 1, 65536, 64), (2, 4, 1, 70000, 96), (64, 8, 8, 4096, 32)])
+@pytest.mark.parametrize("window", [128, 1024])
+def test_attention_scratch_is_bounded(b, heads, kv, l, hd, window):
+    """However many sinks: two slots and the window's own of dk and dv in fp32 for each sink (6 times
+    k's and v's bytes if all are sinks), or those of 1024 workgroups of 128 keys."""
+    for sinks in (1, 4, 64, 1000, 4096, l // 2, l - window - 1):
+        assert 0 <= _scratch_bytes(b, heads, kv, l, hd, window, sinks) <= (
+            6 * 4 * b * kv * l * hd + 2 * 4 * 2 * hd * 1024 * 128)
+
+
+def test_attention_of_sinks_that_reach_the_window(launches, monkeypatch):
+    """Window and sinks that cover a sequence are no window: no sums in parts for the sinks."""
+    blocks = []
+    monkeypatch.setattr(F.ops, "_call", lambda name, block, stream: blocks.append(block))
+    q, k, v = (_rand(1, 2, 100, 8, seed=s) for s in (1, 2, 3))
+    for window, sinks, expect in ((30, 70, (F.NO_WINDOW, 0)), (30, 1000, (F.NO_WINDOW, 0)), (30, 69, (30, 69)), (None, 5, (F.NO_WINDOW, 0))):
+        F.window_attention(q, k, v, window=window, sinks=sinks)
+        fields = struct.unpack("@" + F._ATTN, blocks[-1])
+        assert fields[25] == expect[0] and (window is None or fields[26] == expect[1]), (window, sinks)

@@ -10,6 +10,7 @@ pytestmark = pytest.mark.gpu
 
 torch = pytest.importorskip("torch")
 F = pytest.importorskip("paper_2410_15352_amd.functional")
+whole = pytest.importorskip("test_gpu_functional")
 
 
 def _rand(*shape, seed=0, dtype=torch.bfloat16):
@@ -51,3 +52,37 @@ def test_rotary_positions_written_before_the_backward(pair):
     pos += 9
     with pytest.raises(RuntimeError, match="inplace operation"):
         torch.autograd.grad(y, q, y.detach())
+
+
+def _corners(got, q, k, v, do, window, sinks, lengths=None):
+    """The first and the last heads of k against float64, under the bounds of test_gpu_functional."""
+    G = q.shape[1] // k.shape[1]
+    for b, h in ((slice(0, 1), 0), (slice(-1, None), k.shape[1] - 1)):
+        qs, ks = slice(h * G, (h + 1) * G), slice(h, h + 1)
+        part = [t[b, s].detach() for t, s in zip(got, (qs, qs, ks, ks))]
+        whole._check(part, q[b, qs], k[b, ks], v[b, ks], do[b, qs], window, sinks, None if lengths is None else lengths[b],
+                     q.shape[3] ** -0.5, names=" ".join("o dq dk dv".split()[:len(got)]))
+
+
+@pytest.mark.parametrize("b,heads,kv,l,hd,window,sinks", [
+    (16, 16, 16, 700, 64, 31, 300),   # sinks' blocks enough: one workgroup walks all rows past their windows
+    (2, 8, 4, 1300, 128, 40, 257),
+    (3, 4, 4, 900, 32, 100, 799)])    # one key short of all
+def test_attention_gradients_of_many_sinks(b, heads, kv, l, hd, window, sinks):
+    q = _rand(b, heads, l, hd, seed=1).requires_grad_(True)
+    k, v = (_rand(b, kv, l, hd, seed=s).requires_grad_(True) for s in (2, 3))
+    do = _rand(b, heads, l, hd, seed=4)
+    o = F.window_attention(q, k, v, window=window, sinks=sinks)
+    _corners((o, *torch.autograd.grad(o, (q, k, v), do)), q, k, v, do, window, sinks)
+
+
+def test_attention_of_sinks_that_reach_the_window():
+    q, k, v, do = (_rand(2, 2, 300, 64, seed=s) for s in range(4))
+
+    def run(**rule):
+        t = [x.clone().requires_grad_(True) for x in (q, k, v)]
+        o = F.window_attention(*t, **rule)
+        return [o, *torch.autograd.grad(o, t, do)]
+
+    for a, c in zip(run(window=100, sinks=200), run()):
+        assert torch.equal(a, c)
