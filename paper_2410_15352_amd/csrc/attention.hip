@@ -1074,27 +1074,31 @@ __global__ __launch_bounds__(shared_keys(HD) ? 512 : 256, 2) void k_attn_dkv(Att
 }
 
 // The slots' sum of the first near_keys (or, without near parts, far_keys) keys: four columns
-// of dk or dv per thread.
+// of dk or dv per thread at a time.
+constexpr int64_t kSumGrid = int64_t(1) << 20;
+__host__ __device__ inline int64_t dkv_sum_work(const AttnGradArgs& a) { return int64_t(a.f.b) * a.f.kv * a.near_keys * (a.f.hd / 2); }
+
 __global__ __launch_bounds__(256) void k_attn_dkv_sum(AttnGradArgs ga) {
   const AttnArgs& a = ga.f;
   const int cols = 2 * a.hd / 4;
-  const int64_t u = int64_t(blockIdx.x) * 256 + threadIdx.x, bk_all = int64_t(a.b) * a.kv, row = u / cols;
-  const int col = static_cast<int>(u % cols) * 4, j = static_cast<int>(row % ga.near_keys);
-  const int64_t bk = row / ga.near_keys;
-  if (bk >= bk_all) return;
-  f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int p = 0; p < ga.parts; ++p)
-    s += *reinterpret_cast<const f32x4*>(ga.part + ((p * bk_all + bk) * ga.near_keys + j) * 2 * a.hd + col);
-  if (j < ga.far_keys) {
-    const float* far = ga.part + ga.parts * bk_all * ga.near_keys * 2 * a.hd;
-    for (int p = 0; p < far_slots(a.hd) * ga.chunks; ++p)
-      s += *reinterpret_cast<const f32x4*>(far + ((p * bk_all + bk) * ga.far_keys + j) * 2 * a.hd + col);
+  const int64_t work = dkv_sum_work(ga), bk_all = int64_t(a.b) * a.kv;
+  for (int64_t u = int64_t(blockIdx.x) * 256 + threadIdx.x; u < work; u += int64_t(gridDim.x) * 256) {
+    const int64_t row = u / cols, bk = row / ga.near_keys;
+    const int col = static_cast<int>(u % cols) * 4, j = static_cast<int>(row % ga.near_keys);
+    f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int p = 0; p < ga.parts; ++p)
+      s += *reinterpret_cast<const f32x4*>(ga.part + ((p * bk_all + bk) * ga.near_keys + j) * 2 * a.hd + col);
+    if (j < ga.far_keys) {
+      const float* far = ga.part + ga.parts * bk_all * ga.near_keys * 2 * a.hd;
+      for (int p = 0; p < far_slots(a.hd) * ga.chunks; ++p)
+        s += *reinterpret_cast<const f32x4*>(far + ((p * bk_all + bk) * ga.far_keys + j) * 2 * a.hd + col);
+    }
+    const int b = static_cast<int>(bk / a.kv), hk = static_cast<int>(bk % a.kv);
+    uint16_t* out = col < a.hd ? ga.dk + b * ga.dks[0] + hk * ga.dks[1] + j * ga.dks[2] + col
+                               : ga.dv + b * ga.dvs[0] + hk * ga.dvs[1] + j * ga.dvs[2] + col - a.hd;
+    const u32x2 w = {pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3])};
+    *reinterpret_cast<u32x2*>(out) = w;
   }
-  const int b = static_cast<int>(bk / a.kv), hk = static_cast<int>(bk % a.kv);
-  uint16_t* out = col < a.hd ? ga.dk + b * ga.dks[0] + hk * ga.dks[1] + j * ga.dks[2] + col
-                             : ga.dv + b * ga.dvs[0] + hk * ga.dvs[1] + j * ga.dvs[2] + col - a.hd;
-  const u32x2 w = {pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3])};
-  *reinterpret_cast<u32x2*>(out) = w;
 }
 
 // Far workgroups are 1024 at most, or one to a block of sinks: a chunk costs a slot in fp32 for each
@@ -1136,6 +1140,13 @@ int64_t plan_dkv(AttnGradArgs* g) {
   return 2 * a.hd * bk * (parts * g->near_keys + far_slots(a.hd) * int64_t(g->chunks) * g->far_keys);
 }
 
+int64_t dkv_grid(const AttnGradArgs& a) {
+  const int64_t bk = int64_t(a.f.b) * a.f.kv;
+  return round_up(bk * ceil_div(a.f.lk, 128), kNumXcd) * a.parts + bk * ceil_div(a.far_keys, far_block(a.f.hd)) * a.chunks;
+}
+// A launch has under 2^32 threads.
+bool plan_fits(const AttnGradArgs& a) { return dkv_grid(a) * (shared_keys(a.f.hd) ? 512 : 256) < int64_t(1) << 32; }
+
 bool args_ok(const AttnArgs& a) {
   constexpr int64_t most = int64_t(1) << 30;
   if (a.b < 1 || a.heads < 1 || a.kv < 1 || a.heads % a.kv != 0 || a.lq < 1 || a.lk < 1 || a.hd < 8 || a.hd % 8 != 0 ||
@@ -1173,15 +1184,9 @@ void launch_grads(const AttnGradArgs& a, bool kv, hipStream_t s) {
   const int grid = a.f.b * a.f.heads * static_cast<int>(ceil_div(a.f.lq, 128));
   hipLaunchKernelGGL((k_attn_dq<HD, FINE>), dim3(grid), dim3(256), 0, s, a);
   if (!kv) return;
-  const int bk = a.f.b * a.f.kv;
-  const int blocks = bk * static_cast<int>(ceil_div(a.f.lk, 128));
-  const int grid_kv = static_cast<int>(ceil_div(blocks, kNumXcd)) * kNumXcd * a.parts +
-                      bk * static_cast<int>(ceil_div(a.far_keys, far_block(HD))) * a.chunks;
-  hipLaunchKernelGGL((k_attn_dkv<HD, FINE>), dim3(grid_kv), dim3(shared_keys(HD) ? 512 : 256), 0, s, a);
-  if (a.near_keys > 0) {
-    const int64_t threads = int64_t(bk) * a.near_keys * (a.f.hd / 2);
-    hipLaunchKernelGGL(k_attn_dkv_sum, dim3(static_cast<uint32_t>(ceil_div(threads, 256))), dim3(256), 0, s, a);
-  }
+  hipLaunchKernelGGL((k_attn_dkv<HD, FINE>), dim3(static_cast<uint32_t>(dkv_grid(a))), dim3(shared_keys(HD) ? 512 : 256), 0, s, a);
+  const int64_t sums = ceil_div(dkv_sum_work(a), 256);
+  if (sums > 0) hipLaunchKernelGGL(k_attn_dkv_sum, dim3(static_cast<uint32_t>(sums < kSumGrid ? sums : kSumGrid)), dim3(256), 0, s, a);
 }
 
 template <int HD>
@@ -1222,7 +1227,8 @@ int64_t compact_attention_bwd_scratch(const AttnArgs* a) {
   if (!args_ok(*a)) return -1;
   AttnGradArgs g = {};
   g.f = *a;
-  return plan_dkv(&g);
+  const int64_t floats = plan_dkv(&g);
+  return plan_fits(g) ? floats : -1;
 }
 
 // dk and dv are left out where dk is NULL.
@@ -1232,7 +1238,8 @@ int compact_attention_bwd(const AttnGradArgs* args, void* stream) {
   if (!args_ok(a->f) || a->f.o_low == nullptr || a->gs[2] < 0 || a->gs[2] > kMaxStride || (a->f.lq > 1 && a->gs[2] < a->f.hd)) return -1;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const bool kv = a->dk != nullptr;
-  if (plan_dkv(&plan) > 0 && kv && a->part == nullptr) return -1;
+  const bool parts = plan_dkv(&plan) > 0;
+  if (kv && ((parts && a->part == nullptr) || !plan_fits(plan))) return -1;
   if (a->f.hd <= 64) launch_bwd<64>(*a, kv, s);
   else if (a->f.hd <= 96) launch_bwd<96>(*a, kv, s);
   else launch_bwd<128>(*a, kv, s);

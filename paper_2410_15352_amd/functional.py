@@ -398,6 +398,7 @@ def _attention_expressions(q, k, v, window, sinks, lengths, scale):
 
 
 FEW_ROWS = 32
+MAX_JOINED = 1 << 24  # rows of a split call: a workgroup of 256 threads joins each
 
 
 def attention_splits(b, heads, kv, lq, lk, window, sinks):
@@ -413,13 +414,14 @@ def attention_splits(b, heads, kv, lq, lk, window, sinks):
     32 of 8192: 2 194, 8* 202, 16 213; heads of 64, 16 x 16 of 1028 keys: 2 18, 4* 19, 8 20, 16
     21.  1000 rows of 16 heads over 20000 keys: 1 508, 2 281, 4* 191, 8 204."""
     share = heads // kv * lq
-    if lq <= FEW_ROWS and b * kv <= 65535:
+    rows = b * heads * lq
+    if lq <= FEW_ROWS and b * kv <= 65535 and share <= 32 * 65535 and rows < MAX_JOINED:
         blocks = b * kv * -(-share // 32)
         tiles = -(-min(lk, window + sinks + lq) // 32)
         splits = max(1, min(-(-2048 // blocks), tiles // 4))
         return splits if blocks * splits <= 1024 else min(splits, max(-(-1024 // blocks), tiles // 8))
     blocks = b * heads * -(-lq // 128)
-    if blocks >= 256 or b * heads * lq >= 1 << 24:
+    if blocks >= 256 or rows >= MAX_JOINED:
         return 0
     splits = min(512 // blocks, -(-min(lk, window + sinks + 128) // 64) // 8)
     return splits if splits > 1 else 0
@@ -568,7 +570,7 @@ def window_attention(q, k, v, window=None, sinks=0, lengths=None, scale=None):
     scale = q.shape[3] ** -0.5 if scale is None else float(scale)
     if not (scale > 0 and math.isfinite(scale)):
         raise ValueError("window_attention: scale > 0")
-    if _eager() and _attention_usable(q, k, v):
+    if _eager() and _attention_usable(q, k, v, _tracked(q, k, v)):
         if lengths is not None:
             lengths = lengths.to(torch.int32).contiguous()
         if window is not None and window + sinks >= k.shape[2]:
@@ -580,9 +582,12 @@ def window_attention(q, k, v, window=None, sinks=0, lengths=None, scale=None):
     return _attention_torch(q, k, v, window, sinks, lengths, scale)
 
 
-def _attention_usable(q, k, v):
+def _attention_usable(q, k, v, tracked):
     b, heads, lq, hd = q.shape
     kv, lk = k.shape[1:3]
+    # a launch has under 2^32 threads; dk and dv take a workgroup for 128 keys and up to two for 128 sinks
+    if tracked and 4 * b * kv * -(-lk // 128) * (512 if hd > 96 else 256) >= 1 << 32:
+        return False
     return (q.dtype == _bf16 and hd % 8 == 0 and 8 <= hd <= MAX_HD and min(b, lq, lk) > 0 and max(lq, lk) <= 1 << 30
             and b * heads * -(-lq // 32) < 1 << 24 and b * kv * -(-lk // 32) < 1 << 24
             and _here(q) and _here(k) and _here(v))

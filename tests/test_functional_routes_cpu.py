@@ -308,3 +308,53 @@ def test_attention_of_sinks_that_reach_the_window(launches, monkeypatch):
         F.window_attention(q, k, v, window=window, sinks=sinks)
         fields = struct.unpack("@" + F._ATTN, blocks[-1])
         assert fields[25] == expect[0] and (window is None or fields[26] == expect[1]), (window, sinks)
+
+
+def _limits():
+    """Sizes around the limits of a call's launches: (b, heads, kv, lq, lk, hd)."""
+    for kv in (1, 8, 128):
+        for G in (1, 16, 1 << 12, 1 << 17):
+            for lq in (1, 31, 32, 33, 128, 4096):
+                for rows in (1 << 18, 1 << 21, 1 << 22, 1 << 23, (1 << 24) - 1, 1 << 24, 1 << 28, (1 << 29) - 64):
+                    for b in {max(1, rows // (kv * G * lq)), max(1, rows // (kv * G * lq) - 1), max(1, rows // (kv * G))}:
+                        for lk in (1, 32, 4096, 70000):
+                            for hd in (8, 128):
+                                yield b, kv * G, kv, lq, lk, hd
+
+
+def test_attention_calls_that_are_taken_are_launched(monkeypatch):
+    """What _attention_usable lets through, the entry points take: their limits on a launch's grid."""
+    monkeypatch.setattr(F, "_here", lambda t: True)
+    taken = 0
+    for b, heads, kv, lq, lk, hd in _limits():
+        q, k = (torch.empty(1, dtype=bf16).expand(b, n, l, hd) for n, l in ((heads, lq), (kv, lk)))
+        for window, sinks in ((F.NO_WINDOW, 0), (7, 3), (7, max(0, lk - 8))):
+            if F._attention_usable(q, k, k, False):
+                taken += 1
+                rows = b * heads * lq
+                splits = F.attention_splits(b, heads, kv, lq, lk, window, sinks)
+                few = lq <= F.FEW_ROWS
+                assert 0 <= splits <= 4096
+                if splits > 0:
+                    assert rows < 1 << 24 and b * heads * -(-lq // 128) * splits < 1 << 31
+                    assert not few or b * kv <= 65535 and -(-(heads // kv * lq) // 32) <= 65535
+                if splits == 0 or not few:
+                    assert b * heads * -(-lq // 128) * max(1, splits) * 256 < 1 << 32
+            if F._attention_usable(q, k, k, True):
+                assert _scratch_bytes_of(b, heads, kv, lq, lk, hd, window, sinks) >= 0, (b, heads, kv, lq, lk, hd, window, sinks)
+    assert taken > 500
+
+
+def _scratch_bytes_of(b, heads, kv, lq, lk, hd, window, sinks):
+    lib = pytest.importorskip("paper_2410_15352_amd._lib").load()
+    fn = lib.compact_attention_bwd_scratch
+    fn.restype, fn.argtypes = F._i64, [F._block]
+    rows = (lk * hd, hd, hd)
+    return fn(F._attn_pack(*(0,) * 7, *rows, *rows, *rows, *rows, b, heads, kv, lq, lk, hd, window, sinks, 1.0, 0, 0, 0, 0))
+
+
+def test_attention_plans_that_pass_a_launch_are_refused():
+    """128 columns of dk and dv: 512 threads for 128 keys."""
+    assert _scratch_bytes_of(1 << 20, 8, 8, 1, 32, 128, F.NO_WINDOW, 0) < 0
+    assert _scratch_bytes_of(1 << 20, 8, 8, 1, 32, 64, F.NO_WINDOW, 0) >= 0
+    assert _scratch_bytes_of(1 << 18, 8, 8, 1, 32, 128, F.NO_WINDOW, 0) >= 0

@@ -86,3 +86,13 @@ def test_attention_of_sinks_that_reach_the_window():
 
     for a, c in zip(run(window=100, sinks=200), run()):
         assert torch.equal(a, c)
+
+
+def test_attention_of_very_many_short_sequences():
+    """2^24 rows of 32 to a head: more than are joined, no ranges of keys then."""
+    b, heads, kv, l, hd = 4096, 128, 8, 32, 8
+    q = _rand(b, heads, l, hd, seed=1).requires_grad_(True)
+    k, v = (_rand(b, kv, l, hd, seed=s).requires_grad_(True) for s in (2, 3))
+    do = _rand(b, heads, l, hd, seed=4)
+    o = F.window_attention(q, k, v, window=9, sinks=1)
+    _corners((o, *torch.autograd.grad(o, (q, k, v), do)), q, k, v, do, 9, 1)
