@@ -481,7 +481,9 @@ __device__ __forceinline__ bool attn_fwd(const AttnArgs& a, TilePair<HD>& even, 
   if (mode == kPlain && __syncthreads_or(not_finite(sm.o))) return false;
   const float l = halves_sum(sm.l);
   if (row >= a.lq) return true;
-  const bool empty = sm.m == -__builtin_inff() && l == 0.0f;
+  // no key in this split, which weighs nothing then; without splits: none for the row, which is
+  // before its sequence (of scores that are all -inf the softmax is NaN)
+  const bool empty = a.splits > 0 ? sm.m == -__builtin_inff() && l == 0.0f : p < 0;
   const float f = empty ? 0.0f : 1.0f / l;
   if (a.splits > 0) {
     const int64_t rows = int64_t(a.b) * a.heads * a.lq, at = split * rows + int64_t(bh) * a.lq + row;
@@ -651,8 +653,9 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
   __syncthreads();
   m = red[0];
   for (int w = 1; w < 4; ++w) m = red[w] > m || red[w] != red[w] ? red[w] : m;
-  const bool empty = m == -__builtin_inff();
-  const float shift = empty ? 0.0f : m;
+  const int bh = static_cast<int>(row / a.lq), i = static_cast<int>(row % a.lq);
+  const bool empty = i + length_of(a, bh / a.heads) - a.lq < 0;  // (of scores that are all -inf the softmax is NaN)
+  const float shift = m == -__builtin_inff() ? 0.0f : m;
   float l = 0.0f;
   f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
   const int c = 4 * lane;
@@ -675,7 +678,6 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
     l += weights[g];
   }
   const float f = empty ? 0.0f : 1.0f / l;
-  const int bh = static_cast<int>(row / a.lq), i = static_cast<int>(row % a.lq);
   if (c < a.hd) {
     const float v[4] = {o[0] * f, o[1] * f, o[2] * f, o[3] * f};
     const u32x2 w = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};

@@ -96,3 +96,38 @@ def test_attention_of_very_many_short_sequences():
     do = _rand(b, heads, l, hd, seed=4)
     o = F.window_attention(q, k, v, window=9, sinks=1)
     _corners((o, *torch.autograd.grad(o, (q, k, v), do)), q, k, v, do, 9, 1)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_attention_rows_whose_scores_are_all_minus_infinity(monkeypatch, hd):
+    """What a row sees propagates: the softmax of nothing but -inf is NaN.  A row that sees no key is zero."""
+    b, h, l, window = 2, 2, 200, 4
+    q, do = _rand(b, h, l, hd, seed=1).abs() + 0.5, _rand(b, h, l, hd, seed=2)
+    k, v = _rand(b, h, l, hd, seed=3), _rand(b, h, l, hd, seed=4)
+    k[:, :, 50:61] = -math.inf
+    k[:, :, 190:] = -math.inf
+    lengths = torch.tensor([l, 40], device=dev())  # the second's first 160 rows see nothing
+    for lq, splits, few in ((l, 0, 0), (l, 3, 0), (l, 70, 0), (3, 1, 128), (3, 2, 128)):
+        monkeypatch.setattr(F, "attention_splits", lambda *a: splits)
+        monkeypatch.setattr(F, "FEW_ROWS", few)
+        qs = q[:, :, -lq:]
+        o = F.window_attention(qs, k, v, window=window, lengths=lengths)
+        expect = F._attention_torch(qs.double(), k.double(), v.double(), window, 0, lengths, hd ** -0.5)
+        assert torch.equal(o.isnan(), expect.isnan())
+        assert bool(o[0, :, -3:].isnan().all()) and (lq < l or bool((o[1, :, :160] == 0).all()))
+        if lq == l:
+            assert o[0, 0, :, 0].isnan().sum() == 8 + 7 and not o[1].isnan().any()
+    monkeypatch.undo()
+    t = [x.clone().requires_grad_(True) for x in (q, k, v)]
+    dq, dk, dv = torch.autograd.grad(F.window_attention(*t, window=window), t, do)
+    rows = torch.zeros(l, dtype=torch.bool, device=dev())
+    rows[53:61], rows[193:] = True, True               # rows of such keys alone
+    touched = torch.zeros_like(rows)
+    touched[50:64], touched[190:] = True, True         # and those that see one of them
+    assert bool(dq[:, :, rows].isnan().all()) and not dq[:, :, ~touched].isnan().any()
+    keys = torch.zeros_like(rows)
+    keys[50:61], keys[190:] = True, True
+    assert bool(dk[:, :, keys].isnan().all()) and bool(dv[:, :, keys].isnan().all())
+    far = ~touched
+    far[47:50], far[187:190] = False, False            # (seen by rows that see such a key)
+    assert not dk[:, :, far].isnan().any() and not dv[:, :, far].isnan().any()
