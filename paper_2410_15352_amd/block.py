@@ -53,6 +53,16 @@ class _RMSNormFn(torch.autograd.Function):
         return dx, dg, None
 
 
+def _runs_alone(m, forward):
+    """Calling this module runs its class's forward, this one, and nothing else: no hook, no
+    other forward in its place, not compiled."""
+    return not (m._forward_hooks or m._forward_pre_hooks or m._backward_hooks or m._backward_pre_hooks
+                or _module._global_forward_hooks or _module._global_forward_pre_hooks
+                or _module._global_backward_hooks or _module._global_backward_pre_hooks
+                or "forward" in vars(m) or type(m).forward is not forward
+                or m._compiled_call_impl is not None)
+
+
 class RMSNorm(torch.nn.Module):
     def __init__(self, d, eps=1e-6, device="cuda"):
         super().__init__()
@@ -65,13 +75,7 @@ class RMSNorm(torch.nn.Module):
         return _RMSNormFn.apply(x, self.weight, self.eps)
 
     def _plain(self):
-        """Calling this module runs the forward above and nothing else: no hook, no
-        other forward in its place, not compiled."""
-        return not (self._forward_hooks or self._forward_pre_hooks or self._backward_hooks or self._backward_pre_hooks
-                    or _module._global_forward_hooks or _module._global_forward_pre_hooks
-                    or _module._global_backward_hooks or _module._global_backward_pre_hooks
-                    or "forward" in vars(self) or type(self).forward is not _RMSNORM_FORWARD
-                    or self._compiled_call_impl is not None)
+        return _runs_alone(self, _RMSNORM_FORWARD)
 
     def with_residual(self, x):
         """(x, norm(x)); the returned x is the one to add to later, so that both
@@ -102,6 +106,10 @@ class DenseLinear(torch.nn.Module):
 
     def forward(self, x):
         return ops.dense(x.reshape(-1, x.shape[-1]), self.weight).reshape(*x.shape[:-1], self.weight.shape[1])
+
+
+# Projections that keep nothing of their output.
+_PROJECTIONS = {CompActGroup: CompActGroup.forward, DenseLinear: DenseLinear.forward}
 
 
 class LlamaBlock(torch.nn.Module):
@@ -150,7 +158,10 @@ class LlamaBlock(torch.nn.Module):
         qkv = self.qkv(h.reshape(b * l, d)).reshape(b, l, 3, self.heads, d // self.heads)
         # (three slices would each scatter into a zero-filled tensor of q|k|v's size
         # in the backward, which are then summed)
-        q, k, v = ops.split_qkv(qkv) if self.rope is None else rotary_split_qkv(qkv, self.rope)
+        if self.rope is None:
+            q, k, v = ops.split_qkv(qkv)
+        else:  # in place, unless someone else may hold the projection's output
+            q, k, v = rotary_split_qkv(qkv, self.rope, in_place=_runs_alone(self.qkv, _PROJECTIONS.get(type(self.qkv))))
         if self.window is not None:
             a = window_attention(q, k, v, window=self.window, sinks=self.sinks)
         else:

@@ -332,11 +332,13 @@ class _RotaryQkvFn(torch.autograd.Function):
         return None, None, out
 
 
-def rotary_split_qkv(qkv, rope, positions=None):
+def rotary_split_qkv(qkv, rope, positions=None, in_place=True):
     """q, k (turned) and v (b, heads, l, hd) of qkv (b, l, 3, heads, hd), which a projection
-    has just written: the kernel turns q and k where they stand, so the block keeps no more
-    than without positions."""
+    has just written: in_place, the kernel turns q and k where they stand, so the block keeps no
+    more than without positions."""
     q, k, v = qkv.unbind(2)
+    if not in_place:
+        return tuple(t.transpose(1, 2) for t in (*rope(q, k, positions), v))
     rope._check(q, k, positions)
     if (rope._usable(q, k, positions) and qkv.is_contiguous() and qkv.data_ptr() % 16 == 0
             and not (qkv.is_leaf and qkv.requires_grad)):

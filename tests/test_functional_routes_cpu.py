@@ -358,3 +358,40 @@ def test_attention_plans_that_pass_a_launch_are_refused():
     assert _scratch_bytes_of(1 << 20, 8, 8, 1, 32, 128, F.NO_WINDOW, 0) < 0
     assert _scratch_bytes_of(1 << 20, 8, 8, 1, 32, 64, F.NO_WINDOW, 0) >= 0
     assert _scratch_bytes_of(1 << 18, 8, 8, 1, 32, 128, F.NO_WINDOW, 0) >= 0
+
+
+# --------------------------- the block's projection ---------------------------
+
+def _block():
+    blk = pytest.importorskip("paper_2410_15352_amd.block")
+    torch.manual_seed(0)
+    return blk.LlamaBlock(32, 2, 32, device="cpu", rope=F.Rotary(16), window=4)
+
+
+WATCHED = {
+    "forward hook": lambda b: b.qkv.register_forward_hook(lambda m, x, y: None),
+    "backward hook": lambda b: b.qkv.register_full_backward_hook(lambda m, x, y: None),
+    "hook of all modules": lambda b: torch.nn.modules.module.register_module_forward_hook(lambda m, x, y: None),
+    "forward replaced": lambda b: setattr(b.qkv, "forward", type(b.qkv).forward.__get__(b.qkv)),
+    "module replaced": lambda b: setattr(b, "qkv", torch.nn.Sequential(b.qkv)),
+}
+
+
+@pytest.mark.parametrize("name", list(WATCHED))
+def test_projection_whose_output_may_be_kept_is_not_rotated_in_place(turned_by_kernels, monkeypatch, name):
+    in_place = []
+    monkeypatch.setattr(F, "_rotary_call", lambda *a: in_place.append(a))
+    monkeypatch.setattr(F, "_attention_usable", lambda *a: False)
+    b, x = _block(), _rand(1, 8, 32, seed=1)
+    b(x)
+    assert len(in_place) == 1
+    handle = WATCHED[name](b)
+    try:
+        y = b(x)
+    finally:
+        if handle is not None:
+            handle.remove()
+    assert len(in_place) == 1
+    # (rotated all the same)
+    monkeypatch.setattr(F, "_here", lambda t: False)
+    assert torch.equal(y, b(x))

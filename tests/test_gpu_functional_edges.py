@@ -131,3 +131,18 @@ def test_attention_rows_whose_scores_are_all_minus_infinity(monkeypatch, hd):
     far = ~touched
     far[47:50], far[187:190] = False, False            # (seen by rows that see such a key)
     assert not dk[:, :, far].isnan().any() and not dv[:, :, far].isnan().any()
+
+
+@pytest.mark.parametrize("rank", [None, 16])
+def test_projection_seen_by_a_hook_is_not_rotated(rank):
+    blk = pytest.importorskip("paper_2410_15352_amd.block")
+    torch.manual_seed(0)
+    b = blk.LlamaBlock(128, 2, 256, rank=rank, rope=F.Rotary(64), window=20)
+    x, dy = _rand(2, 100, 128).requires_grad_(True), _rand(2, 100, 128, seed=1)
+    plain = [b(x), *torch.autograd.grad(b(x), x, dy)]
+    kept = []
+    b.qkv.register_forward_hook(lambda m, i, o: kept.append((o, o.detach().clone())))
+    seen = [b(x), *torch.autograd.grad(b(x), x, dy)]
+    assert all(torch.equal(a, c) for a, c in kept)
+    for a, c in zip(seen, plain):
+        assert torch.equal(a, c)
