@@ -180,16 +180,18 @@ class LlamaBlock(torch.nn.Module):
         return [m for m in (self.qkv, self.o, self.gu, self.down) if isinstance(m, CompActGroup)]
 
 
-def block_saved_bytes(b, l, d, heads, ffn, rank=None, rank_down=None, compress_o=False):
+def block_saved_bytes(b, l, d, heads, ffn, rank=None, rank_down=None, compress_o=False, window=None):
     """Table 7 for this block: bytes of the activations one block keeps for
     its backward (bf16 tensors, fp32 inverse RMS and attention log-sum-exp,
-    two int64 scalars of the attention's dropout state).  A CompAct z of r
-    columns is stored with its rows padded to a multiple of 8 elements."""
+    two int64 scalars of the attention's dropout state, or with a window a
+    byte more for each element of x3).  A CompAct z of r columns is stored
+    with its rows padded to a multiple of 8 elements."""
     T = b * l
+    attention = 4 * b * heads * l + 16 if window is None else 4 * ((b * heads * l + 3) // 4 * 4) + T * d
     common = (2 * T * d          # x1
               + 4 * T            # 1 / rms(x1)
               + 2 * T * 3 * d    # q, k, v (one storage)
-              + 4 * b * heads * l + 16
+              + attention
               + 2 * T * d        # x3, also the input of o
               + 2 * T * d + 4 * T  # x5, 1 / rms(x5)
               + 2 * T * 2 * ffn  # x_gate, x_up (one storage)

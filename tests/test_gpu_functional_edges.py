@@ -146,3 +146,16 @@ def test_projection_seen_by_a_hook_is_not_rotated(rank):
     assert all(torch.equal(a, c) for a, c in kept)
     for a, c in zip(seen, plain):
         assert torch.equal(a, c)
+
+
+@pytest.mark.parametrize("l,rope", [(256, True), (256, False), (33, True)])
+def test_block_saved_activations_with_a_window(l, rope):
+    """What the list says a block with windowed attention keeps is what autograd keeps."""
+    nn = pytest.importorskip("test_gpu_nn")
+    blk = nn.blk_mod
+    b, d, heads, ffn = 3, 192, 3, 256
+    for rank in (None, 24):
+        block = blk.LlamaBlock(d, heads, ffn, rank=rank, rope=F.Rotary(64) if rope else None, window=20, sinks=1)
+        x = _rand(b, l, d).requires_grad_(True)
+        block(x).float().sum().backward()
+        assert nn._saved_bytes(block, x)[0] == blk.block_saved_bytes(b, l, d, heads, ffn, rank=rank, window=20)
