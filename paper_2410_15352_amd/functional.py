@@ -383,10 +383,10 @@ def _attention_expressions(q, k, v, window, sinks, lengths, scale):
     kv, lk = k.shape[1:3]
     wide = torch.float64 if q.dtype == torch.float64 else torch.float32
     qw, kw, vw = (t.to(wide) for t in (q, k, v))
-    if lk == 0:
-        return (qw * 0).to(q.dtype)
     if kv != heads:
         kw, vw = (t.repeat_interleave(heads // kv, 1) for t in (kw, vw))
+    if lk == 0:  # (a maximum over nothing is refused; sums over nothing are zero)
+        return torch.matmul(torch.matmul(qw, kw.transpose(2, 3)), vw).to(q.dtype)
     seen = _visible(lq, lk, lengths, window, sinks, q.device)
     used = seen.any(2).unsqueeze(-1)  # (what lies past a sequence, or before every window, may be anything)
     kw, vw = torch.where(used, kw, 0.0), torch.where(used, vw, 0.0)

@@ -395,3 +395,17 @@ def test_projection_whose_output_may_be_kept_is_not_rotated_in_place(turned_by_k
     # (rotated all the same)
     monkeypatch.setattr(F, "_here", lambda t: False)
     assert torch.equal(y, b(x))
+
+
+# ------------------------------- no keys --------------------------------------
+
+@pytest.mark.parametrize("heads,kv", [(2, 2), (4, 2)])
+def test_attention_over_no_keys(heads, kv):
+    """Zeros whatever q holds, and gradients of every input: zeros, and empty ones."""
+    q = torch.full((2, heads, 3, 8), math.nan, dtype=f64).requires_grad_()
+    k, v = (torch.empty(2, kv, 0, 8, dtype=f64).requires_grad_() for _ in range(2))
+    for lengths in (None, torch.zeros(2, dtype=torch.int64)):
+        o = F.window_attention(q, k, v, window=4, lengths=lengths)
+        assert torch.equal(o, torch.zeros_like(o))
+        dq, dk, dv = torch.autograd.grad(o, (q, k, v), torch.ones_like(o))
+        assert torch.equal(dq, torch.zeros_like(dq)) and dk.shape == k.shape and dv.shape == v.shape

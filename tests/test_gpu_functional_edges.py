@@ -159,3 +159,11 @@ def test_block_saved_activations_with_a_window(l, rope):
         x = _rand(b, l, d).requires_grad_(True)
         block(x).float().sum().backward()
         assert nn._saved_bytes(block, x)[0] == blk.block_saved_bytes(b, l, d, heads, ffn, rank=rank, window=20)
+
+
+def test_attention_over_no_keys():
+    q = _rand(2, 4, 3, 64).requires_grad_(True)
+    k, v = (torch.empty(2, 2, 0, 64, dtype=q.dtype, device=dev(), requires_grad=True) for _ in range(2))
+    o = F.window_attention(q, k, v)
+    grads = torch.autograd.grad(o, (q, k, v), torch.ones_like(o))
+    assert not o.any() and not grads[0].any() and grads[1].shape == k.shape and grads[2].shape == v.shape
