@@ -18,6 +18,7 @@ import contextlib
 import ctypes
 import math
 import struct
+from operator import index
 
 import torch
 
@@ -76,6 +77,15 @@ def _rows(t):
     return t, s
 
 
+LEAST_FACTOR = 2.0 ** -60  # of scales and temperatures: their squares and inverses are fp32 numbers
+
+
+def _tensors(what, *given):
+    for t in given:
+        if t is not None and not isinstance(t, torch.Tensor):
+            raise TypeError(f"{what}: tensors")
+
+
 def _tracked(*tensors):
     """A gradient of some tensor is wanted."""
     return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
@@ -97,6 +107,9 @@ def _rotary_frequencies(dims, base, scaling, factor, original_length, low, high)
             return x * (keep + (1 - keep) / factor)
         return [part(x) for x in f], 0.1 * math.log(factor) + 1
     return f, 1.0
+
+
+MAX_POSITION = 1 << 53  # positions are fp64 factors
 
 
 class Rotary(torch.nn.Module):
@@ -127,7 +140,8 @@ class Rotary(torch.nn.Module):
             raise ValueError('rotary layout: "half" or "interleaved"')
         if scaling not in ("none", "linear", "ntk", "parts"):
             raise ValueError('rotary scaling: "none", "linear", "ntk" or "parts"')
-        if not (base > 0 and factor >= 1 and original_length > 0 and high > low) or scaling == "ntk" and dims == 2:
+        if (not (base > 0 and factor >= 1 and original_length > 0 and high > low) or scaling == "ntk" and dims == 2
+                or not all(map(math.isfinite, (base, factor, original_length, low, high)))):
             raise ValueError("rotary: base > 0, factor >= 1, original_length > 0, high > low, and dims > 2 with ntk")
         self.dims, self.interleaved = dims, layout == "interleaved"
         f, self.magnitude = _rotary_frequencies(dims, float(base), scaling, float(factor), original_length, low, high)
@@ -167,6 +181,8 @@ class Rotary(torch.nn.Module):
         for t in (q, k):
             if t is None:
                 continue
+            if not isinstance(t, torch.Tensor):
+                raise TypeError("rotary: q and k are tensors")
             if t.dim() != 4 or t.shape[:2] != q.shape[:2] or t.shape[3] != q.shape[3]:
                 raise ValueError("rotary: q (b, l, heads, hd) and k (b, l, kv, hd)")
             if not t.is_floating_point() or t.dtype != q.dtype or t.device != q.device:
@@ -180,6 +196,8 @@ class Rotary(torch.nn.Module):
                 raise ValueError("rotary positions: shape (l,) or (b, l)")
         elif positions is not None and not isinstance(positions, int):
             raise TypeError("rotary positions: None, an int or a tensor of integers")
+        elif positions is not None and not -MAX_POSITION <= positions <= MAX_POSITION:
+            raise ValueError("rotary positions: within 2^53")
 
     def _usable(self, *tensors_and_positions):
         if not _eager():
@@ -556,14 +574,16 @@ def window_attention(q, k, v, window=None, sinks=0, lengths=None, scale=None):
 
     The kernels take bf16 with heads of up to 128 elements, a multiple of 8.  In the torch
     expressions an infinite or NaN key or value that some rows see makes the others NaN too.  A gradient of a row with NaN is NaN."""
-    if q.dim() != 4 or k.dim() != 4 or v.dim() != 4:
-        raise ValueError("window_attention: q (b, heads, lq, hd), k and v (b, kv, lk, hd)")
+    _tensors("window_attention q, k, v and lengths", q, k, v, lengths)
+    if q.dim() != 4 or k.dim() != 4 or v.dim() != 4 or q.shape[3] == 0:
+        raise ValueError("window_attention: q (b, heads, lq, hd), k and v (b, kv, lk, hd), hd >= 1")
     if k.shape != v.shape or q.shape[0] != k.shape[0] or q.shape[3] != k.shape[3]:
         raise ValueError(f"window_attention: q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}")
     if k.shape[1] == 0 or q.shape[1] % k.shape[1] != 0:
         raise ValueError(f"window_attention: {q.shape[1]} query heads over {k.shape[1]} of k and v")
     if not q.is_floating_point() or q.dtype != k.dtype or q.dtype != v.dtype or not q.device == k.device == v.device:
         raise TypeError("window_attention: q, k and v of one floating type on one device")
+    window, sinks = None if window is None else index(window), index(sinks)
     if window is not None and window < 1 or sinks < 0:
         raise ValueError("window_attention: window >= 1 (or None) and sinks >= 0")
     if lengths is not None:
@@ -572,7 +592,7 @@ def window_attention(q, k, v, window=None, sinks=0, lengths=None, scale=None):
     scale = q.shape[3] ** -0.5 if scale is None else float(scale)
     if not (scale > 0 and math.isfinite(scale)):
         raise ValueError("window_attention: scale > 0")
-    if _eager() and _attention_usable(q, k, v, _tracked(q, k, v)):
+    if _eager() and LEAST_FACTOR < scale < 1 / LEAST_FACTOR and _attention_usable(q, k, v, _tracked(q, k, v)):
         if lengths is not None:
             lengths = lengths.to(torch.int32).contiguous()
         if window is not None and window + sinks >= k.shape[2]:
@@ -688,6 +708,10 @@ def _distill_usable(logits, top, ids, targets):
             and top.stride(1) == 1 and ids.stride(1) == 1 and (targets is None or _here(targets) and targets.is_contiguous()))
 
 
+def _distill_taken(temperature):
+    return LEAST_FACTOR < temperature < 1 / LEAST_FACTOR
+
+
 def distill_loss(logits, top_logits, top_ids, targets=None, temperature=1.0, weight=1.0):
     """The mean over the rows of
 
@@ -700,10 +724,11 @@ def distill_loss(logits, top_logits, top_ids, targets=None, temperature=1.0, wei
     weight < 1.  An id or a target past V makes the loss, and its row's gradient, NaN.
 
     fp32 scalar.  The kernels take dense bf16 or fp32 logits and K up to 1024."""
+    _tensors("distill_loss logits, top_logits, top_ids and targets", logits, top_logits, top_ids, targets)
     if logits.dim() != 2 or top_logits.dim() != 2 or top_logits.shape != top_ids.shape or top_logits.shape[0] != logits.shape[0]:
         raise ValueError("distill_loss: logits (rows, V), top_logits and top_ids (rows, K)")
-    if top_logits.shape[1] < 1:
-        raise ValueError("distill_loss: at least one entry a row")
+    if top_logits.shape[1] < 1 or logits.shape[1] < 1:
+        raise ValueError("distill_loss: at least one logit and one entry a row")
     if not logits.is_floating_point() or not top_logits.is_floating_point() or top_ids.dtype not in (torch.int64, torch.int32):
         raise TypeError("distill_loss: floating logits, int64 or int32 ids")
     if targets is not None and (targets.shape != logits.shape[:1] or targets.dtype != torch.int64):
@@ -715,7 +740,7 @@ def distill_loss(logits, top_logits, top_ids, targets=None, temperature=1.0, wei
         raise ValueError("distill_loss: temperature > 0 and weight in [0, 1]")
     if targets is None and weight != 1:
         raise ValueError("distill_loss: a weight below 1 needs targets")
-    if _eager() and logits.is_cuda:
+    if _eager() and logits.is_cuda and _distill_taken(temperature):
         dense = logits if logits.is_contiguous() else logits.contiguous()
         dense = dense if dense.data_ptr() % 16 == 0 else dense.clone()
         top, ids = (t.detach() if t.stride(1) == 1 else t.detach().contiguous() for t in (top_logits, top_ids))

@@ -409,3 +409,55 @@ def test_attention_over_no_keys(heads, kv):
         assert torch.equal(o, torch.zeros_like(o))
         dq, dk, dv = torch.autograd.grad(o, (q, k, v), torch.ones_like(o))
         assert torch.equal(dq, torch.zeros_like(dq)) and dk.shape == k.shape and dv.shape == v.shape
+
+
+# ------------------------------- refusals -------------------------------------
+
+def _attend(**change):
+    t = dict(q=torch.zeros(2, 2, 3, 8), k=torch.zeros(2, 2, 4, 8), v=torch.zeros(2, 2, 4, 8))
+    return F.window_attention(**{**t, **change})
+
+
+def _distill(**change):
+    t = dict(logits=torch.zeros(2, 4), top_logits=torch.zeros(2, 1), top_ids=torch.zeros(2, 1).long())
+    return F.distill_loss(**{**t, **change})
+
+
+@pytest.mark.parametrize("call", [
+    lambda: _attend(window=2.5), lambda: _attend(window=2, sinks=1.0), lambda: _attend(window="4"), lambda: _attend(lengths=[4, 4]),
+    lambda: _attend(q=[1]), lambda: _distill(targets=[0, 1], weight=0.5), lambda: _distill(top_ids=[[0], [0]]),
+    lambda: F.Rotary(8)([1.0])])
+def test_arguments_of_other_kinds_are_refused(call):
+    with pytest.raises(TypeError):
+        call()
+
+
+@pytest.mark.parametrize("call", [
+    lambda: _attend(q=torch.zeros(2, 2, 3, 0), k=torch.zeros(2, 2, 4, 0), v=torch.zeros(2, 2, 4, 0)),
+    lambda: _distill(logits=torch.zeros(2, 0)), lambda: F.Rotary(8, factor=math.inf), lambda: F.Rotary(8, base=math.inf),
+    lambda: F.Rotary(8, scaling="parts", original_length=math.inf), lambda: F.Rotary(8, high=math.inf),
+    lambda: F.Rotary(8)(torch.zeros(1, 2, 1, 8), positions=1 << 63), lambda: F.Rotary(8)(torch.zeros(1, 2, 1, 8), positions=-1 << 70)])
+def test_values_past_what_is_defined_are_refused(call):
+    with pytest.raises(ValueError):
+        call()
+
+
+def test_arguments_that_stay_allowed():
+    import numpy as np
+    o = _attend(window=np.int64(2), sinks=np.int32(1))
+    assert o.shape == (2, 2, 3, 8)
+    assert F.Rotary(8)(torch.zeros(1, 2, 1, 8), positions=1 << 40).shape == (1, 2, 1, 8)
+    assert _distill(logits=torch.zeros(0, 4), top_logits=torch.zeros(0, 1), top_ids=torch.zeros(0, 1).long()).isnan()
+
+
+def test_factors_past_fp32_are_the_torch_expressions(launches):
+    """The kernels hold scale and temperature in fp32; others are not theirs."""
+    q, k, v = (_rand(1, 2, 5, 8, seed=s) for s in (1, 2, 3))
+    for scale in (1e-45, 1e-60, 1e40):
+        assert F.window_attention(q, k, v, scale=scale).shape == q.shape
+    x, top, ids = _rand(2, 8, dtype=f32), _rand(2, 2, dtype=f32), torch.tensor([[0, 1], [2, 3]])
+    assert not F._distill_taken(1e-45) and not F._distill_taken(1e40) and F._distill_taken(2.0)
+    assert F.distill_loss(x, top, ids, temperature=1e40).dtype == f32
+    assert launches == []
+    F.window_attention(q, k, v, scale=1e-3)
+    assert launches == ["compact_attention_fwd"]
