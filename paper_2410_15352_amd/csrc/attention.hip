@@ -6,7 +6,12 @@
 //   D = sum(do o),  dS = P (do.v - D),  dq = scale dS k,  dk = scale dS^T q,  dv = P^T do.
 //
 // All products run as 32x32x16 bf16 MFMAs with fp32 sums; P and dS are rounded to bf16 as
-// their operands, statistics, sums and accumulators are fp32.
+// their operands, statistics, sums and accumulators are fp32.  P in one bf16 part leaves o and dv,
+// rounded themselves, 1.2 to 1.42 times as far from the exact ones as their own rounding; a second
+// part would cost a third product beside the forward's two.
+//
+// Kernel times below are medians of 100 passes in a row (the first dozen run 10 to 15% longer);
+// comparisons of two forms were timed alone, one after the other.
 //
 // Every product is laid out so that what the softmax yields is the next product's operand
 // as it stands: with keys as rows and queries as columns (S^T = K Q^T) a lane holds 16 of
@@ -385,11 +390,11 @@ struct Softmax {
 // Bound by the latency of a wave's own chain (scores, maximum, exponentials, P V) with two or
 // three waves on a SIMD: at heads of 64 the matrix units work 23 % of the time and the vector
 // units 65 %, at 128 the matrix units 40 %; LDS has no bank conflicts.  Tried and slower: the
-// next tile's scores among this one's exponentials (heads of 64: 125-145 us for 105 at
+// next tile's scores among this one's exponentials (heads of 64: 125-145 us for 105, alone, at
 // 4 x 4096, 16 heads, window 1024; heads of 128: 3-7 % faster, but its two tiles of scores do
 // not fit the registers), 64 columns per wave (no longer two workgroups per CU).
-// Measured: that 105 us, 574 TFLOP/s over the pairs that are seen; 557 us, 865 TFLOP/s, at
-// 16384 rows, 16 heads on 4 of 128, window 4096; 26 us at 3 x 1531 rows, 10 on 2 of 80, window
+// Measured: there 112 us, 540 TFLOP/s over the pairs that are seen; 551 us, 875 TFLOP/s, at
+// 16384 rows, 16 heads on 4 of 128, window 4096; 28 us at 3 x 1531 rows, 10 on 2 of 80, window
 // 301; 19 us at 32 x 256 rows, 8 heads, window 128.  A large matrix product: 1223 TFLOP/s.
 template <int HD>
 struct TilePair {
@@ -692,7 +697,7 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
 // too.  Where the sums are not finite the work is done again with clean values, and NaN in the
 // rows that see a key that had others.
 //
-// Bound as the forward.  Measured: 160 us at 4 x 4096 rows, 16 heads of 64, window 1024; 742 us,
+// Bound as the forward.  Measured: 148 us at 4 x 4096 rows, 16 heads of 64, window 1024; 744 us,
 // 970 TFLOP/s of its three products, at 16384 rows, 16 heads on 4 of 128, window 4096; 24 us at
 // 32 x 256 rows, 8 heads of 64, window 128.  (Three waves to a SIMD at heads of 64, with places
 // in LDS formed for each tile: 352 us with the other gradients for 344.)
@@ -824,7 +829,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnGradArgs ga) {
 //
 // Bound by the chain of one wave (products, exponentials, products) with two to a SIMD, and with
 // 128 columns by LDS too: a step's fragments take 1.5 times as long to read as its products.
-// Measured: 209 us at 4 x 4096 rows, 16 heads of 64, window 1024; 1213 us, 790 TFLOP/s of its four
+// Measured: 194 us at 4 x 4096 rows, 16 heads of 64, window 1024; 1187 us, 810 TFLOP/s of its four
 // products, at 16384 rows, 16 heads on 4 of 128, window 4096; 27 us at 32 x 256 rows, 8 heads of
 // 64, window 128.  Both halves of a tile in one stretch of code were slower (2702 us with the
 // gradient of q for 2580, spilled or at one wave to a SIMD), and so were three waves at heads of

@@ -15,11 +15,12 @@
 // gradient's.  The gradient is formed where the loss is, for dloss = 1; the backward runs
 // the same kernel again, which ends at once where dloss is 1 indeed.
 //
-// Measured, loss and gradient in bf16: 8192 rows of 32000 logits 275 us, 3.8 TB/s, at T = 2 with
-// targets (two exponentials per logit and walk), 243 us, 4.3 TB/s, at T = 1; 4096 rows of 131072
-// without targets 508 us, 4.2 TB/s; a large copy reaches 5.2 TB/s.  Of it 12 us are the entries'
-// kernel and 5 the mean's.  Rows of a thousand logits are bound by a row's chain of walks and
-// barriers: 16384 of them 83 us, 0.8 TB/s.
+// Measured, loss and gradient in bf16 (medians of 100 passes in a row): 8192 rows of 32000 logits
+// 235 us, 4.5 TB/s, at T = 2 with targets (two exponentials per logit and walk), 224 us, 4.7 TB/s, at
+// T = 1; 4096 rows of 131072 without targets 484 us, 4.4 TB/s; a large copy reaches 5.2 TB/s.  Beside
+// them 12 to 15 us of the entries' kernel, 5 of the mean's and 5 of the backward's look at dloss.
+// Rows of a thousand logits are bound by a row's chain of walks and barriers: 16384 of them 56 us,
+// 1.2 TB/s, and 18 for the entries.
 #include <hip/hip_runtime.h>
 
 #include "common.hpp"
@@ -391,7 +392,7 @@ void launch_row(const DistillArgs& a, hipStream_t s) {
 
 template <bool F32>
 void launch(const DistillArgs& a, hipStream_t s) {
-  // The smallest workgroup whose registers hold a row, or all but the last 3% of it.  us by
+  // The smallest workgroup whose registers hold a row, or all but the last 3% of it.  us of whole calls by
   // threads x chunks, loss and gradient in bf16 at T = 2 (the rule's *):
   //             256 x 1  256 x 4  256 x 16  512 x 16  1024 x 16
   //   16384 x   1000  84*     140      402       784      1540

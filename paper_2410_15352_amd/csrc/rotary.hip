@@ -10,8 +10,8 @@
 // exact for any position, where an fp32 product is off by 2^-24 of the angle), and so are the
 // tokens' places in the up to three tensors of a call; then they serve every head.
 //
-// Measured: 12.7 us, 5.3 TB/s, for q and k of 32 x 256 tokens, 16 heads of 64 in bf16; 207 us,
-// 4.75 TB/s, for 2 x 12001 tokens, 32 and 8 heads of 128 in fp32, the first half turned; 3.3 us,
+// Measured: 12.9 us, 5.2 TB/s, for q and k of 32 x 256 tokens, 16 heads of 64 in bf16; 206 us,
+// 4.8 TB/s, for 2 x 12001 tokens, 32 and 8 heads of 128 in fp32, the first half turned; 4.3 us,
 // a launch, for one token of 8 sequences.  (A large copy reaches 5.2 TB/s.)
 #include <hip/hip_runtime.h>
 
@@ -96,6 +96,9 @@ __global__ __launch_bounds__(256) void k_rotary(RotaryArgs a, RotaryPlan pl) {
     }
     const double turn = static_cast<double>(pos) * a.turns[i];
     float s, c;
+    // (the part of a turn is rounded to fp32, off by 2^-26 of a turn at most, 9e-8 radians: fp32
+    // rotations are 1.3 times as far from the exact ones as with the sine of the fp64 angle, which
+    // would cost fp64 polynomials for every pair; bf16 ones as near)
     sincospif(2.0f * static_cast<float>(turn - rint(turn)), &s, &c);
     cs[u] = make_float2(a.magnitude * c, a.magnitude * (a.inverse ? -s : s));
     if (i < a.count) {

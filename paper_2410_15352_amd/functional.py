@@ -423,8 +423,8 @@ MAX_JOINED = 1 << 24  # rows of a split call: a workgroup of 256 threads joins e
 
 def attention_splits(b, heads, kv, lq, lk, window, sinks):
     """Ranges of keys that are worked on apart and joined (0: the rows alone fill the card).
-    Up to FEW_ROWS rows a head: a wave takes 32 rows of the heads that share keys and a range,
-    of at least 4 tiles of 32 keys, or 8 past 1024 waves, and 2048 waves at most.  More rows: a
+    Up to FEW_ROWS rows a head (and MAX_JOINED in all): a wave takes 32 rows of the heads that share keys and
+    a range, of at least 4 tiles of 32 keys, or 8 past 1024 waves, and 2048 waves at most.  More rows: a
     workgroup takes 128 of one head; ranges of at least 8 tiles of 64 keys where 256 workgroups
     are not reached.  us, waves / workgroups: 4 x 8192 keys, 32 heads on 8 of 128, 8 rows 35 / 66,
     32 rows 64 / 68, 64 rows 103 / 78; 8 x 4096 keys, 16 heads of 64, 32 rows 34 / 32, 64 rows
@@ -569,8 +569,9 @@ def window_attention(q, k, v, window=None, sinks=0, lengths=None, scale=None):
     A sequence has L keys: lk, or lengths[b] of them (integers on the device, 0 .. lk; what lies
     past them is not read).  Its rows are its last lq positions: row i stands at p = i + L - lq
     and sees key j when j <= p and (p - j < window or j < sinks); window None: every j <= p.
-    A row that sees no key (lq > L) gives zeros and passes no gradient.  A key that a row does
-    not see has no part in it, whatever it holds.  scale: 1 / sqrt(hd) if None.
+    A row that sees no key (lq > L) gives zeros and passes no gradient; one that sees scores of
+    -inf alone gives NaN.  A key that a row does not see has no part in it, whatever it holds.
+    scale: 1 / sqrt(hd) if None.
 
     The kernels take bf16 with heads of up to 128 elements, a multiple of 8.  In the torch
     expressions an infinite or NaN key or value that some rows see makes the others NaN too.  A gradient of a row with NaN is NaN."""
@@ -671,7 +672,9 @@ def _distill_call(logits, top, ids, targets, scratch, temperature, weight, loss=
 
 class _DistillFn(torch.autograd.Function):
     """The loss, and with it the gradient for dloss = 1, while a row is in registers: the
-    backward finds dloss to be 1 on the GPU and leaves it, or forms it again."""
+    backward finds dloss to be 1 on the GPU and leaves it, or forms it again.  (The gradient is
+    held beside the logits till then, not as a saved tensor: what the backward returns must not
+    be shared.)"""
 
     @staticmethod
     def forward(ctx, logits, top, ids, targets, temperature, weight):
@@ -723,7 +726,9 @@ def distill_loss(logits, top_logits, top_ids, targets=None, temperature=1.0, wei
     part.  With targets (rows,) rows whose target is -100 do not count, and they are needed where
     weight < 1.  An id or a target past V makes the loss, and its row's gradient, NaN.
 
-    fp32 scalar.  The kernels take dense bf16 or fp32 logits and K up to 1024."""
+    fp32 scalar.  The kernels take dense bf16 or fp32 logits and K up to 1024; they form the
+    gradient with the loss and hold it for the backward, as many bytes as the logits.  Of a loss
+    that is multiplied before its backward it is formed a second time there."""
     _tensors("distill_loss logits, top_logits, top_ids and targets", logits, top_logits, top_ids, targets)
     if logits.dim() != 2 or top_logits.dim() != 2 or top_logits.shape != top_ids.shape or top_logits.shape[0] != logits.shape[0]:
         raise ValueError("distill_loss: logits (rows, V), top_logits and top_ids (rows, K)")
