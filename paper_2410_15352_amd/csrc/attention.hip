@@ -85,7 +85,9 @@ struct Tile {
 // form their products plainly and look at their sums at the end, where such a NaN cannot
 // hide; only then they do their work again:
 //   kClean     such values as zeros
-//   kPos, kNeg 1 where the value is +inf or NaN, -inf or NaN, else 0
+//   kPos, kNeg 1 where the value is +inf or NaN, -inf or NaN, else 0; with them the forward reads
+//              keys of zeros, so that it counts those a row sees (a softmax's weights may
+//              underflow, and would lose them)
 enum Values { kPlain, kClean, kPos, kNeg };
 
 __device__ __forceinline__ uint32_t value_pair(uint32_t w, int mode) {
@@ -419,8 +421,9 @@ __device__ __forceinline__ bool attn_fwd(const AttnArgs& a, TilePair<HD>& even, 
   Copy<HD> ck, cv;
   ck.init(a.ks[2], a.hd, tid);
   cv.init(a.vs[2], a.hd, tid);
+  const int Lk = mode >= kPos ? 0 : L;
   auto fetch = [&](int t, TilePair<HD>& to) {
-    ck.issue(k, a.ks[2], walk.key(t), L, a.hd, to.k, wave);
+    ck.issue(k, a.ks[2], walk.key(t), Lk, a.hd, to.k, wave);
     cv.issue(v, a.vs[2], walk.key(t), L, a.hd, to.v, wave);
   };
   // the tiles of this split (all of them without splits)
@@ -567,7 +570,7 @@ __device__ __forceinline__ bool attn_split(const AttnArgs& a, WaveTiles<HD>& eve
     cv.issue(v, a.vs[2], walk.key(t), walk.key(t) + rows_of(t), a.hd, to.v[wave], 0);
   };
   auto fetch_k = [&](int t) {
-    const __amdgpu_buffer_rsrc_t rs = tile_rows(k, a.ks[2], walk.key(t), rows_of(t), a.hd);
+    const __amdgpu_buffer_rsrc_t rs = tile_rows(k, a.ks[2], walk.key(t), mode >= kPos ? 0 : rows_of(t), a.hd);
 #pragma unroll
     for (int s = 0; s < KS; ++s)
       kf[s] = __builtin_amdgcn_raw_buffer_load_b128(rs, 16 * s + 8 * (lane >> 5) < a.hd ? koff + 32 * s : 0x7FFFFFF0, 0, 0);

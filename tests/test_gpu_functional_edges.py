@@ -190,3 +190,27 @@ def test_attention_gradients_of_few_keys_keep_their_digits(monkeypatch, hd, lq, 
     for name, g, r in zip(("dq", "dk"), got, ref):
         least = (r.to(torch.bfloat16).double() - r).norm()
         assert (g.cpu().double() - r).norm() <= 1.2 * least, (name, float((g.cpu().double() - r).norm() / least))
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
+def test_attention_values_that_are_seen_propagate_however_small_their_weight(monkeypatch, hd, value):
+    """A key whose score lies 400 below the row's largest has a weight that fp32 does not hold;
+    its infinity or NaN is in the row's mean all the same, before the large score as after it."""
+    l = 200
+    q = torch.zeros(1, 2, l, hd, dtype=torch.bfloat16, device=dev())
+    q[..., 0] = 20
+    k, v = torch.zeros_like(q), _rand(1, 2, l, hd, seed=1)
+    k[..., 150, 0] = 20                      # a score of 400 from row 150 on
+    v[:, 0, 3, 5], v[:, 1, 170, 5] = value, value
+    rows = torch.arange(l, device=dev())
+    for lq, splits, few in ((l, 0, 0), (l, 2, 0), (l, 3, 0), (3, 1, 128), (3, 3, 128)):
+        monkeypatch.setattr(F, "attention_splits", lambda *a: splits)
+        monkeypatch.setattr(F, "FEW_ROWS", few)
+        o = F.window_attention(q[:, :, -lq:], k, v, window=198, sinks=2, scale=1.0)
+        hit = torch.zeros(2, l, dtype=torch.bool, device=dev())
+        hit[0], hit[1] = rows >= 3, rows >= 170
+        hit = hit[:, -lq:]
+        assert torch.equal(~o[0, ..., 5].isfinite(), hit), (lq, splits)
+        others = torch.arange(hd, device=dev()) != 5
+        assert bool(o[..., others].isfinite().all())
