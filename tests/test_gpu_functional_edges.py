@@ -214,3 +214,26 @@ def test_attention_values_that_are_seen_propagate_however_small_their_weight(mon
         assert torch.equal(~o[0, ..., 5].isfinite(), hit), (lq, splits)
         others = torch.arange(hd, device=dev()) != 5
         assert bool(o[..., others].isfinite().all())
+
+
+def test_saved_tensors_kept_on_the_host():
+    """save_on_cpu gives back dense copies: the same gradients."""
+    rope = F.Rotary(64)
+    q, k, v, do = (_rand(2, 70, n, 64, seed=s) for s, n in enumerate((4, 2, 2, 4)))
+    lengths, pos = torch.tensor([70, 31], device=dev()), torch.arange(70, device=dev())
+    x, top = _rand(9, 1001), _rand(9, 5, seed=1)
+    ids, targets = torch.arange(45, device=dev()).view(9, 5) * 20, torch.arange(9, device=dev())
+
+    def run():
+        t = [y.clone().requires_grad_(True) for y in (q, k, v)]
+        z = x.clone().requires_grad_(True)
+        rq, rk = rope(t[0], t[1], positions=pos)
+        o = F.window_attention(rq.transpose(1, 2), rk.transpose(1, 2), t[2].transpose(1, 2), window=20, sinks=1, lengths=lengths)
+        loss = F.distill_loss(z, top, ids, targets=targets, temperature=2.0, weight=0.5)
+        return lambda: torch.autograd.grad((o, loss), (*t, z), (do.transpose(1, 2), torch.tensor(3.0, device=dev())))
+
+    plain = run()()
+    with torch.autograd.graph.save_on_cpu():
+        back = run()
+    for a, c in zip(back(), plain):
+        assert torch.equal(a, c)
