@@ -50,6 +50,7 @@ ops._SIGNATURES.update({
 _TYPES = ops._TYPES
 _device_now = torch._C._cuda_getDevice
 _is_compiling = torch.compiler.is_compiling
+_Tensor = torch.Tensor
 
 
 def _here(t):
@@ -77,13 +78,7 @@ def _rows(t):
     return t, s
 
 
-LEAST_FACTOR = 2.0 ** -60  # of scales and temperatures: their squares and inverses are fp32 numbers
-
-
-def _tensors(what, *given):
-    for t in given:
-        if t is not None and not isinstance(t, torch.Tensor):
-            raise TypeError(f"{what}: tensors")
+LEAST_FACTOR, MOST_FACTOR = 2.0 ** -60, 2.0 ** 60  # scales and temperatures: their squares and inverses are fp32 numbers
 
 
 def _tracked(*tensors):
@@ -181,7 +176,7 @@ class Rotary(torch.nn.Module):
         for t in (q, k):
             if t is None:
                 continue
-            if not isinstance(t, torch.Tensor):
+            if not isinstance(t, _Tensor):
                 raise TypeError("rotary: q and k are tensors")
             if t.dim() != 4 or t.shape[:2] != q.shape[:2] or t.shape[3] != q.shape[3]:
                 raise ValueError("rotary: q (b, l, heads, hd) and k (b, l, kv, hd)")
@@ -288,6 +283,8 @@ def _saved_positions(ctx, x):
     if not isinstance(ctx.positions, tuple):
         return ctx.positions
     (positions,), (dtype, shape) = ctx.saved_tensors, ctx.positions
+    if positions.dtype is dtype and positions.shape == shape and positions.device == x.device:
+        return positions
     return positions.to(x.device, dtype).reshape(shape)
 
 
@@ -575,7 +572,9 @@ def window_attention(q, k, v, window=None, sinks=0, lengths=None, scale=None):
 
     The kernels take bf16 with heads of up to 128 elements, a multiple of 8.  In the torch
     expressions an infinite or NaN key or value that some rows see makes the others NaN too.  A gradient of a row with NaN is NaN."""
-    _tensors("window_attention q, k, v and lengths", q, k, v, lengths)
+    if not (isinstance(q, _Tensor) and isinstance(k, _Tensor) and isinstance(v, _Tensor)
+            and (lengths is None or isinstance(lengths, _Tensor))):
+        raise TypeError("window_attention: q, k, v and lengths are tensors")
     if q.dim() != 4 or k.dim() != 4 or v.dim() != 4 or q.shape[3] == 0:
         raise ValueError("window_attention: q (b, heads, lq, hd), k and v (b, kv, lk, hd), hd >= 1")
     if k.shape != v.shape or q.shape[0] != k.shape[0] or q.shape[3] != k.shape[3]:
@@ -593,13 +592,14 @@ def window_attention(q, k, v, window=None, sinks=0, lengths=None, scale=None):
     scale = q.shape[3] ** -0.5 if scale is None else float(scale)
     if not (scale > 0 and math.isfinite(scale)):
         raise ValueError("window_attention: scale > 0")
-    if _eager() and LEAST_FACTOR < scale < 1 / LEAST_FACTOR and _attention_usable(q, k, v, _tracked(q, k, v)):
+    tracked = torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad)
+    if _eager() and LEAST_FACTOR < scale < MOST_FACTOR and _attention_usable(q, k, v, tracked):
         if lengths is not None:
             lengths = lengths.to(torch.int32).contiguous()
         if window is not None and window + sinks >= k.shape[2]:
             window, sinks = None, 0  # every earlier key is one or the other
         q, k, v = _attn_tensor(q), _attn_tensor(k), _attn_tensor(v)
-        if _tracked(q[0], k[0], v[0]):
+        if tracked:
             return _AttentionFn.apply(q[0], k[0], v[0], (q[1], k[1], v[1]), window, sinks, lengths, scale)
         return _attention_apply(q, k, v, window, sinks, lengths, scale)[0]
     return _attention_torch(q, k, v, window, sinks, lengths, scale)
@@ -693,7 +693,7 @@ class _DistillFn(torch.autograd.Function):
         # (the gradient's buffer and the scratch are of the forward's types and sizes)
         if (torch.is_grad_enabled() or not _eager() or not _plain(dloss) or not _distill_usable(logits, top, ids, targets)
                 or (logits.dtype, logits.shape, top.shape) != ctx.size
-                or targets is not None and not ops._companion(targets, torch.int64, len(logits))):
+                or targets is not None and (targets.dtype is not torch.int64 or targets.shape != logits.shape[:1])):
             targets = targets if targets is None else targets.to(torch.int64)
             return (ops._torch_grad(lambda t: _distill_torch(t, top, ids, targets, *rule), logits, dloss),
                     None, None, None, None, None)
@@ -712,7 +712,7 @@ def _distill_usable(logits, top, ids, targets):
 
 
 def _distill_taken(temperature):
-    return LEAST_FACTOR < temperature < 1 / LEAST_FACTOR
+    return LEAST_FACTOR < temperature < MOST_FACTOR
 
 
 def distill_loss(logits, top_logits, top_ids, targets=None, temperature=1.0, weight=1.0):
@@ -729,7 +729,9 @@ def distill_loss(logits, top_logits, top_ids, targets=None, temperature=1.0, wei
     fp32 scalar.  The kernels take dense bf16 or fp32 logits and K up to 1024; they form the
     gradient with the loss and hold it for the backward, as many bytes as the logits.  Of a loss
     that is multiplied before its backward it is formed a second time there."""
-    _tensors("distill_loss logits, top_logits, top_ids and targets", logits, top_logits, top_ids, targets)
+    if not (isinstance(logits, _Tensor) and isinstance(top_logits, _Tensor) and isinstance(top_ids, _Tensor)
+            and (targets is None or isinstance(targets, _Tensor))):
+        raise TypeError("distill_loss: logits, top_logits, top_ids and targets are tensors")
     if logits.dim() != 2 or top_logits.dim() != 2 or top_logits.shape != top_ids.shape or top_logits.shape[0] != logits.shape[0]:
         raise ValueError("distill_loss: logits (rows, V), top_logits and top_ids (rows, K)")
     if top_logits.shape[1] < 1 or logits.shape[1] < 1:
