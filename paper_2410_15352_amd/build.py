@@ -29,6 +29,7 @@ UNITS = [
     ("block_ops.hip", []),
     ("rotary.hip", []),
     ("attention.hip", []),
+    ("packed.hip", []),
     ("distill.hip", []),
     ("kernels_tile.hip", ["-mllvm", "-enable-misched=false", "-mllvm", "-enable-post-misched=false"]),
     ("kernels_w4.hip", ["-mllvm", "-enable-misched=false", "-mllvm", "-enable-post-misched=false"]),

@@ -1,5 +1,5 @@
 // Arguments of the kernels behind functional.py: rotary positions (rotary.hip),
-// attention with a window and sinks (attention.hip), distillation (distill.hip).
+// attention with a window and sinks (attention.hip; packed.hip), distillation (distill.hip).
 // All pointers are device pointers; strides are in elements.  Entry points return
 // 0, -1 (a size they do not take) or -5 (HIP error).
 #pragma once
@@ -53,6 +53,7 @@ struct AttnGradArgs {
   int64_t gs[3], dqs[3], dks[3], dvs[3];
   float* part;                   // [compact_attention_bwd_scratch()]
   int32_t parts, near_keys, chunks, far_keys, fine;  // set by the entry point
+  int32_t sequences;             // packed: how many
 };
 
 struct DistillArgs {

@@ -4,10 +4,11 @@
                        frequencies scaled for long contexts
     window_attention   attention with a sliding window and a few first tokens that stay
                        visible (sinks); training, prompts, and single tokens over a cache
+    packed_attention   the same inside each of several sequences that lie end to end
     distill_loss       distillation from a teacher's top logits, beside the targets
 
 On the current GPU they run the HIP kernels of libcompact.so (csrc/rotary.hip, attention.hip,
-distill.hip) on the current stream, forward and backward: bf16 (Rotary and distill_loss fp32
+packed.hip, distill.hip) on the current stream, forward and backward: bf16 (Rotary and distill_loss fp32
 too), any strides whose rows start on 16-byte boundaries (others are copied first).  Other
 types and places, autocast, tracing and functorch take the torch expressions beside each
 function, and so does a backward that is itself recorded or batched.  Arguments that no form
@@ -26,7 +27,7 @@ from . import _block_ops as ops
 from . import _lib
 from ._block_ops import _eager, _i64, _plain, _stream, _vp
 
-__all__ = ["Rotary", "window_attention", "distill_loss"]
+__all__ = ["Rotary", "window_attention", "packed_attention", "packed_positions", "distill_loss"]
 
 _bf16 = torch.bfloat16
 
@@ -35,7 +36,7 @@ _bf16 = torch.bfloat16
 _ROTARY = struct.Struct("@" + 3 * "2Q6q2i" + "2Q4q8if").pack
 _ATTN = "7Q12q8if2i2Q"
 _attn_pack = struct.Struct("@" + _ATTN).pack
-_attn_grad_pack = struct.Struct("@" + _ATTN + "5Q12qQ5i").pack
+_attn_grad_pack = struct.Struct("@" + _ATTN + "5Q12qQ6i").pack
 _distill_pack = struct.Struct("@11Q5q6i2f").pack
 _block = ctypes.c_char_p
 
@@ -43,6 +44,8 @@ ops._SIGNATURES.update({
     "compact_rotary": [_block, _vp],
     "compact_attention_fwd": [_block, _vp],
     "compact_attention_bwd": [_block, _vp],
+    "compact_packed_fwd": [_block, _vp, ctypes.c_int, _i64, ctypes.c_int, _vp, _vp],
+    "compact_packed_bwd": [_block, ctypes.c_int, _vp, _vp],
     "compact_distill": [_block, _vp],
 })
 
@@ -402,7 +405,11 @@ def _attention_expressions(q, k, v, window, sinks, lengths, scale):
         kw, vw = (t.repeat_interleave(heads // kv, 1) for t in (kw, vw))
     if lk == 0:  # (a maximum over nothing is refused; sums over nothing are zero)
         return torch.matmul(torch.matmul(qw, kw.transpose(2, 3)), vw).to(q.dtype)
-    seen = _visible(lq, lk, lengths, window, sinks, q.device)
+    return _attend(qw, kw, vw, _visible(lq, lk, lengths, window, sinks, q.device), scale).to(q.dtype)
+
+
+def _attend(qw, kw, vw, seen, scale):
+    """softmax(scale q k^T) v over the keys seen."""
     used = seen.any(2).unsqueeze(-1)  # (what lies past a sequence, or before every window, may be anything)
     kw, vw = torch.where(used, kw, 0.0), torch.where(used, vw, 0.0)
     s = torch.matmul(qw, kw.transpose(2, 3).contiguous()) * scale
@@ -411,7 +418,7 @@ def _attention_expressions(q, k, v, window, sinks, lengths, scale):
     top = torch.where(some, s.detach().amax(-1, keepdim=True), 0.0)
     e = torch.exp(s - top)
     p = e / torch.where(some, e.sum(-1, keepdim=True), 1.0)
-    return torch.matmul(p, vw).to(q.dtype)
+    return torch.matmul(p, vw)
 
 
 FEW_ROWS = 32
@@ -555,7 +562,7 @@ class _AttentionFn(torch.autograd.Function):
         delta = scratch.data_ptr()
         ops._call("compact_attention_bwd",
                   _attn_grad_pack(*fields, do[0].data_ptr(), dq.data_ptr(), *outs, delta, *do[1], *dq_strides, *strides,
-                                  delta + -(-rows // 4) * 16 if floats > 0 else 0, 0, 0, 0, 0, 0), _stream(q))
+                                  delta + -(-rows // 4) * 16 if floats > 0 else 0, 0, 0, 0, 0, 0, 0), _stream(q))
         return dq, dk, dv, *none
 
 
@@ -614,6 +621,194 @@ def _attention_usable(q, k, v, tracked):
     return (q.dtype == _bf16 and hd % 8 == 0 and 8 <= hd <= MAX_HD and min(b, lq, lk) > 0 and max(lq, lk) <= 1 << 30
             and b * heads * -(-lq // 32) < 1 << 24 and b * kv * -(-lk // 32) < 1 << 24
             and _here(q) and _here(k) and _here(v))
+
+
+# --------------------------- packed sequences -------------------------------
+
+MOST_SEQUENCES = (1 << 24) - 1
+
+
+def _bounds(starts, rows):
+    """The running maximum of the starts, each within the rows."""
+    return starts.to(torch.int64).clamp(0, rows).cummax(0).values
+
+
+def packed_positions(starts, rows):
+    """The position of each of `rows` rows in its sequence (int64; 0 for rows of none), for Rotary."""
+    e, i = _bounds(starts, rows), torch.arange(rows, device=starts.device)
+    s = torch.searchsorted(e, i, right=True)
+    return torch.where((s > 0) & (s < len(e)), i - e[(s - 1).clamp(min=0)], 0)
+
+
+def _packed_torch(q, k, v, starts, window, sinks, scale):
+    """The attention as torch expressions, in fp32 (fp64 for fp64)."""
+    rows, heads, kv = q.shape[0], q.shape[1], k.shape[1]
+    wide = torch.float64 if q.dtype == torch.float64 else torch.float32
+    e, i = _bounds(starts, rows), torch.arange(rows, device=q.device)
+    s = torch.searchsorted(e, i, right=True)  # 0, or n + 1: no sequence
+    p, j = i.unsqueeze(1), i
+    seen = (s.unsqueeze(1) == s) & ((s > 0) & (s < len(e))).unsqueeze(1) & (j <= p)
+    if window is not None:
+        seen = seen & ((p - j < window) | (packed_positions(starts, rows) < sinks))
+    with _as_typed(q):
+        qw, kw, vw = (t.to(wide).transpose(0, 1).unsqueeze(0) for t in (q, k, v))
+        if kv != heads:
+            kw, vw = (t.repeat_interleave(heads // kv, 1) for t in (kw, vw))
+        if rows == 0:
+            return torch.matmul(torch.matmul(qw, kw.transpose(2, 3)), vw).squeeze(0).transpose(0, 1).to(q.dtype)
+        return _attend(qw, kw, vw, seen.view(1, 1, rows, rows), scale).squeeze(0).transpose(0, 1).to(q.dtype)
+
+
+def _packed_tensor(t):
+    """A bf16 (rows, heads, hd) tensor as the kernels take it, and its strides: (0, head, row)."""
+    rows, heads, hd = t.shape
+    x, y, z = t.stride()
+    x, y = x if rows > 1 else 0, y if heads > 1 else 0
+    if z != 1 or (t.data_ptr() | 2 * (x | y)) % 16 != 0 or rows > 1 and not hd <= x <= MAX_ROW_STRIDE:
+        t = t.contiguous()
+        t = t if t.data_ptr() % 16 == 0 else t.clone()
+        x, y = heads * hd if rows > 1 else 0, hd if heads > 1 else 0
+    return t, (0, y, x)
+
+
+def _packed_fields(q, k, v, o, stats, window, sinks, scale):
+    """q, k, v, o: (tensor, strides); a padded batch of one sequence, but for the table of the rows."""
+    rows, heads, hd = q[0].shape
+    kv, lse = k[0].shape[1], stats.data_ptr()
+    stat = rows * heads
+    return (q[0].data_ptr(), k[0].data_ptr(), v[0].data_ptr(), o[0].data_ptr(), lse,
+            lse + -(-stat // 4) * 16 if stats.numel() > stat else 0, 0, *q[1], *k[1], *v[1], *o[1], 1, heads, kv, rows, rows, hd,
+            NO_WINDOW if window is None else min(window, NO_WINDOW), min(sinks, NO_WINDOW), scale, 0, 0, 0, 0)
+
+
+def _packed_table_words(n, rows):
+    return 4 + 2 * (-(-(n + 3) // 4) * 4) + 4 * (rows // 128 + min(n + 2, rows))
+
+
+def _packed_scratch(block, n):
+    fn = _fns.get("packed")
+    if fn is None:
+        fn = _fns["packed"] = _lib.load().compact_packed_bwd_scratch
+        fn.restype, fn.argtypes = _i64, [_block, ctypes.c_int]
+    return fn(block, n)
+
+
+def _packed_apply(q, k, v, starts, window, sinks, scale, tracked=False):
+    """q, k, v: as _packed_tensor gives them; (o, the statistics that a backward wants, the table of the rows)"""
+    rows, heads, hd = q[0].shape
+    device, n = q[0].device, starts.shape[0] - 1
+    o = torch.empty(rows, heads, hd, dtype=_bf16, device=device)
+    stats = torch.empty(_stats_count((1, heads, rows, hd), tracked), dtype=torch.float32, device=device)
+    table = torch.empty(_packed_table_words(n, rows), dtype=torch.int32, device=device)
+    ops._call("compact_packed_fwd", _attn_pack(*_packed_fields(q, k, v, (o, (0, hd, heads * hd)), stats, window, sinks, scale)),
+              starts.data_ptr(), starts.dtype == torch.int64, starts.stride(0), n, table.data_ptr(), _stream(stats))
+    return o, stats, table
+
+
+class _PackedFn(torch.autograd.Function):
+    """Keeps q, k, v, o, one fp32 number a row and a byte an element beside o, and the table that the
+    forward made of the starts."""
+
+    @staticmethod
+    def forward(ctx, q, k, v, strides, starts, window, sinks, scale):
+        o, stats, table = _packed_apply(*zip((q, k, v), strides), starts, window, sinks, scale, tracked=True)
+        ctx.rule = window, sinks, scale
+        ctx.shapes = q.shape, k.shape, starts.shape[0] - 1
+        ctx.save_for_backward(q, k, v, o, stats, table)
+        return o
+
+    @staticmethod
+    def backward(ctx, do):
+        q, k, v, o, stats, table = ctx.saved_tensors
+        window, sinks, scale = ctx.rule
+        shape, kv_shape, n = ctx.shapes
+        rows, heads, hd = shape
+        none = (None,) * 5
+        words = _packed_table_words(n, rows)
+        if (torch.is_grad_enabled() or not _eager() or not _here(do)
+                or not ops._companion(stats, torch.float32, _stats_count((1, heads, rows, hd), True))
+                or not ops._companion(table, torch.int32, words)
+                or not all(t.dtype is _bf16 and t.shape == s and _here(t)
+                           for t, s in ((q, shape), (k, kv_shape), (v, kv_shape), (o, shape)))):
+            recorded = torch.is_grad_enabled()
+            starts = table.reshape(-1)[5:6 + n].to(q.device)
+            with torch.enable_grad():
+                # (aliases: of v = f(k), k's own gradient must not hold what reaches k through v)
+                leaves = [x.view_as(x) if recorded and x.requires_grad else x.detach().requires_grad_(True) for x in (q, k, v)]
+                y = _packed_torch(*leaves, starts, window, sinks, scale)
+                return (*torch.autograd.grad(y, leaves, do, create_graph=recorded), *none)
+        do = _packed_tensor(do if do.dtype is _bf16 else do.to(_bf16))
+        fields = _packed_fields(_packed_tensor(q), _packed_tensor(k), _packed_tensor(v), _packed_tensor(o), stats, window, sinks, scale)
+        device, stat = q.device, rows * heads
+        dq = torch.empty(shape, dtype=_bf16, device=device)
+        dk = dv = None
+        outs, kv, floats = (0, 0), kv_shape[1], 0
+        if ctx.needs_input_grad[1] or ctx.needs_input_grad[2]:
+            dk, dv = torch.empty(kv_shape, dtype=_bf16, device=device), torch.empty(kv_shape, dtype=_bf16, device=device)
+            outs = dk.data_ptr(), dv.data_ptr()
+            floats = _packed_scratch(_attn_pack(*fields), n)
+        scratch = torch.empty(-(-stat // 4) * 4 + floats, dtype=torch.float32, device=device)  # D, and sums in parts
+        delta = scratch.data_ptr()
+        ops._call("compact_packed_bwd",
+                  _attn_grad_pack(*fields, do[0].data_ptr(), dq.data_ptr(), *outs, delta, *do[1], 0, hd, heads * hd,
+                                  *(0, hd, kv * hd) * 2, delta + -(-stat // 4) * 16 if floats > 0 else 0, 0, 0, 0, 0, 0, n),
+                  n, table.data_ptr(), _stream(q))
+        return dq, dk, dv, *none
+
+
+def packed_attention(q, k, v, starts, window=None, sinks=0, scale=None):
+    """softmax(scale q k^T) v inside each of n sequences that lie end to end: q (rows, heads, hd), k
+    and v (rows, kv, hd), heads a multiple of kv (query head h reads head h kv // heads).
+
+    starts (n + 1,), integers on the device, ascending: sequence s holds the rows starts[s] ..
+    starts[s + 1] - 1 (none where they are equal).  Row p of a sequence sees its key j when
+    j <= p and (p - j < window or j < sinks); window None: every j <= p.  Rows of no sequence,
+    before the first or behind the last, give zeros and pass no gradient.  (A start below an
+    earlier one, or past the rows, is taken as that one, or as the last row's end.)
+    scale: 1 / sqrt(hd) if None.
+
+    The kernels take bf16 with heads of up to 128 elements, a multiple of 8; what a row does not
+    see has no part in it, whatever it holds, and a row whose scores are all -inf gives NaN, as in
+    window_attention.  packed_positions(starts, rows) gives Rotary its positions."""
+    if not (isinstance(q, _Tensor) and isinstance(k, _Tensor) and isinstance(v, _Tensor) and isinstance(starts, _Tensor)):
+        raise TypeError("packed_attention: q, k, v and starts are tensors")
+    if q.dim() != 3 or k.dim() != 3 or v.dim() != 3 or q.shape[2] == 0:
+        raise ValueError("packed_attention: q (rows, heads, hd), k and v (rows, kv, hd), hd >= 1")
+    if k.shape != v.shape or q.shape[0] != k.shape[0] or q.shape[2] != k.shape[2]:
+        raise ValueError(f"packed_attention: q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}")
+    if k.shape[1] == 0 or q.shape[1] % k.shape[1] != 0:
+        raise ValueError(f"packed_attention: {q.shape[1]} query heads over {k.shape[1]} of k and v")
+    if not q.is_floating_point() or q.dtype != k.dtype or q.dtype != v.dtype or not q.device == k.device == v.device:
+        raise TypeError("packed_attention: q, k and v of one floating type on one device")
+    if starts.dim() != 1 or starts.shape[0] < 2 or starts.device != q.device or starts.dtype not in (torch.int32, torch.int64):
+        raise ValueError("packed_attention: starts (n + 1,), n >= 1, of int32 or int64 on q's device")
+    window, sinks = None if window is None else index(window), index(sinks)
+    if window is not None and window < 1 or sinks < 0:
+        raise ValueError("packed_attention: window >= 1 (or None) and sinks >= 0")
+    scale = q.shape[2] ** -0.5 if scale is None else float(scale)
+    if not (scale > 0 and math.isfinite(scale)):
+        raise ValueError("packed_attention: scale > 0")
+    tracked = torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad)
+    if _eager() and LEAST_FACTOR < scale < MOST_FACTOR and _packed_usable(q, k, v, starts, tracked):
+        if window is not None and window + sinks >= q.shape[0]:
+            window, sinks = None, 0  # every earlier key is one or the other
+        q, k, v = _packed_tensor(q), _packed_tensor(k), _packed_tensor(v)
+        if tracked:
+            return _PackedFn.apply(q[0], k[0], v[0], (q[1], k[1], v[1]), starts, window, sinks, scale)
+        return _packed_apply(q, k, v, starts, window, sinks, scale)[0]
+    return _packed_torch(q, k, v, starts, window, sinks, scale)
+
+
+def _packed_usable(q, k, v, starts, tracked):
+    rows, heads, hd = q.shape
+    kv, n = k.shape[1], starts.shape[0] - 1
+    items = rows // 128 + min(n + 2, rows)
+    # a launch has under 2^32 threads: dk and dv take a workgroup for each item, up to two for its sinks, and up to
+    # 2^20 more in parts
+    if tracked and (3 * items * kv + (1 << 20) + 1024) * (512 if hd > 96 else 256) >= 1 << 32:
+        return False
+    return (q.dtype == _bf16 and hd % 8 == 0 and 8 <= hd <= MAX_HD and 0 < rows <= 1 << 30 and n <= MOST_SEQUENCES and heads > 0
+            and items * heads < 1 << 24 and heads * -(-rows // 32) < 1 << 24 and _here(q) and _here(k) and _here(v) and _here(starts))
 
 
 # ----------------------------- distillation ---------------------------------

@@ -1,0 +1,189 @@
+"""Attention over packed sequences without a GPU: the torch expressions against the definition
+written out element by element in 64 bits, their gradients against differences, what is refused,
+and which form answers (launches noted, not made)."""
+import math
+import struct
+
+import pytest
+
+torch = pytest.importorskip("torch")
+F = pytest.importorskip("paper_2410_15352_amd.functional")
+
+bf16, f32, f64 = torch.bfloat16, torch.float32, torch.float64
+
+
+def _rand(*shape, seed=0, dtype=f64):
+    return torch.randn(*shape, generator=torch.Generator().manual_seed(seed + sum(shape)), dtype=f64).to(dtype)
+
+
+def _by_element(q, k, v, starts, window, sinks, scale):
+    rows, heads, hd = q.shape
+    kv = k.shape[1]
+    o = torch.zeros_like(q)
+    for first, end in zip(starts, starts[1:]):
+        for i in range(first, end):
+            for h in range(heads):
+                g = h * kv // heads
+                keys = [j for j in range(first, i + 1) if window is None or i - j < window or j - first < sinks]
+                w = [math.exp(scale * float(q[i, h] @ k[j, g])) for j in keys]
+                o[i, h] = sum(x * v[j, g] for x, j in zip(w, keys)) / sum(w)
+    return o
+
+
+@pytest.mark.parametrize("starts", [[0, 9], [0, 1, 4, 9], [2, 2, 7, 7], [0, 0, 0], [9, 9], [3, 5]], ids=str)
+@pytest.mark.parametrize("window,sinks", [(None, 0), (2, 1), (1, 0), (3, 20)])
+def test_against_the_definition(starts, window, sinks):
+    q, k, v = _rand(9, 4, 6, seed=1), _rand(9, 2, 6, seed=2), _rand(9, 2, 6, seed=3)
+    for dtype in (torch.int32, torch.int64):
+        o = F.packed_attention(q, k, v, torch.tensor(starts, dtype=dtype), window=window, sinks=sinks, scale=0.7)
+        assert torch.allclose(o, _by_element(q, k, v, starts, window, sinks, 0.7), atol=1e-12)
+
+
+def test_starts_out_of_order():
+    """Taken as the running maximum within the rows."""
+    q, k, v = (_rand(9, 1, 4, seed=s) for s in (1, 2, 3))
+    for given, meant in (([-3, 5, 2, 20], [0, 5, 5, 9]), ([4, 1, 7], [4, 4, 7])):
+        o = F.packed_attention(q, k, v, torch.tensor(given))
+        assert torch.allclose(o, _by_element(q, k, v, meant, None, 0, 0.5), atol=1e-12)
+        assert torch.equal(F.packed_positions(torch.tensor(given), 9), F.packed_positions(torch.tensor(meant), 9))
+
+
+def test_positions():
+    assert F.packed_positions(torch.tensor([1, 4, 4, 6], dtype=torch.int32), 8).tolist() == [0, 0, 1, 2, 0, 1, 0, 0]
+
+
+def test_gradient():
+    t = [_rand(7, h, 4, seed=h).requires_grad_() for h in (4, 2, 2)]
+    starts = torch.tensor([0, 3, 6])
+    assert torch.autograd.gradcheck(lambda q, k, v: F.packed_attention(q, k, v, starts, window=2, sinks=1), t)
+    # rows of no sequence: zeros, and no gradient
+    o = F.packed_attention(*t, starts)
+    assert torch.equal(o[6], torch.zeros_like(o[6]))
+    for g in torch.autograd.grad(o, t, torch.ones_like(o)):
+        assert torch.equal(g[6], torch.zeros_like(g[6]))
+
+
+def test_no_rows():
+    q = torch.zeros(0, 2, 8)
+    assert F.packed_attention(q, q, q, torch.tensor([0, 0])).shape == q.shape
+
+
+_Z = torch.zeros(4, 2, 8)
+_S = torch.tensor([0, 4])
+
+
+@pytest.mark.parametrize("error,call", [
+    (TypeError, lambda: F.packed_attention(_Z, _Z, _Z, [0, 4])),
+    (TypeError, lambda: F.packed_attention(_Z, _Z, None, _S)),
+    (TypeError, lambda: F.packed_attention(_Z, _Z, _Z.double(), _S)),
+    (TypeError, lambda: F.packed_attention(_Z.long(), _Z.long(), _Z.long(), _S)),
+    (TypeError, lambda: F.packed_attention(_Z, _Z, _Z, _S, window=1.5)),
+    (ValueError, lambda: F.packed_attention(_Z[0], _Z, _Z, _S)),
+    (ValueError, lambda: F.packed_attention(_Z, _Z[:3], _Z[:3], _S)),
+    (ValueError, lambda: F.packed_attention(_Z, _Z[..., :4], _Z[..., :4], _S)),
+    (ValueError, lambda: F.packed_attention(_Z[:, :1], _Z, _Z, _S)),
+    (ValueError, lambda: F.packed_attention(_Z, _Z[:, :0], _Z[:, :0], _S)),
+    (ValueError, lambda: F.packed_attention(_Z[..., :0], _Z[..., :0], _Z[..., :0], _S)),
+    (ValueError, lambda: F.packed_attention(_Z, _Z, _Z, _S[:1])),
+    (ValueError, lambda: F.packed_attention(_Z, _Z, _Z, _S.view(1, 2))),
+    (ValueError, lambda: F.packed_attention(_Z, _Z, _Z, _S.float())),
+    (ValueError, lambda: F.packed_attention(_Z, _Z, _Z, _S.to("meta"))),
+    (ValueError, lambda: F.packed_attention(_Z, _Z, _Z, _S, window=0)),
+    (ValueError, lambda: F.packed_attention(_Z, _Z, _Z, _S, sinks=-1)),
+    (ValueError, lambda: F.packed_attention(_Z, _Z, _Z, _S, scale=0.0)),
+    (ValueError, lambda: F.packed_attention(_Z, _Z, _Z, _S, scale=math.inf))])
+def test_refuses(error, call):
+    with pytest.raises(error):
+        call()
+
+
+def test_under_autocast_stays_in_32_bits():
+    t = [_rand(9, 2, 8, seed=s, dtype=f32) for s in (1, 2, 3)]
+    plain = F.packed_attention(*t, torch.tensor([0, 4, 9]), window=4)
+    with torch.autocast("cpu", dtype=bf16):
+        assert torch.equal(F.packed_attention(*t, torch.tensor([0, 4, 9]), window=4), plain)
+
+
+# ------------------------------- routes --------------------------------------
+
+@pytest.fixture
+def launches(monkeypatch):
+    """Entry points called, in order, with their arguments."""
+    calls = []
+    monkeypatch.setattr(F, "_here", F._plain)
+    monkeypatch.setattr(F, "_stream", lambda t: 0)
+    monkeypatch.setattr(F.ops, "_call", lambda name, *args: calls.append((name, args)))
+    monkeypatch.setattr(F.ops, "_companion", lambda t, dtype, count: (
+        t.dtype == dtype and t.numel() == count and F._plain(t) and t.is_contiguous()))
+    monkeypatch.setattr(F, "_packed_scratch", lambda block, n: 0)
+    return calls
+
+
+def test_kernels_answer(launches):
+    q, k, v = (_rand(9, h, 8, seed=h, dtype=bf16).requires_grad_() for h in (4, 2, 2))
+    starts = torch.tensor([0, 4, 9])
+    o = F.packed_attention(q, k, v, starts, window=3, sinks=1)
+    assert o.shape == (9, 4, 8)
+    g = torch.autograd.grad(o, (q, k, v), torch.ones_like(o))
+    assert [x.shape for x in g] == [(9, 4, 8), (9, 2, 8), (9, 2, 8)]
+    assert [name for name, _ in launches] == ["compact_packed_fwd", "compact_packed_bwd"]
+    fields = struct.unpack("@" + F._ATTN, launches[0][1][0])
+    # strides (none of a batch, head, row) of q, k, v, o; sizes
+    assert fields[7:19] == (0, 8, 32, 0, 8, 16, 0, 8, 16, 0, 8, 32) and fields[19:27] == (1, 4, 2, 9, 9, 8, 3, 1)
+    assert launches[0][1][2:5] == (True, 1, 2)
+
+
+def test_table_holds_every_item():
+    """As many items as rows // 128 + min(n + 2, rows), whatever the bounds."""
+    import random
+    rng = random.Random(1)
+    for _ in range(300):
+        rows, n = rng.choice((1, 5, 127, 128, 129, 1000)), rng.choice((1, 2, 7, 300))
+        e = sorted(rng.randint(0, rows) for _ in range(n + 1))
+        bounds = [0, *e, rows]
+        items = sum(-(-(b - a) // 128) for a, b in zip(bounds, bounds[1:]))
+        assert items <= rows // 128 + min(n + 2, rows)
+        words = F._packed_table_words(n, rows)
+        assert words == 4 + 2 * ((n + 3 + 3) // 4 * 4) + 4 * (rows // 128 + min(n + 2, rows))
+
+
+@pytest.mark.parametrize("change", [
+    lambda t: t.long() if t.dtype == torch.int32 else t,
+    lambda t: torch.stack((t, t), 1)[:, 0] if t.dtype == torch.int32 else t,
+    lambda t: t.float() if t.dtype == bf16 else t])
+def test_saved_tensors_changed_by_a_hook(launches, monkeypatch, change):
+    """What a hook gave back in another type or layout does not reach the kernels; the bounds are the table's."""
+    q, k, v = (_rand(9, 2, 8, seed=s, dtype=bf16).requires_grad_() for s in (1, 2, 3))
+    starts, do = torch.tensor([0, 4, 8], dtype=torch.int32), _rand(9, 2, 8, seed=4, dtype=bf16)
+    apply = F._packed_apply
+
+    def filled(*a, **k):
+        o, stats, table = apply(*a, **k)
+        table[4:9] = torch.tensor([0, 0, 4, 8, 9])
+        return o, stats, table
+    monkeypatch.setattr(F, "_packed_apply", filled)
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: t, change):
+        o = F.packed_attention(q, k, v, starts, window=3, sinks=1)
+    g = torch.autograd.grad(o, (q, k, v), do)
+    assert [name for name, _ in launches] == ["compact_packed_fwd"]
+    wide = [t.detach().double().requires_grad_() for t in (q, k, v)]
+    for a, e in zip(g, torch.autograd.grad(F.packed_attention(*wide, starts, window=3, sinks=1), wide, do.double())):
+        assert (a.double() - e).abs().max() <= 2.0 ** -7 * e.abs().max()
+
+
+@pytest.mark.parametrize("make", [lambda t: t.float(), lambda t: t[..., :7], lambda t: t[:0]])
+def test_what_the_kernels_do_not_take(launches, make):
+    q = make(_rand(9, 2, 16, dtype=bf16))
+    assert F.packed_attention(q, q, q, torch.tensor([0, 4])).shape == q.shape and not launches
+
+
+def test_strides_that_the_kernels_take(launches):
+    buf = _rand(9, 3, 2, 16, dtype=bf16)
+    q, k, v = buf.unbind(1)
+    F.packed_attention(q, k, v, torch.tensor([0, 4]))
+    args = struct.unpack("@" + F._ATTN, launches[-1][1][0])
+    assert args[0] == q.data_ptr() and args[7:10] == (0, 16, 96)  # as they are
+    for t in (buf.unbind(1)[0].transpose(0, 1).contiguous().transpose(0, 1), q[:1].expand(9, 2, 16), _rand(9, 2, 20, dtype=bf16)[..., 4:]):
+        F.packed_attention(t, k, v, torch.tensor([0, 4]))
+        args = struct.unpack("@" + F._ATTN, launches[-1][1][0])
+        assert args[7:10] in ((0, 144, 16), (0, 16, 32)) and args[0] % 16 == 0 and (args[9] >= 16)
