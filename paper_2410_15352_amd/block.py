@@ -24,10 +24,10 @@ from torch.nn.modules import module as _module
 from torch.nn.attention import SDPBackend, sdpa_kernel
 
 from . import _block_ops as ops
-from .functional import distill_loss, rotary_split_qkv, window_attention
+from .functional import distill_loss, packed_attention, packed_positions, rotary_split_qkv, window_attention
 from .nn import CompActAdam, CompActGroup, CompActLinear
 
-__all__ = ["RMSNorm", "DenseLinear", "LlamaBlock", "LlamaModel", "block_saved_bytes", "make_optimizers"]
+__all__ = ["RMSNorm", "DenseLinear", "LlamaBlock", "LlamaModel", "block_saved_bytes", "make_optimizers", "gradients"]
 
 
 def _pad8(c):
@@ -119,7 +119,11 @@ class LlamaBlock(torch.nn.Module):
     also makes the attention output projection a CompAct layer (which saves
     memory only where attention does not keep its output).  rope: a Rotary that
     turns q and k; window, sinks: attention over the last `window` tokens and the
-    first `sinks` ones (window_attention)."""
+    first `sinks` ones (window_attention).
+
+    forward(x, starts=...): x (1, l, d) holds sequences that lie end to end, as
+    packed_attention takes them, and positions count from each one's start (positions:
+    those, where the caller has them)."""
 
     def __init__(self, d, heads, ffn, rank=None, rank_down=None, seeds=None, alpha=1.0,
                  compress_o=False, device="cuda", weights=None, proj="gaussian", rope=None, window=None, sinks=0):
@@ -151,8 +155,12 @@ class LlamaBlock(torch.nn.Module):
         else:
             self.o = DenseLinear(d, d, device, Wo)
 
-    def forward(self, x):
+    def forward(self, x, starts=None, positions=None):
         b, l, d = x.shape
+        if starts is not None and b != 1:
+            raise ValueError("LlamaBlock: packed sequences are one batch entry, (1, l, d)")
+        if starts is not None and positions is None and self.rope is not None:
+            positions = packed_positions(starts, l)
         # (a norm that was replaced or subclassed is called as any module)
         x, h = self.norm1.with_residual(x) if type(self.norm1) is RMSNorm else (x, self.norm1(x))
         qkv = self.qkv(h.reshape(b * l, d)).reshape(b, l, 3, self.heads, d // self.heads)
@@ -161,8 +169,11 @@ class LlamaBlock(torch.nn.Module):
         if self.rope is None:
             q, k, v = ops.split_qkv(qkv)
         else:  # in place, unless someone else may hold the projection's output
-            q, k, v = rotary_split_qkv(qkv, self.rope, in_place=_runs_alone(self.qkv, _PROJECTIONS.get(type(self.qkv))))
-        if self.window is not None:
+            q, k, v = rotary_split_qkv(qkv, self.rope, positions, in_place=_runs_alone(self.qkv, _PROJECTIONS.get(type(self.qkv))))
+        if starts is not None:
+            q, k, v = (t.squeeze(0).transpose(0, 1) for t in (q, k, v))
+            a = packed_attention(q, k, v, starts, window=self.window, sinks=self.sinks).transpose(0, 1).unsqueeze(0)
+        elif self.window is not None:
             a = window_attention(q, k, v, window=self.window, sinks=self.sinks)
         else:
             with sdpa_kernel([SDPBackend.FLASH_ATTENTION]):
@@ -209,7 +220,8 @@ class LlamaModel(torch.nn.Module):
     """Token embedding, n_layers blocks, final RMSNorm and the output layer
     (uncompressed), with the mean cross-entropy of next-token prediction, or, given
     a teacher's (top_logits, top_ids), both (b, l, K), with distill_loss.  rope, window
-    and sinks as in LlamaBlock."""
+    and sinks as in LlamaBlock.  With starts, the tokens (rows,) or (1, rows) are sequences that
+    lie end to end.  logits(tokens, starts=...) gives (rows, V), for the losses of finetune.py."""
 
     def __init__(self, vocab, d, heads, ffn, n_layers, rank=None, alpha=1.0, device="cuda", proj="gaussian", rope=None,
                  window=None, sinks=0):
@@ -222,12 +234,24 @@ class LlamaModel(torch.nn.Module):
         self.norm = RMSNorm(d, device=device)
         self.head = DenseLinear(d, vocab, device)
 
-    def forward(self, tokens, targets, teacher=None, temperature=1.0, weight=0.5):
+    def logits(self, tokens, starts=None):
+        if starts is not None:
+            if tokens.dim() != 1 and tokens.shape[:-1].numel() != 1:
+                raise ValueError("LlamaModel: packed tokens are (rows,) or (1, rows)")
+            tokens = tokens.reshape(1, -1)
         x = self.embed[tokens]
-        for blk in self.blocks:
-            x = blk(x)
+        if starts is None:
+            for blk in self.blocks:
+                x = blk(x)
+        else:
+            positions = packed_positions(starts, tokens.shape[1]) if any(blk.rope is not None for blk in self.blocks) else None
+            for blk in self.blocks:
+                x = blk(x, starts, positions)
         logits = self.head(self.norm(x))
-        logits, targets = logits.reshape(-1, logits.shape[-1]), targets.reshape(-1)
+        return logits.reshape(-1, logits.shape[-1])
+
+    def forward(self, tokens, targets, teacher=None, temperature=1.0, weight=0.5, starts=None):
+        logits, targets = self.logits(tokens, starts), targets.reshape(-1)
         if teacher is None:
             return ops.cross_entropy(logits, targets)
         top, ids = (t.reshape(-1, t.shape[-1]) for t in teacher)
@@ -249,3 +273,10 @@ def make_optimizers(model, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, reseed_period=
     if params:
         opts.append(torch.optim.Adam(params, lr=lr, betas=betas, eps=eps, foreach=True))
     return opts
+
+
+def gradients(model):
+    """What clip_grad_norm takes of a model: the compressed gradients of the CompAct layers that had
+    a backward pass, which lie beside autograd, and every other parameter's gradient."""
+    found = [g for mod in model.modules() if isinstance(mod, CompActGroup) and mod.grad_ready for g in mod.ghat]
+    return found + [p.grad for p in model.parameters() if p.grad is not None and p.numel() > 0]

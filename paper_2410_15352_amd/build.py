@@ -31,6 +31,8 @@ UNITS = [
     ("attention.hip", []),
     ("packed.hip", []),
     ("distill.hip", []),
+    ("finetune.hip", []),
+    ("clip.hip", []),
     ("kernels_tile.hip", ["-mllvm", "-enable-misched=false", "-mllvm", "-enable-post-misched=false"]),
     ("kernels_w4.hip", ["-mllvm", "-enable-misched=false", "-mllvm", "-enable-post-misched=false"]),
 ]

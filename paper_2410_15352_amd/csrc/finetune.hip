@@ -1,0 +1,422 @@
+// Losses over the log-probabilities of given tokens.  For a row x of V logits and its target t,
+// with m = max x, s = sum exp(x - m):
+//
+//   l = x_t - m - log s,    dl / dx_v = [v = t] - exp(x_v - m) / s
+//
+// log-probabilities: l, and dx from a given dl.
+// preference: of n pairs of sequences, S = sum over a sequence's rows of (l - reference),
+//   D = beta (S_first - S_second),  loss = mean of (1 - e) softplus(-D) + e softplus(D),
+//   dloss / dl = +- beta (sigmoid(D) - (1 - e)) / n  in the rows of the first, the second.
+// policy: ratio r = exp(l - old), advantage A, bounds lo = 1 - low, hi = 1 + high,
+//   loss = mean over the N rows that count of -min(r A, clamp(r, lo, hi) A) + kl (exp(d) - d - 1),
+//   d = reference - l;   dl = ((r clamped away ? 0 : -A r) - kl (exp(d) - 1)) / N.
+//
+// Rows whose target is ignore_index do not count: l = 0, no gradient, and they are not read; a
+// target past V makes a row NaN.  A row without a gradient (dl = 0) has zeros, whatever its logits are.
+//
+// All are bound by HBM: the logits of a row that counts are read once for l, and once more for the
+// gradient where that needs sums over other rows first (log-probabilities, preference); the policy
+// loss holds a row in registers and forms both.  l is put together in fp64 (a few operations a
+// row): the sums of exponentials are fp32, and what is left of l - reference is a difference of
+// near numbers.
+#include <hip/hip_runtime.h>
+
+#include "common.hpp"
+#include "functional.hpp"
+#include "rows.hpp"
+
+namespace compact {
+namespace {
+
+__device__ __forceinline__ double log_prob(float xt, float m, float s) {
+  return static_cast<double>(xt) - static_cast<double>(m) - log(static_cast<double>(s));
+}
+
+// ---------------------------- log-probabilities ------------------------------
+// A workgroup per row: each thread keeps a running maximum and sum over its chunks, four at a time.
+template <bool F32>
+__global__ __launch_bounds__(256) void k_token_fwd(TokenArgs a) {
+  using R = Row<F32>;
+  constexpr int N = R::kN, U = 4;
+  __shared__ float red[4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t row = blockIdx.x, target = a.target[row];
+  const float ninf = -__builtin_inff();
+  if (target == a.ignore_index) {
+    if (tid == 0) a.out[row] = 0.0f;
+    return;
+  }
+  const R r(row, a.V);
+  float m = ninf, s = 0.0f;
+  auto add = [&](float top) {  // a new maximum
+    if (top > m) {
+      s *= __builtin_amdgcn_exp2f((m - top) * kLog2e);
+      m = top;
+    }
+  };
+  if (r.end_of(tid) >= 0) {
+    const float x = r.one(a.x, r.end_of(tid));
+    add(x);
+    s += __builtin_amdgcn_exp2f((x - (m == ninf ? 0.0f : m)) * kLog2e);
+  }
+#pragma unroll 1
+  for (int c = 0; c + tid < r.chunks; c += 256 * U) {
+    u32x4 x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) x[u] = r.load(a.x, true, c + 256 * u, tid);
+    float top = ninf;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      r.ends(x[u], c + 256 * u + tid);
+#pragma unroll
+      for (int e = 0; e < N; ++e) top = fmaxf(top, R::value(x[u], e));
+    }
+    add(top);
+    const float shift = m == ninf ? 0.0f : m;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < N; ++e) s += __builtin_amdgcn_exp2f((R::value(x[u], e) - shift) * kLog2e);
+  }
+  float top = wave_max(m);
+  if (lane == 0) red[wave] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  const float shift = top == ninf ? 0.0f : top;
+  __syncthreads();
+  // (a thread without a logit above -inf has m = -inf; its sum is 0, or NaN)
+  s = wave_sum(s * __builtin_amdgcn_exp2f(((m == ninf ? shift : m) - shift) * kLog2e));
+  if (lane == 0) red[wave] = s;
+  __syncthreads();
+  if (tid == 0) {
+    s = (red[0] + red[1]) + (red[2] + red[3]);
+    const bool in = target >= 0 && target < a.V;
+    const double l = in ? log_prob(r.one(a.x, static_cast<uint32_t>(target)), shift, s) : __builtin_nan("");
+    a.out[row] = static_cast<float>(a.reference != nullptr ? l - static_cast<double>(a.reference[row]) : l);
+    if (a.stats != nullptr) {
+      a.stats[2 * row] = shift;
+      a.stats[2 * row + 1] = s;
+    }
+  }
+}
+
+// The logits' gradient: a workgroup per row, four chunks of a thread in flight.
+template <bool F32>
+__global__ __launch_bounds__(256) void k_token_bwd(TokenArgs a) {
+  using R = Row<F32>;
+  constexpr int N = R::kN, U = 4;
+  const int tid = threadIdx.x;
+  const int64_t row = blockIdx.x, target = a.target[row];
+  const R r(row, a.V);
+  float g = 0.0f;
+  if (target != a.ignore_index) {
+    g = a.grad[row];
+    if (a.dloss != nullptr) g *= a.dloss[0];
+    if (target < 0 || target >= a.V) g = __builtin_nanf("");
+  }
+  g = uniform(g);
+  if (g == 0.0f) {
+    const float none[N] = {};
+    if (r.end_of(tid) >= 0) r.put(a.dx, r.end_of(tid), 0.0f);
+#pragma unroll 4
+    for (int c = 0; c + tid < r.chunks; c += 256) r.store(a.dx, c, tid, none);
+    return;
+  }
+  const float m = uniform(a.stats[2 * row]), f = uniform(-g / a.stats[2 * row + 1]);
+  auto grad = [&](float v) { return f * __builtin_amdgcn_exp2f((v - m) * kLog2e); };
+  const int at = static_cast<int>(target);  // (past V every element is NaN)
+  const int end = r.end_of(tid);
+  if (end >= 0) r.put(a.dx, end, grad(r.one(a.x, end)) + (end == at ? g : 0.0f));
+#pragma unroll 1
+  for (int c = 0; c + tid < r.chunks; c += 256 * U) {
+    u32x4 x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) x[u] = r.load(a.x, true, c + 256 * u, tid);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float v[N];
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[e] = grad(R::value(x[u], e));
+      const int k = at - r.head - (c + 256 * u + tid) * N;
+      if (static_cast<uint32_t>(k) < static_cast<uint32_t>(N)) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] += e == k ? g : 0.0f;
+      }
+      r.store(a.dx, c + 256 * u, tid, v);
+    }
+  }
+}
+
+// ---------------------------- preference pairs -------------------------------
+__device__ __forceinline__ double block_sum(double v, double* lds) {
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d, 64);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+  __syncthreads();
+  return (lds[0] + lds[1]) + (lds[2] + lds[3]);
+}
+
+// A workgroup per pair: the sums of both sequences (fp64, in a fixed order), the pair's loss, and
+// the slope of the mean for each of their rows.  The first and the last workgroup clear the rows
+// before and behind all sequences.  Starts are taken as their running maximum within the rows.
+__global__ __launch_bounds__(256) void k_pairs(PairArgs a) {
+  __shared__ double lds[4];
+  __shared__ long long most[4];
+  const int tid = threadIdx.x;
+  const int64_t pair = blockIdx.x;
+  auto start = [&](int64_t i) {
+    const int64_t x = a.starts64 ? static_cast<const int64_t*>(a.starts)[i * a.stride] : static_cast<const int32_t*>(a.starts)[i * a.stride];
+    return x < 0 ? int64_t(0) : x > a.rows ? a.rows : x;
+  };
+  long long first = 0;
+  for (int64_t i = tid; i <= 2 * pair; i += 256) first = max(first, static_cast<long long>(start(i)));
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) first = max(first, __shfl_xor(first, d, 64));
+  if ((tid & 63) == 0) most[tid >> 6] = first;
+  __syncthreads();
+  const int64_t e0 = max(max(most[0], most[1]), max(most[2], most[3]));
+  const int64_t e1 = max(e0, start(2 * pair + 1)), e2 = max(e1, start(2 * pair + 2));
+  double s0 = 0.0, s1 = 0.0;
+#pragma unroll 4
+  for (int64_t i = e0 + tid; i < e1; i += 256) s0 += static_cast<double>(a.gain[i]);
+#pragma unroll 4
+  for (int64_t i = e1 + tid; i < e2; i += 256) s1 += static_cast<double>(a.gain[i]);
+  s0 = block_sum(s0, lds);
+  s1 = block_sum(s1, lds);
+  const double beta = a.beta, eps = a.smoothing, delta = beta * (s0 - s1), away = exp(-fabs(delta));
+  // sigmoid(D) - (1 - e), of which both parts keep their digits where D is large
+  const double up = delta >= 0.0 ? 1.0 / (1.0 + away) : away / (1.0 + away), down = delta >= 0.0 ? away / (1.0 + away) : 1.0 / (1.0 + away);
+  const float slope = static_cast<float>(beta / static_cast<double>(a.n) * (eps * up - (1.0 - eps) * down));
+  if (tid == 0) {
+    const double soft = log1p(away);
+    // softplus(-D), softplus(D); of an infinite D times a factor of zero: nothing
+    const double low = (delta < 0.0 ? -delta : delta >= 0.0 ? 0.0 : delta) + soft, high = (delta > 0.0 ? delta : 0.0) + soft;
+    a.loss_pair[pair] = static_cast<float>((1.0 - eps) * low + (eps == 0.0 ? 0.0 : eps * high));
+    a.rewards[2 * pair] = static_cast<float>(beta * s0);
+    a.rewards[2 * pair + 1] = static_cast<float>(beta * s1);
+  }
+  for (int64_t i = e0 + tid; i < e1; i += 256) a.slope[i] = slope;
+  for (int64_t i = e1 + tid; i < e2; i += 256) a.slope[i] = -slope;
+  if (pair == 0)
+    for (int64_t i = tid; i < e0; i += 256) a.slope[i] = 0.0f;
+  if (pair == a.n - 1)
+    for (int64_t i = e2 + tid; i < a.rows; i += 256) a.slope[i] = 0.0f;
+}
+
+// The mean of n values: fp64 sums in a fixed order, by one workgroup of 1024.
+__device__ __forceinline__ void store_mean(const float* v, int64_t n, double count, float* out) {
+  __shared__ double s[1024];
+  double l = 0.0;
+#pragma unroll 4
+  for (int64_t r = threadIdx.x; r < n; r += 1024) l += static_cast<double>(v[r]);
+  s[threadIdx.x] = l;
+  __syncthreads();
+  for (int d = 512; d > 0; d >>= 1) {
+    if (static_cast<int>(threadIdx.x) < d) s[threadIdx.x] += s[threadIdx.x + d];
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) out[0] = static_cast<float>(s[0] / count);
+}
+
+__global__ __launch_bounds__(1024) void k_pairs_mean(PairArgs a) { store_mean(a.loss_pair, a.n, static_cast<double>(a.n), a.loss); }
+
+// ------------------------------- policy --------------------------------------
+__global__ __launch_bounds__(1024) void k_policy_count(PolicyArgs a) {
+  __shared__ int red[16];
+  int c = 0;
+#pragma unroll 8
+  for (int64_t r = threadIdx.x; r < a.rows; r += 1024) c += a.target[r] != a.ignore_index ? 1 : 0;
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) c += __shfl_xor(c, d, 64);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = c;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < 16; ++w) c += red[w];
+    a.count[0] = static_cast<float>(c);
+  }
+}
+
+// One row per workgroup at a time; NC chunks per thread in registers, any more are read again for
+// each walk.
+template <bool F32, int THREADS, int NC>
+__global__ __launch_bounds__(THREADS, 4) void k_policy(PolicyArgs a) {
+  using R = Row<F32>;
+  constexpr int N = R::kN, NW = THREADS / 64;
+  __shared__ float smax[NW], ssum[NW];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const float ninf = -__builtin_inff();
+  float scale = 1.0f;
+  if (a.dloss != nullptr) {
+    scale = a.dloss[0];
+    if (a.unless_one && scale == 1.0f) return;
+  }
+  scale = uniform(scale / a.count[0]);
+
+  u32x4 x[NC];
+  float xe;   // this thread's single element
+  int64_t target;
+  bool live;  // else the row has no part: no loss, no gradient, and nothing is read
+  auto head_of = [&](int64_t row) {
+    target = row < a.rows ? a.target[row] : a.ignore_index;
+    live = target != a.ignore_index;
+  };
+  head_of(blockIdx.x);
+  {
+    const R r(live ? blockIdx.x : 0, a.V);
+    xe = live && r.end_of(tid) >= 0 ? r.one(a.x, r.end_of(tid)) : ninf;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) x[i] = r.load(a.x, live, THREADS * i, tid);
+  }
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const R r(row, a.V);
+    const int64_t aim = target;
+    float m = live ? xe : 0.0f, g = 0.0f, f = 0.0f;  // the gradient of l, and the factor of the exponentials
+    if (live) {
+      const bool in = aim >= 0 && aim < a.V;
+      const float xt = in ? r.one(a.x, static_cast<uint32_t>(aim)) : __builtin_nanf("");
+      const float old = a.old[row], A = a.advantage[row], ref = a.reference != nullptr ? a.reference[row] : 0.0f;
+      auto walk = [&](auto f) {
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+          f(x[i]);
+          asm volatile("" : "+v"(x[i]));
+          __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll 1
+        for (int c = THREADS * NC; c + tid < r.chunks; c += THREADS) f(r.load(a.x, true, c, tid));
+      };
+#pragma unroll
+      for (int i = 0; i < NC; ++i) r.ends(x[i], tid + THREADS * i);
+      walk([&](const u32x4& c) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) m = fmaxf(m, R::value(c, e));
+      });
+      m = wave_max(m);
+      if (lane == 0) smax[wave] = m;
+      __syncthreads();
+      m = wave_max(smax[lane & (NW - 1)]);
+      m = uniform(m == ninf ? 0.0f : m);
+      float s = __builtin_amdgcn_exp2f((xe - m) * kLog2e);
+      walk([&](const u32x4& c) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) s += __builtin_amdgcn_exp2f((R::value(c, e) - m) * kLog2e);
+      });
+      s = wave_sum(s);
+      if (lane == 0) ssum[wave] = s;
+      __syncthreads();
+      s = uniform(wave_sum(lane < NW ? ssum[lane & (NW - 1)] : 0.0f));
+      const double l = log_prob(xt, m, s);
+      const float lo = 1.0f - a.low, hi = 1.0f + a.high, ratio = expf(static_cast<float>(l - static_cast<double>(old)));
+      const bool clamped = (A > 0.0f && ratio > hi) || (A < 0.0f && ratio < lo);
+      const float away = a.reference != nullptr ? static_cast<float>(static_cast<double>(ref) - l) : 0.0f;
+      const float odds = a.reference != nullptr ? expm1f(away) : 0.0f;
+      g = clamped ? 0.0f : -A * ratio;
+      if (a.reference != nullptr) g -= a.kl * odds;
+      if (a.loss_row != nullptr && tid == 0) {
+        float loss = -A * (clamped ? (A > 0.0f ? hi : lo) : ratio);
+        if (a.reference != nullptr) loss += a.kl * (odds - away);
+        a.loss_row[row] = loss;
+        a.logp[row] = static_cast<float>(l);
+      }
+      g = uniform(g * scale);
+      f = uniform(g == 0.0f ? 0.0f : -g / s);
+    } else if (a.loss_row != nullptr && tid == 0) {
+      a.loss_row[row] = 0.0f;
+      a.logp[row] = 0.0f;
+    }
+    const bool none = g == 0.0f;
+    auto grad = [&](const u32x4& c, int skip) {
+      float v[N] = {};
+      if (!none) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = f * __builtin_amdgcn_exp2f((R::value(c, e) - m) * kLog2e);
+        const int k = static_cast<int>(aim) - r.head - (skip + tid) * N;
+        if (static_cast<uint32_t>(k) < static_cast<uint32_t>(N)) {
+#pragma unroll
+          for (int e = 0; e < N; ++e) v[e] += e == k ? g : 0.0f;
+        }
+      }
+      r.store(a.dx, skip, tid, v);
+    };
+    if (a.dx != nullptr) {
+      const int end = r.end_of(tid);
+      if (end >= 0) r.put(a.dx, end, none ? 0.0f : f * __builtin_amdgcn_exp2f((xe - m) * kLog2e) + (end == static_cast<int>(aim) ? g : 0.0f));
+#pragma unroll 1
+      for (int c = THREADS * NC; c + tid < r.chunks; c += THREADS) grad(r.load(a.x, true, c, tid), c);
+    }
+    const int64_t next_row = row + gridDim.x;
+    head_of(next_row);
+    const R next(live ? next_row : row, a.V);
+    xe = live && next.end_of(tid) >= 0 ? next.one(a.x, next.end_of(tid)) : ninf;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      if (a.dx != nullptr) grad(x[i], THREADS * i);
+      x[i] = next.load(a.x, live, THREADS * i, tid);
+      __builtin_amdgcn_sched_barrier(0);  // (all loads at once would want registers of their own)
+    }
+  }
+}
+
+__global__ __launch_bounds__(1024) void k_policy_mean(PolicyArgs a) { store_mean(a.loss_row, a.rows, static_cast<double>(a.count[0]), a.loss); }
+
+template <bool F32, int THREADS, int NC>
+void launch_policy(const PolicyArgs& a, hipStream_t s) {
+  const int64_t most = 256 * ((NC > 4 ? 1024 : 1536) / THREADS);
+  hipLaunchKernelGGL((k_policy<F32, THREADS, NC>), dim3(static_cast<uint32_t>(a.rows < most ? a.rows : most)), dim3(THREADS), 0, s, a);
+}
+
+template <bool F32>
+void launch_policy(const PolicyArgs& a, hipStream_t s) {
+  const int64_t chunks = a.V / (F32 ? 4 : 8);
+  if (chunks <= 256) launch_policy<F32, 256, 1>(a, s);
+  else if (chunks <= 1024) launch_policy<F32, 256, 4>(a, s);
+  else if (chunks <= 4096 + 128) launch_policy<F32, 256, 16>(a, s);
+  else if (chunks <= 8192 + 256) launch_policy<F32, 512, 16>(a, s);
+  else launch_policy<F32, 1024, 16>(a, s);
+}
+
+bool rows_ok(int64_t rows, int64_t V) { return rows >= 1 && rows < int64_t(1) << 24 && V >= 1 && V <= int64_t(1) << 28; }
+int status() { return hipGetLastError() == hipSuccess ? 0 : -5; }
+
+}  // namespace
+}  // namespace compact
+
+using namespace compact;
+
+extern "C" {
+
+int compact_token_logprobs(const TokenArgs* a, void* stream) {
+  if (!rows_ok(a->rows, a->V)) return -1;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const dim3 grid(static_cast<uint32_t>(a->rows)), block(256);
+  if (a->backward) {
+    if (a->f32) hipLaunchKernelGGL((k_token_bwd<true>), grid, block, 0, s, *a);
+    else hipLaunchKernelGGL((k_token_bwd<false>), grid, block, 0, s, *a);
+  } else if (a->f32) {
+    hipLaunchKernelGGL((k_token_fwd<true>), grid, block, 0, s, *a);
+  } else {
+    hipLaunchKernelGGL((k_token_fwd<false>), grid, block, 0, s, *a);
+  }
+  return status();
+}
+
+int compact_preference_pairs(const PairArgs* a, void* stream) {
+  if (!rows_ok(a->rows, 1) || a->n < 1 || a->n >= int64_t(1) << 24) return -1;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  hipLaunchKernelGGL(k_pairs, dim3(static_cast<uint32_t>(a->n)), dim3(256), 0, s, *a);
+  hipLaunchKernelGGL(k_pairs_mean, dim3(1), dim3(1024), 0, s, *a);
+  return status();
+}
+
+int compact_policy(const PolicyArgs* a, void* stream) {
+  if (!rows_ok(a->rows, a->V) || !(a->low >= 0.0f) || !(a->high >= 0.0f)) return -1;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (!a->ready) hipLaunchKernelGGL(k_policy_count, dim3(1), dim3(1024), 0, s, *a);
+  if (a->f32) launch_policy<true>(*a, s);
+  else launch_policy<false>(*a, s);
+  if (a->loss_row != nullptr) hipLaunchKernelGGL(k_policy_mean, dim3(1), dim3(1024), 0, s, *a);
+  return status();
+}
+
+}  // extern "C"

@@ -1,5 +1,6 @@
 // Arguments of the kernels behind functional.py: rotary positions (rotary.hip),
-// attention with a window and sinks (attention.hip; packed.hip), distillation (distill.hip).
+// attention with a window and sinks (attention.hip; packed.hip), distillation (distill.hip); and
+// of those behind finetune.py (finetune.hip, clip.hip).
 // All pointers are device pointers; strides are in elements.  Entry points return
 // 0, -1 (a size they do not take) or -5 (HIP error).
 #pragma once
@@ -73,6 +74,59 @@ struct DistillArgs {
   int32_t unless_one;            // with dloss: nothing to do where that is 1
   int32_t ready;                 // entries, stats and count are those of an earlier call
   float temperature, weight;
+};
+
+// Log-probabilities of the rows' targets, and the logits' gradient from theirs.
+struct TokenArgs {
+  const void* x;                 // [rows][V] bf16 or fp32 (f32)
+  const int64_t* target;         // [rows]
+  const float* reference;        // [rows] taken off the log-probabilities, or NULL
+  float* out;                    // [rows]
+  float* stats;                  // [rows] pairs: the maximum, and the sum of exponentials beside it; forward: or NULL
+  const float* grad;             // backward: [rows], the gradient of `out`
+  const float* dloss;            // a factor of all of `grad`, or NULL
+  void* dx;
+  int64_t rows, V, ignore_index;
+  int32_t f32, backward;
+};
+
+// Pairs of sequences: their log-ratios' sums, the loss, and its gradient by row.
+struct PairArgs {
+  const float* gain;             // [rows] log-probabilities less the reference's
+  const void* starts;            // [2 n + 1] int64 (starts64) or int32, stride apart
+  float* rewards;                // [n][2]
+  float* slope;                  // [rows]
+  float* loss_pair;              // [n] scratch
+  float* loss;
+  int64_t stride, rows, n;
+  int32_t starts64;
+  float beta, smoothing;
+};
+
+// The clipped policy loss.
+struct PolicyArgs {
+  const void* x;                 // [rows][V] bf16 or fp32 (f32)
+  const int64_t* target;         // [rows]
+  const float *old, *advantage;  // [rows]
+  const float* reference;        // [rows], or NULL: no KL term
+  float* count;                  // rows that count
+  float* loss_row;               // [rows], or NULL: no loss
+  float* loss;                   // their mean
+  float* logp;                   // [rows], with loss_row
+  void* dx;                      // gradient of x, or NULL
+  const float* dloss;            // NULL: 1
+  int64_t rows, V, ignore_index;
+  int32_t f32;
+  int32_t unless_one;            // with dloss: nothing to do where that is 1
+  int32_t ready;                 // count is that of an earlier call
+  float low, high, kl;
+};
+
+// A tensor of compact_clip: dense, of bf16 or fp32 (f32).
+struct ClipTensor {
+  uint64_t at;
+  int64_t count;
+  int64_t f32;
 };
 
 }  // namespace compact
