@@ -61,15 +61,15 @@ __device__ __forceinline__ double one_square(uint64_t at, int64_t i) {
   return v * v;
 }
 
-// The tensor of this workgroup's piece, and the piece's number in it.
-__device__ __forceinline__ int tensor_of(const Tensors& t, uint32_t& piece) {
+// The tensor of piece `id` of a launch, and the piece's number in it.
+__device__ __forceinline__ int tensor_of(const Tensors& t, uint32_t id, uint32_t& piece) {
   int lo = 0, hi = t.tensors - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
-    if (t.first[mid] <= blockIdx.x) lo = mid;
+    if (t.first[mid] <= id) lo = mid;
     else hi = mid - 1;
   }
-  piece = blockIdx.x - t.first[lo];
+  piece = id - t.first[lo];
   return lo;
 }
 
@@ -105,7 +105,7 @@ __device__ __forceinline__ double block_sum(double v, double* lds) {
 __global__ __launch_bounds__(256) void k_norm_pieces(Tensors t, double* part) {
   __shared__ double lds[4];
   uint32_t piece;
-  const int i = tensor_of(t, piece);
+  const int i = tensor_of(t, blockIdx.x, piece);
   const int64_t count = t.count[i] >> 1;
   double s = t.count[i] & 1 ? piece_sum<true>(t.at[i], count, piece) : piece_sum<false>(t.at[i], count, piece);
   s = block_sum(s, lds);
@@ -154,31 +154,36 @@ __device__ __forceinline__ void scale_piece(uint64_t at, int64_t count, uint32_t
 __global__ __launch_bounds__(256) void k_clip_pieces(Tensors t, const float* norm) {
   const float f = norm[1];
   if (f == 1.0f) return;
-  uint32_t piece;
-  const int i = tensor_of(t, piece);
+  uint32_t piece;  // the last ones first: what the norm read last may still be in the cache
+  const int i = tensor_of(t, gridDim.x - 1 - blockIdx.x, piece);
   const int64_t count = t.count[i] >> 1;
   if (t.count[i] & 1) scale_piece<true>(t.at[i], count, piece, f);
   else scale_piece<false>(t.at[i], count, piece, f);
 }
 
-// f(table, grid) for each launch.
+// Entry i of the list joins a launch's table.
+void append(Tensors& t, const ClipTensor& e, uint32_t& grid) {
+  t.at[t.tensors] = e.at;
+  t.count[t.tensors] = e.count * 2 + (e.f32 ? 1 : 0);
+  t.first[t.tensors++] = grid;
+  grid += static_cast<uint32_t>(pieces_of(e.at, e.count, e.f32 != 0));
+}
+
+// f(table, grid) for each launch: of kMostTensors entries from i0 on, forward or from the list's
+// end.  (Entries without elements are those that were given twice.)
 template <typename F>
-void for_tables(const ClipTensor* list, int64_t n, F f) {
-  Tensors t = {};
-  uint32_t grid = 0, piece0 = 0;
-  for (int64_t i = 0; i < n; ++i) {
-    const uint32_t pieces = static_cast<uint32_t>(pieces_of(list[i].at, list[i].count, list[i].f32 != 0));
-    t.at[t.tensors] = list[i].at;
-    t.count[t.tensors] = list[i].count * 2 + (list[i].f32 ? 1 : 0);
-    t.first[t.tensors++] = grid;
-    grid += pieces;
-    if (t.tensors == kMostTensors || i == n - 1) {
-      t.piece0 = piece0;
-      f(t, grid);
-      piece0 += grid;
-      t.tensors = 0;
-      grid = 0;
-    }
+void for_tables(const ClipTensor* list, int64_t n, bool backward, F f) {
+  const int64_t tables = ceil_div(n, kMostTensors);
+  uint32_t piece0 = 0;
+  for (int64_t k = 0; k < tables; ++k) {
+    const int64_t i0 = (backward ? tables - 1 - k : k) * kMostTensors, i1 = i0 + kMostTensors < n ? i0 + kMostTensors : n;
+    Tensors t = {};
+    uint32_t grid = 0;
+    for (int64_t i = i0; i < i1; ++i)
+      if (list[i].count > 0) append(t, list[i], grid);
+    t.piece0 = piece0;
+    piece0 += grid;
+    if (grid > 0) f(t, grid);
   }
 }
 
@@ -189,33 +194,41 @@ using namespace compact;
 
 extern "C" {
 
-// The pieces that compact_clip has sums of.  `order`: room for n indexes.  -1: sizes it does not
-// take; -2: two tensors overlap.
-int64_t compact_clip_pieces(const ClipTensor* list, int64_t n, int64_t* order) {
-  int64_t pieces = 0;
+// The pieces that compact_clip has sums of.  A tensor that is given twice keeps its elements in one
+// of its entries.  `order`: room for n indexes.  -1: sizes it does not take; -2: two tensors overlap.
+int64_t compact_clip_pieces(ClipTensor* list, int64_t n, int64_t* order) {
   for (int64_t i = 0; i < n; ++i) {
-    if (list[i].count < 1 || list[i].count >= int64_t(1) << 40 || list[i].at % (list[i].f32 ? 4 : 2) != 0) return -1;
-    pieces += pieces_of(list[i].at, list[i].count, list[i].f32 != 0);
+    if (list[i].count < 0 || list[i].count >= int64_t(1) << 40 || list[i].at % (list[i].f32 ? 4 : 2) != 0) return -1;
     order[i] = i;
   }
-  if (pieces >= int64_t(1) << 24) return -1;  // (a launch has under 2^32 threads)
-  std::sort(order, order + n, [&](int64_t a, int64_t b) { return list[a].at < list[b].at; });
-  for (int64_t i = 1; i < n; ++i) {
-    const ClipTensor& before = list[order[i - 1]];
-    if (before.at + static_cast<uint64_t>(before.count) * (before.f32 ? 4 : 2) > list[order[i]].at) return -2;
+  std::sort(order, order + n, [&](int64_t a, int64_t b) { return list[a].at != list[b].at ? list[a].at < list[b].at : a < b; });
+  int64_t pieces = 0, last = -1;
+  for (int64_t i = 0; i < n; ++i) {
+    ClipTensor& t = list[order[i]];
+    if (t.count == 0) continue;
+    if (last >= 0) {
+      const ClipTensor& before = list[last];
+      if (t.at == before.at && t.count == before.count && t.f32 == before.f32) {
+        t.count = 0;
+        continue;
+      }
+      if (before.at + static_cast<uint64_t>(before.count) * (before.f32 ? 4 : 2) > t.at) return -2;
+    }
+    pieces += pieces_of(t.at, t.count, t.f32 != 0);
+    last = order[i];
   }
-  return pieces;
+  return pieces < int64_t(1) << 24 ? pieces : -1;  // (a launch has under 2^32 threads)
 }
 
 // out: the norm and the factor.  bounded: whether the tensors are scaled.
 int compact_clip(const ClipTensor* list, int64_t n, double most, int bounded, double* part, int64_t pieces, float* out, void* stream) {
   hipStream_t s = static_cast<hipStream_t>(stream);
-  for_tables(list, n, [&](const Tensors& t, uint32_t grid) {
+  for_tables(list, n, false, [&](const Tensors& t, uint32_t grid) {
     hipLaunchKernelGGL(k_norm_pieces, dim3(grid), dim3(256), 0, s, t, part);
   });
   hipLaunchKernelGGL(k_norm, dim3(1), dim3(1024), 0, s, part, pieces, bounded ? most : __builtin_inf(), out);
   if (bounded)
-    for_tables(list, n, [&](const Tensors& t, uint32_t grid) { hipLaunchKernelGGL(k_clip_pieces, dim3(grid), dim3(256), 0, s, t, out); });
+    for_tables(list, n, true, [&](const Tensors& t, uint32_t grid) { hipLaunchKernelGGL(k_clip_pieces, dim3(grid), dim3(256), 0, s, t, out); });
   return hipGetLastError() == hipSuccess ? 0 : -5;
 }
 

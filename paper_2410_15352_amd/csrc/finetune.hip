@@ -148,60 +148,83 @@ __global__ __launch_bounds__(256) void k_token_bwd(TokenArgs a) {
 }
 
 // ---------------------------- preference pairs -------------------------------
-__device__ __forceinline__ double block_sum(double v, double* lds) {
+// THREADS threads per pair (a wave, or a workgroup of 256): the sums of both sequences (fp64, in a
+// fixed order), the pair's loss, and the slope of the mean for each of their rows.  The first and
+// the last pair clear the rows before and behind all sequences.  Starts are taken as their running
+// maximum within the rows.  lds: room for 4 numbers of 64 bits.
+template <int THREADS, typename T, typename F>
+__device__ __forceinline__ T joined(T v, T* lds, F join) {
 #pragma unroll
-  for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d, 64);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-  __syncthreads();
-  return (lds[0] + lds[1]) + (lds[2] + lds[3]);
+  for (int d = 32; d > 0; d >>= 1) v = join(v, __shfl_xor(v, d, 64));
+  if constexpr (THREADS > 64) {
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = join(join(lds[0], lds[1]), join(lds[2], lds[3]));
+  }
+  return v;
 }
 
-// A workgroup per pair: the sums of both sequences (fp64, in a fixed order), the pair's loss, and
-// the slope of the mean for each of their rows.  The first and the last workgroup clear the rows
-// before and behind all sequences.  Starts are taken as their running maximum within the rows.
-__global__ __launch_bounds__(256) void k_pairs(PairArgs a) {
-  __shared__ double lds[4];
-  __shared__ long long most[4];
-  const int tid = threadIdx.x;
-  const int64_t pair = blockIdx.x;
+template <int THREADS>
+__device__ __forceinline__ double pair_loss(const PairArgs& a, int64_t pair, int tid, double* lds) {
   auto start = [&](int64_t i) {
     const int64_t x = a.starts64 ? static_cast<const int64_t*>(a.starts)[i * a.stride] : static_cast<const int32_t*>(a.starts)[i * a.stride];
-    return x < 0 ? int64_t(0) : x > a.rows ? a.rows : x;
+    return static_cast<long long>(x < 0 ? 0 : x > a.rows ? a.rows : x);
   };
+  const auto add = [](double x, double y) { return x + y; };
   long long first = 0;
-  for (int64_t i = tid; i <= 2 * pair; i += 256) first = max(first, static_cast<long long>(start(i)));
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) first = max(first, __shfl_xor(first, d, 64));
-  if ((tid & 63) == 0) most[tid >> 6] = first;
-  __syncthreads();
-  const int64_t e0 = max(max(most[0], most[1]), max(most[2], most[3]));
-  const int64_t e1 = max(e0, start(2 * pair + 1)), e2 = max(e1, start(2 * pair + 2));
+  for (int64_t i = tid; i <= 2 * pair; i += THREADS) first = max(first, start(i));
+  const int64_t e0 = joined<THREADS>(first, reinterpret_cast<long long*>(lds), [](long long x, long long y) { return max(x, y); });
+  const int64_t e1 = max(static_cast<long long>(e0), start(2 * pair + 1)), e2 = max(static_cast<long long>(e1), start(2 * pair + 2));
   double s0 = 0.0, s1 = 0.0;
 #pragma unroll 4
-  for (int64_t i = e0 + tid; i < e1; i += 256) s0 += static_cast<double>(a.gain[i]);
+  for (int64_t i = e0 + tid; i < e1; i += THREADS) s0 += static_cast<double>(a.gain[i]);
 #pragma unroll 4
-  for (int64_t i = e1 + tid; i < e2; i += 256) s1 += static_cast<double>(a.gain[i]);
-  s0 = block_sum(s0, lds);
-  s1 = block_sum(s1, lds);
+  for (int64_t i = e1 + tid; i < e2; i += THREADS) s1 += static_cast<double>(a.gain[i]);
+  s0 = joined<THREADS>(s0, lds, add);
+  s1 = joined<THREADS>(s1, lds, add);
   const double beta = a.beta, eps = a.smoothing, delta = beta * (s0 - s1), away = exp(-fabs(delta));
   // sigmoid(D) - (1 - e), of which both parts keep their digits where D is large
   const double up = delta >= 0.0 ? 1.0 / (1.0 + away) : away / (1.0 + away), down = delta >= 0.0 ? away / (1.0 + away) : 1.0 / (1.0 + away);
   const float slope = static_cast<float>(beta / static_cast<double>(a.n) * (eps * up - (1.0 - eps) * down));
+  for (int64_t i = e0 + tid; i < e1; i += THREADS) a.slope[i] = slope;
+  for (int64_t i = e1 + tid; i < e2; i += THREADS) a.slope[i] = -slope;
+  if (pair == 0)
+    for (int64_t i = tid; i < e0; i += THREADS) a.slope[i] = 0.0f;
+  if (pair == a.n - 1)
+    for (int64_t i = e2 + tid; i < a.rows; i += THREADS) a.slope[i] = 0.0f;
   if (tid == 0) {
-    const double soft = log1p(away);
-    // softplus(-D), softplus(D); of an infinite D times a factor of zero: nothing
-    const double low = (delta < 0.0 ? -delta : delta >= 0.0 ? 0.0 : delta) + soft, high = (delta > 0.0 ? delta : 0.0) + soft;
-    a.loss_pair[pair] = static_cast<float>((1.0 - eps) * low + (eps == 0.0 ? 0.0 : eps * high));
     a.rewards[2 * pair] = static_cast<float>(beta * s0);
     a.rewards[2 * pair + 1] = static_cast<float>(beta * s1);
   }
-  for (int64_t i = e0 + tid; i < e1; i += 256) a.slope[i] = slope;
-  for (int64_t i = e1 + tid; i < e2; i += 256) a.slope[i] = -slope;
-  if (pair == 0)
-    for (int64_t i = tid; i < e0; i += 256) a.slope[i] = 0.0f;
-  if (pair == a.n - 1)
-    for (int64_t i = e2 + tid; i < a.rows; i += 256) a.slope[i] = 0.0f;
+  // softplus(-D), softplus(D); of an infinite D times a factor of zero: nothing
+  const double soft = log1p(away);
+  const double low = (delta < 0.0 ? -delta : delta >= 0.0 ? 0.0 : delta) + soft, high = (delta > 0.0 ? delta : 0.0) + soft;
+  return (1.0 - eps) * low + (eps == 0.0 ? 0.0 : eps * high);
+}
+
+__global__ __launch_bounds__(256) void k_pairs(PairArgs a) {
+  __shared__ double lds[4];
+  const double loss = pair_loss<256>(a, blockIdx.x, threadIdx.x, lds);
+  if (threadIdx.x == 0) a.loss_pair[blockIdx.x] = static_cast<float>(loss);
+}
+
+// A few pairs: a wave each, and their mean, in one workgroup.
+constexpr int kFewPairs = 64;
+constexpr int64_t kFewPairRows = 32768;
+__global__ __launch_bounds__(1024) void k_few_pairs(PairArgs a) {
+  __shared__ double loss[kFewPairs];
+  const int lane = threadIdx.x & 63;
+  for (int pair = threadIdx.x >> 6; pair < a.n; pair += 16) {
+    const double v = pair_loss<64>(a, pair, lane, nullptr);
+    if (lane == 0) loss[pair] = v;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    double s = 0.0;
+    for (int pair = 0; pair < a.n; ++pair) s += loss[pair];
+    a.loss[0] = static_cast<float>(s / static_cast<double>(a.n));
+  }
 }
 
 // The mean of n values: fp64 sums in a fixed order, by one workgroup of 1024.
@@ -404,6 +427,10 @@ int compact_token_logprobs(const TokenArgs* a, void* stream) {
 int compact_preference_pairs(const PairArgs* a, void* stream) {
   if (!rows_ok(a->rows, 1) || a->n < 1 || a->n >= int64_t(1) << 24) return -1;
   hipStream_t s = static_cast<hipStream_t>(stream);
+  if (a->n <= kFewPairs && a->rows <= kFewPairRows) {
+    hipLaunchKernelGGL(k_few_pairs, dim3(1), dim3(1024), 0, s, *a);
+    return status();
+  }
   hipLaunchKernelGGL(k_pairs, dim3(static_cast<uint32_t>(a->n)), dim3(256), 0, s, *a);
   hipLaunchKernelGGL(k_pairs_mean, dim3(1), dim3(1024), 0, s, *a);
   return status();

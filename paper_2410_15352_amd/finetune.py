@@ -18,13 +18,14 @@ import ctypes
 import math
 import struct
 from array import array
+from itertools import chain
 
 import torch
 
 from . import _block_ops as ops
 from . import _lib
 from ._block_ops import IGNORE, _eager, _i64, _plain, _stream, _vp
-from .functional import _block, _bounds, _here, _tracked
+from .functional import _block, _bounds, _device_now, _here, _tracked
 
 __all__ = ["token_logprobs", "preference_loss", "policy_loss", "clip_grad_norm"]
 
@@ -406,16 +407,34 @@ def _clip_pieces(entries, n):
 _fns = {}
 
 
-def _clip_apply(tensors, max_norm):
-    """Dense bf16 and fp32 tensors of the current device."""
-    entries = array("Q", [x for t in tensors for x in (t.data_ptr(), t.numel(), _CLIP_KINDS[t.dtype])])
-    at, n = entries.buffer_info()[0], len(tensors)
+# Asked of many tensors, by calls that map makes: a loop in Python takes three times as long.
+_pointers, _numels, _devices, _dtypes, _dense_all = (
+    _Tensor.data_ptr, _Tensor.numel, _Tensor.get_device, _Tensor.dtype.__get__, _Tensor.is_contiguous)
+
+
+def _clip_entries(tensors):
+    """Addresses, elements and kinds of dense bf16 and fp32 tensors of the current GPU; None of others."""
+    if not set(map(type, tensors)).issubset(ops._TYPES):
+        return None
+    at = set(map(_devices, tensors))  # -1: the CPU
+    if len(at) != 1 or min(at) < 0 or at != {_device_now()}:
+        return None
+    try:
+        at, kinds = map(_pointers, tensors), [_CLIP_KINDS[d] for d in map(_dtypes, tensors)]
+        entries = array("Q", chain.from_iterable(zip(at, map(_numels, tensors), kinds)))
+    except (KeyError, RuntimeError):  # another type; a tensor that wraps another has no pointer
+        return None
+    return entries if all(map(_dense_all, tensors)) else None
+
+
+def _clip_apply(entries, device, max_norm):
+    at, n = entries.buffer_info()[0], len(entries) // 3
     pieces = _clip_pieces(at, n)
     if pieces == -2:
         raise ValueError("clip_grad_norm: two of the tensors overlap")
     if pieces < 0:
         return None
-    scratch = torch.empty(pieces + 1, dtype=torch.float64, device=tensors[0].device)
+    scratch = torch.empty(pieces + 1, dtype=torch.float64, device=device)
     out = scratch[pieces:].view(_f32)
     ops._call("compact_clip", at, n, 0.0 if max_norm is None else max_norm, max_norm is not None, scratch.data_ptr(), pieces,
               out.data_ptr(), _stream(scratch))
@@ -444,30 +463,41 @@ def clip_grad_norm(tensors, max_norm=None):
             raise ValueError("clip_grad_norm: max_norm >= 0")
         if math.isinf(max_norm):
             max_norm = None
+    entries = _clip_entries(given) if given and _eager() else None
+    if entries is not None:
+        norm = _clip_apply(entries, given[0].device, max_norm)
+        if norm is not None:
+            if max_norm is not None:
+                _changed(given)
+            return norm
     for t in given:
         if not isinstance(t, _Tensor) or not t.is_floating_point() or t.layout != torch.strided:
             raise TypeError("clip_grad_norm: dense floating tensors")
     device = given[0].device if given else None
     if any(t.device != device for t in given):
         raise ValueError("clip_grad_norm: tensors of one device")
-    unique = list({(t.data_ptr(), t.shape, t.stride(), t.dtype): t for t in given if t.numel() > 0}.values()) if _addressable(given) else given
-    if max_norm is not None and any(not t.is_contiguous() and torch._debug_has_internal_overlap(t) == 1 for t in unique):
+    given = [t for t in given if t.numel() > 0]
+    if all(map(_plain, given)):
+        given = list({(t.data_ptr(), t.shape, t.stride(), t.dtype): t for t in given}.values())
+    if max_norm is not None and any(not t.is_contiguous() and torch._debug_has_internal_overlap(t) == 1 for t in given):
         raise ValueError("clip_grad_norm: a tensor whose elements lie on one another is not scaled")
-    if unique and _eager() and unique[0].is_cuda and all(t.dtype in _CLIP_KINDS and _here(t) for t in unique):
-        dense = [t if t.is_contiguous() else _flat(t) for t in unique]
-        norm = _clip_apply(dense, max_norm)
+    if given and _eager():
+        dense = [t if t.is_contiguous() else _flat(t) for t in given]
+        entries = _clip_entries(dense)
+        norm = None if entries is None else _clip_apply(entries, device, max_norm)
         if norm is not None:
             if max_norm is not None:
-                for t, d in zip(unique, dense):
-                    if d is not t and d.data_ptr() != t.data_ptr():
+                for t, d in zip(given, dense):
+                    if d.data_ptr() != t.data_ptr():
                         t.copy_(d)
-                torch.autograd.graph.increment_version([t for t in unique if not t.is_inference()])
+                _changed(given)
             return norm
-    return _clip_torch(unique, max_norm, device)
+    return _clip_torch(given, max_norm, device)
 
 
-def _addressable(tensors):
-    return all(_plain(t) for t in tensors)
+def _changed(tensors):
+    """Whoever saved them is told."""
+    torch.autograd.graph.increment_version([t for t in tensors if not t.is_inference()])
 
 
 def _flat(t):

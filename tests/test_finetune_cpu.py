@@ -301,13 +301,19 @@ def test_recorded_backward(launches, which):
 def test_clip_entries(monkeypatch):
     """What the launches are told of each tensor: address, elements, kind; views in any order of dimensions as they are."""
     calls = []
-    monkeypatch.setattr(FT, "_here", FT._plain)
+    monkeypatch.setattr(FT, "_devices", lambda t: 0)
+    monkeypatch.setattr(FT, "_device_now", lambda: 0)
     monkeypatch.setattr(FT, "_stream", lambda t: 0)
     monkeypatch.setattr(FT, "_clip_pieces", lambda at, n: n)
     monkeypatch.setattr(FT.ops, "_call", lambda name, at, n, *a: calls.append((name, (FT.ctypes.c_uint64 * (3 * n)).from_address(at)[:], a)))
     t = [_rand(4, 6, dtype=bf16), _rand(4, 6, dtype=f32).t(), _rand(3, dtype=f32), _rand(4, 6, dtype=f32)[:, :5]]
-    FT._clip_apply([FT._flat(x) if not x.is_contiguous() else x for x in t], 1.0)
+    was = t[3].clone()
+    FT.clip_grad_norm([*t, None], 1.0)
     name, entries, rest = calls[0]
     assert name == "compact_clip" and rest[:2] == (1.0, True)
     assert entries[:9] == [t[0].data_ptr(), 24, 0, t[1].data_ptr(), 24, 1, t[2].data_ptr(), 3, 1]
-    assert entries[9] != t[3].data_ptr() and entries[10:] == [20, 1]
+    assert entries[9] != t[3].data_ptr() and entries[10:] == [20, 1] and torch.equal(t[3], was)
+    FT.clip_grad_norm([t[0], t[2]])
+    assert calls[1][1] == [t[0].data_ptr(), 24, 0, t[2].data_ptr(), 3, 1] and calls[1][2][:2] == (0.0, False)
+    FT.clip_grad_norm([t[0], t[2].half()], 1.0)
+    assert len(calls) == 2
