@@ -57,9 +57,11 @@ struct Tile {
     else return (r >> 2) & 3;
   }
   static __device__ __forceinline__ int at(int r, int c) { return r * (HD * 2) + ((c ^ swz(r)) * 16); }
-  // rows r0 + lane mod 32, the 8 columns 16 s + 8 (lane / 32)
+  // rows r0 + lane mod 32, the 8 columns 16 s + 8 (lane / 32).  (Here and below r0 is a multiple of 16,
+  // which swz does not see: added behind it, it is a constant of the reading instruction and wants
+  // no register.)
   static __device__ __forceinline__ u32x4 row_frag(const char* t, int r0, int s, int lane) {
-    return *reinterpret_cast<const u32x4*>(t + at(r0 + (lane & 31), 2 * s + (lane >> 5)));
+    return *reinterpret_cast<const u32x4*>(t + at(lane & 31, 2 * s + (lane >> 5)) + r0 * (HD * 2));
   }
   // column 32 d + lane mod 32 of the rows r0 + 4 h + (0..3), r0 + 8 + 4 h + (0..3), h = lane / 32.
   // In a 16-lane group the transposing read hands output lane t, element j, the element
@@ -70,9 +72,9 @@ struct Tile {
     u32x4 out;
 #pragma unroll
     for (int hh = 0; hh < 2; ++hh) {
-      const int r = r0 + 4 * (g >> 1) + 8 * hh + j;
+      const int r = 4 * (g >> 1) + 8 * hh + j;
       const bf16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
-          (lds_bf16x4*)(const_cast<char*>(t) + at(r, c) + 8 * (q & 1)));
+          (lds_bf16x4*)(const_cast<char*>(t) + at(r, c) + 8 * (q & 1) + r0 * (HD * 2)));
       const u32x2 w = __builtin_bit_cast(u32x2, v);
       out[2 * hh] = w.x;
       out[2 * hh + 1] = w.y;
@@ -199,6 +201,24 @@ __device__ __forceinline__ f32x16 zero16() {
 #pragma unroll
   for (int v = 0; v < 16; ++v) z[v] = 0.0f;
   return z;
+}
+
+// N products in order, use(i, factor), of factors that are read from LDS, AHEAD of them on their
+// way.  (Left alone the compiler reads each factor right before its product, which then waits for
+// LDS every time.)  Only vector and scalar arithmetic may be moved across a product's place.
+template <int N, int AHEAD, typename Read, typename Use>
+__device__ __forceinline__ void products(Read read, Use use) {
+  constexpr int kArithmetic = 0x2 | 0x4 | 0x400;
+  decltype(read(0)) f[AHEAD];
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) f[i] = read(i);
+  __builtin_amdgcn_sched_barrier(kArithmetic);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    use(i, f[i % AHEAD]);
+    if (i + AHEAD < N) f[i % AHEAD] = read(i + AHEAD);
+    __builtin_amdgcn_sched_barrier(kArithmetic);
+  }
 }
 
 // Row (of 32) of element v of a result: 8 (v / 4) + 4 (lane / 32) + v mod 4.
@@ -466,12 +486,9 @@ __device__ __forceinline__ bool attn_fwd(const AttnArgs& a, const Span<PACKED>& 
     const int j0 = walk.key(t);
     if (w0 > last || none_seen(j0, kBN, pmin, pmax, a.window, a.sinks)) return;
     f32x16 s[2];
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-      s[kb] = zero16();
-#pragma unroll
-      for (int st = 0; st < KS; ++st) s[kb] = mfma32x32x16(Tile<HD>::row_frag(now.k, 32 * kb, st, lane), qf[st], s[kb]);
-    }
+    s[0] = s[1] = zero16();
+    products<2 * KS, 4>([&](int i) { return Tile<HD>::row_frag(now.k, 32 * (i & 1), i >> 1, lane); },
+                        [&](int i, const u32x4& f) { s[i & 1] = mfma32x32x16(f, qf[i >> 1], s[i & 1]); });
     if (!all_seen(j0, kBN, pmin, pmax, a.window, a.sinks)) {
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
@@ -497,11 +514,9 @@ __device__ __forceinline__ bool attn_fwd(const AttnArgs& a, const Span<PACKED>& 
       pf[2 * kb] = two[0];
       pf[2 * kb + 1] = two[1];
     }
-#pragma unroll
-    for (int st = 0; st < 4; ++st)
-#pragma unroll
-      for (int d = 0; d < HD / 32; ++d)
-        sm.o[d] = mfma32x32x16(Tile<HD>::col_frag(now.v, 16 * st, d, lane), pf[st], sm.o[d]);
+    constexpr int ND = HD / 32;
+    products<4 * ND, 4>([&](int i) { return Tile<HD>::col_frag(now.v, 16 * (i / ND), i % ND, lane); },
+                        [&](int i, const u32x4& f) { sm.o[i % ND] = mfma32x32x16(f, pf[i / ND], sm.o[i % ND]); });
   };
   for (int t = t0; t < t1; t += 2) {
     step(t, even, odd);
@@ -544,6 +559,8 @@ __device__ __forceinline__ bool attn_fwd(const AttnArgs& a, const Span<PACKED>& 
 // 970 TFLOP/s of its three products, at 16384 rows, 16 heads on 4 of 128, window 4096; 24 us at
 // 32 x 256 rows, 8 heads of 64, window 128.  (Three waves to a SIMD at heads of 64, with places
 // in LDS formed for each tile: 352 us with the other gradients for 344.)
+constexpr int kDqAhead = 4, kDkvAhead = 2;
+
 template <int HD, bool FINE, bool PACKED>
 __device__ __forceinline__ bool attn_dq(const AttnGradArgs& ga, const Span<PACKED>& sp, TilePair<HD>& even, TilePair<HD>& odd,
                                         int* bad_key, int h, int q0, int mode) {
@@ -610,11 +627,11 @@ __device__ __forceinline__ bool attn_dq(const AttnGradArgs& ga, const Span<PACKE
 #pragma unroll kUnroll
     for (int kb = 0; kb < 2; ++kb) {
       f32x16 s = zero16(), dp = zero16();
-#pragma unroll
-      for (int st = 0; st < KS; ++st) {
-        s = mfma32x32x16(Tile<HD>::row_frag(now.k, 32 * kb, st, lane), qf[st], s);
-        dp = mfma32x32x16(Tile<HD>::row_frag(now.v, 32 * kb, st, lane), gf[st], dp);
-      }
+      products<2 * KS, kDqAhead>([&](int i) { return Tile<HD>::row_frag(i & 1 ? now.v : now.k, 32 * kb, i >> 1, lane); },
+                                 [&](int i, const u32x4& f) {
+                                   if (i & 1) dp = mfma32x32x16(f, gf[i >> 1], dp);
+                                   else s = mfma32x32x16(f, qf[i >> 1], s);
+                                 });
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[e] = exp2_fast(__builtin_fmaf(s[e], c, -lse)) * (dp[e] - delta);
       if (edge) {
@@ -627,14 +644,12 @@ __device__ __forceinline__ bool attn_dq(const AttnGradArgs& ga, const Span<PACKE
       u32x4 ds[2], dr[2];
       pack_steps(s, ds);
       if constexpr (FINE) pack_rest(s, ds, dr);
-#pragma unroll
-      for (int st = 0; st < 2; ++st)
-#pragma unroll
-        for (int d = 0; d < HD / 32; ++d) {
-          const u32x4 kf = Tile<HD>::col_frag(now.k, 32 * kb + 16 * st, d, lane);
-          dq[d] = mfma32x32x16(kf, ds[st], dq[d]);
-          if constexpr (FINE) dq[d] = mfma32x32x16(kf, dr[st], dq[d]);
-        }
+      constexpr int ND = HD / 32;
+      products<2 * ND, kDqAhead>([&](int i) { return Tile<HD>::col_frag(now.k, 32 * kb + 16 * (i / ND), i % ND, lane); },
+                                 [&](int i, const u32x4& f) {
+                                   dq[i % ND] = mfma32x32x16(f, ds[i / ND], dq[i % ND]);
+                                   if constexpr (FINE) dq[i % ND] = mfma32x32x16(f, dr[i / ND], dq[i % ND]);
+                                 });
     }
   };
   for (int t = 0; t < walk.count; t += 2) {
@@ -709,8 +724,8 @@ __device__ __forceinline__ bool attn_dkv(const AttnGradArgs& ga, const Span<PACK
   constexpr int KS = HD / 16;
   constexpr bool SHARED = shared_keys(HD);
   const AttnArgs& a = ga.f;
-  int tid = threadIdx.x;
-  if constexpr (PACKED) asm volatile("" : "+v"(tid));
+  int tid = threadIdx.x;  // (places formed anew for each walk: kept for the second, which hardly ever comes, they spill)
+  asm volatile("" : "+v"(tid));
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), G = a.heads / a.kv;
   const int hk = job.bk % a.kv, lq = sp.rows, L = sp.L, off = L - lq;
   const bool far = job.far != 0, halves = SHARED || far;  // a wave has one half of each tile's rows
@@ -793,18 +808,25 @@ __device__ __forceinline__ bool attn_dkv(const AttnGradArgs& ga, const Span<PACK
       const bool all = far ? w0 + 31 < a.sinks && pmin - (w0 + 31) >= a.window : w0 + 31 <= pmin && pmax - w0 < a.window;
       const bool edge = mode != kPlain || i1st + 31 >= lq || w0 + 31 > kl || !all;
       f32x16 s = zero16(), dp = zero16();
-#pragma unroll
-      for (int st = 0; st < KS; ++st) {
-        u32x4 k1, v1;
-        if constexpr (SHARED) {
-          k1 = Tile<HD>::row_frag(keys.k[kw >> 1], 32 * (kw & 1), st, lane);
-          v1 = Tile<HD>::row_frag(keys.v[kw >> 1], 32 * (kw & 1), st, lane);
-        } else {
-          k1 = kf[st];
-          v1 = vf[st];
-        }
-        s = mfma32x32x16(Tile<HD>::row_frag(now.q, 32 * qb, st, ln), k1, s);
-        dp = mfma32x32x16(Tile<HD>::row_frag(now.g, 32 * qb, st, ln), v1, dp);
+      if constexpr (SHARED) {
+        struct Pair {
+          u32x4 row, key;
+        };
+        products<2 * KS, kDkvAhead>(
+            [&](int i) {
+              return Pair{Tile<HD>::row_frag(i & 1 ? now.g : now.q, 32 * qb, i >> 1, ln),
+                          Tile<HD>::row_frag(i & 1 ? keys.v[kw >> 1] : keys.k[kw >> 1], 32 * (kw & 1), i >> 1, lane)};
+            },
+            [&](int i, const Pair& f) {
+              if (i & 1) dp = mfma32x32x16(f.row, f.key, dp);
+              else s = mfma32x32x16(f.row, f.key, s);
+            });
+      } else {
+        products<2 * KS, 2 * kDkvAhead>([&](int i) { return Tile<HD>::row_frag(i & 1 ? now.g : now.q, 32 * qb, i >> 1, ln); },
+                                        [&](int i, const u32x4& f) {
+                                          if (i & 1) dp = mfma32x32x16(f, vf[i >> 1], dp);
+                                          else s = mfma32x32x16(f, kf[i >> 1], s);
+                                        });
       }
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
@@ -831,15 +853,18 @@ __device__ __forceinline__ bool attn_dkv(const AttnGradArgs& ga, const Span<PACK
       pack_steps(dp, df);
       u32x4 dr[2];
       if constexpr (FINE) pack_rest(dp, df, dr);
-#pragma unroll
-      for (int st = 0; st < 2; ++st)
-#pragma unroll
-        for (int d = 0; d < HD / 32; ++d) {
-          dv[d] = mfma32x32x16(Tile<HD>::col_frag(now.g, 32 * qb + 16 * st, d, ln), pf[st], dv[d]);
-          const u32x4 qt = Tile<HD>::col_frag(now.q, 32 * qb + 16 * st, d, ln);
-          dk[d] = mfma32x32x16(qt, df[st], dk[d]);
-          if constexpr (FINE) dk[d] = mfma32x32x16(qt, dr[st], dk[d]);
-        }
+      constexpr int ND = HD / 32;
+      products<4 * ND, 2 * kDkvAhead>(
+          [&](int i) { return Tile<HD>::col_frag(i & 1 ? now.q : now.g, 32 * qb + 16 * (i / (2 * ND)), i / 2 % ND, ln); },
+          [&](int i, const u32x4& f) {
+            const int st = i / (2 * ND), d = i / 2 % ND;
+            if (!(i & 1)) {
+              dv[d] = mfma32x32x16(f, pf[st], dv[d]);
+            } else {
+              dk[d] = mfma32x32x16(f, df[st], dk[d]);
+              if constexpr (FINE) dk[d] = mfma32x32x16(f, dr[st], dk[d]);
+            }
+          });
     }
   };
   for (int t = 0; t < steps; t += 2) {

@@ -143,8 +143,8 @@ template <int HD>
 __global__ __launch_bounds__(256, 2) void k_packed_fwd(AttnArgs a, const int32_t* count, const int4* items) {
   __shared__ __attribute__((aligned(16))) TilePair<HD> even, odd;
   const uint32_t id = blockIdx.x, at = id / a.heads;
-  if (static_cast<int>(at) >= count[0]) return;
-  const int4 item = item_at(items, at);
+  const int4 item = item_at(items, at);  // (read beside the count, not behind it: past it is room, too)
+  if (static_cast<int>(at) >= scalar(count[0])) return;
   const Span<true> sp(item.x, item.y, item.w);
 #pragma unroll 1
   for (int mode = kPlain; mode <= kNeg; ++mode) {
@@ -159,8 +159,8 @@ __global__ __launch_bounds__(256, 2) void k_packed_dq(AttnGradArgs ga, const int
   __shared__ int bad_key[kBN];
   const int heads = ga.f.heads;
   const uint32_t id = blockIdx.x, at = id / heads;
-  if (static_cast<int>(at) >= count[0]) return;
   const int4 item = item_at(items, at);
+  if (static_cast<int>(at) >= scalar(count[0])) return;
   const Span<true> sp(item.x, item.y, item.w);
   const int h = head_of(id % heads, heads);
 #pragma unroll 1
@@ -185,8 +185,8 @@ __global__ __launch_bounds__(shared_keys(HD) ? 512 : 256, 2) void k_packed_dkv(A
   DkvJob job;
   if (blockIdx.x < near) {
     const uint32_t r = blockIdx.x / kv, at = r / ga.parts;
-    if (static_cast<int>(at) >= count[0]) return;
     item = item_at(items, at);
+    if (static_cast<int>(at) >= scalar(count[0])) return;
     job = {static_cast<int>(blockIdx.x % kv), ((item.y + 127) / 128 - 1 - item.z) * 128, static_cast<int>(r % ga.parts), 0};
     if (item.w < 0 && job.slot > 0) return;  // (rows of no sequence: zeros, written once)
   } else {
