@@ -77,13 +77,11 @@ __device__ __forceinline__ bool attn_split(const AttnArgs& a, WaveTiles<HD>& eve
     const int j0 = walk.key(t);
     fetch_v(t + 1, next);
     if (mode != kPlain) convert_tile<HD, TN, 64>(now.v[wave], mode, nullptr, lane);
-    f32x16 s = zero16();
+    f32x16 one[1] = {zero16()}, &s = one[0];
 #pragma unroll
     for (int st = 0; st < KS; ++st) s = mfma32x32x16(kf[st], qf[st], s);
     fetch_k(t + 1);
-    if (!all_seen(j0, TN, pmin, pmax, a.window, a.sinks)) {
-      hide_unseen(s, -__builtin_inff(), j0 + 4 * (lane >> 5), p, j0 < a.sinks, a.window, a.sinks);
-    }
+    if (!all_seen(j0, TN, pmin, pmax, a.window, a.sinks)) hide_unseen(one, -__builtin_inff(), j0, p, a.window, a.sinks, lane);
     float top = s[0];
 #pragma unroll
     for (int e = 1; e < 16; ++e) top = max_of(top, s[e]);

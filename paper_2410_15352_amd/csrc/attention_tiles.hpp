@@ -277,17 +277,21 @@ __device__ __forceinline__ bool seen(int j, int p, int window, int sinks) {
   return (j <= p) & ((p - j < window) | (j < sinks));
 }
 
-// The elements of a result whose key (`first` the lane's first) is not seen; past the sinks one
-// difference decides.
-__device__ __forceinline__ void hide_unseen(f32x16& s, float hidden, int first, int p, bool sinks_here, int window, int sinks) {
-  if (!sinks_here) {
-    const int d = p - first;
+// Elements 32 kb + 8 (e / 4) + e mod 4 behind a lane's first: hidden where past(that number).  (Numbers
+// that the compare holds as a constant: differences of them would each want a register.)
+template <int NB, typename F>
+__device__ __forceinline__ void hide(f32x16 (&s)[NB], float hidden, F past) {
 #pragma unroll
-    for (int e = 0; e < 16; ++e) s[e] = static_cast<uint32_t>(d - (8 * (e >> 2) + (e & 3))) < static_cast<uint32_t>(window) ? s[e] : hidden;
-  } else {
+  for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
-    for (int e = 0; e < 16; ++e) s[e] = seen(first + 8 * (e >> 2) + (e & 3), p, window, sinks) ? s[e] : hidden;
-  }
+    for (int e = 0; e < 16; ++e) s[kb][e] = past(32 * kb + 8 * (e >> 2) + (e & 3)) ? hidden : s[kb][e];
+}
+
+// What a lane's row p does not see of the 32 NB keys from j0 on.
+template <int NB>
+__device__ __forceinline__ void hide_unseen(f32x16 (&s)[NB], float hidden, int j0, int p, int window, int sinks, int lane) {
+  const int first = j0 + 4 * (lane >> 5), last = p - first, before = last - window, behind = sinks - first;
+  hide(s, hidden, [&](int k) { return (k > last) | ((k <= before) & (k >= behind)); });
 }
 
 // No key of j0 .. j0 + n - 1 is seen from a position in pmin .. pmax / all are from all of them.
@@ -489,13 +493,7 @@ __device__ __forceinline__ bool attn_fwd(const AttnArgs& a, const Span<PACKED>& 
     s[0] = s[1] = zero16();
     products<2 * KS, 4>([&](int i) { return Tile<HD>::row_frag(now.k, 32 * (i & 1), i >> 1, lane); },
                         [&](int i, const u32x4& f) { s[i & 1] = mfma32x32x16(f, qf[i >> 1], s[i & 1]); });
-    if (!all_seen(j0, kBN, pmin, pmax, a.window, a.sinks)) {
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          s[kb][e] = seen(j0 + 32 * kb + acc_row(e, lane), p, a.window, a.sinks) ? s[kb][e] : -__builtin_inff();
-    }
+    if (!all_seen(j0, kBN, pmin, pmax, a.window, a.sinks)) hide_unseen(s, -__builtin_inff(), j0, p, a.window, a.sinks, lane);
     float top = max_of(s[0][0], s[1][0]);
 #pragma unroll
     for (int e = 1; e < 16; ++e) top = max_of(max_of(top, s[0][e]), s[1][e]);
@@ -626,7 +624,7 @@ __device__ __forceinline__ bool attn_dq(const AttnGradArgs& ga, const Span<PACKE
     constexpr int kUnroll = HD == 64 ? 2 : 1;
 #pragma unroll kUnroll
     for (int kb = 0; kb < 2; ++kb) {
-      f32x16 s = zero16(), dp = zero16();
+      f32x16 one[1] = {zero16()}, &s = one[0], dp = zero16();
       products<2 * KS, kDqAhead>([&](int i) { return Tile<HD>::row_frag(i & 1 ? now.v : now.k, 32 * kb, i >> 1, lane); },
                                  [&](int i, const u32x4& f) {
                                    if (i & 1) dp = mfma32x32x16(f, gf[i >> 1], dp);
@@ -639,7 +637,7 @@ __device__ __forceinline__ bool attn_dq(const AttnGradArgs& ga, const Span<PACKE
 #pragma unroll
           for (int e = 0; e < 16; ++e) s[e] = bad_key[32 * kb + acc_row(e, lane)] ? __builtin_nanf("") : s[e];
         }
-        hide_unseen(s, 0.0f, j0 + 32 * kb + 4 * (lane >> 5), p, j0 < a.sinks, a.window, a.sinks);
+        hide_unseen(one, 0.0f, j0 + 32 * kb, p, a.window, a.sinks, lane);
       }
       u32x4 ds[2], dr[2];
       pack_steps(s, ds);
