@@ -349,22 +349,44 @@ __device__ __forceinline__ uint32_t low_bytes(const float (&v)[4], const u32x2& 
   return out;
 }
 
-// Columns of a transposed result (lane mod 32: the row of the output) as rows of bf16.
+// This wave's writes to LDS before its reads of them, and the other way round.  (LDS serves a wave in
+// order; the compiler must not change it.)
+__device__ __forceinline__ void in_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// Columns of a transposed result (lane mod 32: the row of the output) as rows of bf16: those from
+// `begin` up to `end` of 32.  A lane holds four values of its row here and there; they go through a
+// wave's own 64 HD bytes of LDS (its rows as in a tile), so that neighbouring lanes store a row's
+// neighbouring chunks.  (Stored as they stand, 8 bytes at a time to 32 rows, a large part of short
+// sequences' time went into four times as many requests to L2.)
+// low: also what the rounding took off, in rows of hd bytes that follow one another, by way of
+// 32 HD bytes at t_low.
 template <int HD>
-__device__ __forceinline__ void store_rows(const f32x16 (&acc)[HD / 32], float f, uint16_t* row, int hd, int lane,
-                                           int8_t* low = nullptr) {
+__device__ __forceinline__ void store_rows(const f32x16 (&acc)[HD / 32], float f, uint16_t* rows, int64_t stride, int begin, int end,
+                                           int hd, char* t, int lane, int8_t* low = nullptr, char* t_low = nullptr) {
+  asm volatile("" : "+v"(lane));  // (places formed here: hoisted to the kernel's beginning, they spill)
+  auto low_at = [](int r, int c) { return r * HD + ((c ^ (r & (HD == 96 ? 3 : HD / 8 - 1))) * 8); };  // chunk c of 8 bytes
+  in_order();
 #pragma unroll
   for (int d = 0; d < HD / 32; ++d)
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      const int c = 32 * d + 8 * g + 4 * (lane >> 5);
-      if (c < hd) {
-        const float v[4] = {acc[d][4 * g] * f, acc[d][4 * g + 1] * f, acc[d][4 * g + 2] * f, acc[d][4 * g + 3] * f};
-        const u32x2 w = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-        *reinterpret_cast<u32x2*>(row + c) = w;
-        if (low != nullptr) *reinterpret_cast<uint32_t*>(low + c) = low_bytes(v, w);
-      }
+      const float v[4] = {acc[d][4 * g] * f, acc[d][4 * g + 1] * f, acc[d][4 * g + 2] * f, acc[d][4 * g + 3] * f};
+      const u32x2 w = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+      *reinterpret_cast<u32x2*>(t + Tile<HD>::at(lane & 31, 4 * d + g) + 8 * (lane >> 5)) = w;
+      if (low != nullptr) *reinterpret_cast<uint32_t*>(t_low + low_at(lane & 31, 4 * d + g) + 4 * (lane >> 5)) = low_bytes(v, w);
     }
+  in_order();
+#pragma unroll
+  for (int i = 0; i < HD / 16; ++i) {
+    const int idx = i * 64 + lane, r = idx / (HD / 8), c = idx % (HD / 8);
+    if (r >= begin && r < end && c * 8 < hd) {
+      *reinterpret_cast<u32x4*>(rows + r * stride + c * 8) = *reinterpret_cast<const u32x4*>(t + Tile<HD>::at(r, c));
+      if (low != nullptr) *reinterpret_cast<u32x2*>(low + int64_t(r) * hd + c * 8) = *reinterpret_cast<const u32x2*>(t_low + low_at(r, c));
+    }
+  }
 }
 
 template <int HD>
@@ -520,15 +542,19 @@ __device__ __forceinline__ bool attn_fwd(const AttnArgs& a, const Span<PACKED>& 
     step(t, even, odd);
     if (t + 1 < t1) step(t + 1, odd, even);
   }
-  if (mode == kPlain && __syncthreads_or(not_finite(sm.o))) return false;
+  if (mode == kPlain) {
+    if (__syncthreads_or(not_finite(sm.o))) return false;
+  } else {
+    __syncthreads();
+  }
   const float l = halves_sum(sm.l);
-  if (row >= lq) return true;
   const int64_t at_row = sp.row_of(a, h) + row;
   // no key in this split, which weighs nothing then; without splits: none for the row, which is
   // before its sequence (of scores that are all -inf the softmax is NaN)
   const bool empty = a.splits > 0 ? sm.m == -__builtin_inff() && l == 0.0f : p < 0;
   const float f = empty ? 0.0f : 1.0f / l;
   if (a.splits > 0) {
+    if (row >= lq) return true;
     const int64_t rows = int64_t(a.b) * a.heads * a.lq, at = split * rows + at_row;
     if (mode >= kPos) {
       mark_rows<HD>(sm.o, mode, a.part_o + at * a.hd, a.hd, lane);
@@ -538,13 +564,14 @@ __device__ __forceinline__ bool attn_fwd(const AttnArgs& a, const Span<PACKED>& 
     if (lane < 32) a.part_lse[at] = empty ? -__builtin_inff() : sm.m + log2f(l);
     return true;
   }
-  uint16_t* out = sp.at(a.o, a.os, h) + row * a.os[2];
+  uint16_t* out = sp.at(a.o, a.os, h) + w0 * a.os[2];
   if (mode >= kPos) {
-    mark_rows<HD>(sm.o, mode, out, a.hd, lane);
+    if (row < lq) mark_rows<HD>(sm.o, mode, out + (lane & 31) * a.os[2], a.hd, lane);
     return true;
   }
-  store_rows<HD>(sm.o, f, out, a.hd, lane, a.o_low == nullptr ? nullptr : a.o_low + at_row * a.hd);
-  if (lane < 32) a.lse[at_row] = empty ? __builtin_inff() : sm.m + log2f(l);
+  store_rows<HD>(sm.o, f, out, a.os[2], 0, lq - w0, a.hd, reinterpret_cast<char*>(&even) + wave * 64 * HD, lane,
+                 a.o_low == nullptr ? nullptr : a.o_low + (sp.row_of(a, h) + w0) * a.hd, reinterpret_cast<char*>(&odd) + wave * 32 * HD);
+  if (row < lq && lane < 32) a.lse[at_row] = empty ? __builtin_inff() : sm.m + log2f(l);
   return true;
 }
 
@@ -654,9 +681,13 @@ __device__ __forceinline__ bool attn_dq(const AttnGradArgs& ga, const Span<PACKE
     step(t, even, odd);
     if (t + 1 < walk.count) step(t + 1, odd, even);
   }
-  if (mode == kPlain && __syncthreads_or(not_finite(dq))) return false;
-  if (row < lq)
-    store_rows<HD>(dq, a.scale, sp.at(ga.dq, ga.dqs, h) + row * ga.dqs[2], a.hd, lane);
+  if (mode == kPlain) {
+    if (__syncthreads_or(not_finite(dq))) return false;
+  } else {
+    __syncthreads();
+  }
+  store_rows<HD>(dq, a.scale, sp.at(ga.dq, ga.dqs, h) + w0 * ga.dqs[2], ga.dqs[2], 0, lq - w0, a.hd,
+                 reinterpret_cast<char*>(&even) + wave * 64 * HD, lane);
   return true;
 }
 
@@ -871,7 +902,7 @@ __device__ __forceinline__ bool attn_dkv(const AttnGradArgs& ga, const Span<PACK
   }
   if (mode == kPlain) {
     if (__syncthreads_or(not_finite(dk) || not_finite(dv))) return false;
-  } else if (SHARED) {
+  } else {
     __syncthreads();
   }
   if constexpr (SHARED) {
@@ -900,7 +931,15 @@ __device__ __forceinline__ bool attn_dkv(const AttnGradArgs& ga, const Span<PACK
     join(dv);
     if (wave & 1) return true;
   }
-  if (far || (PACKED ? L > 0 && (ga.parts > 1 ? j < L : j < ga.far_keys) : j < ga.near_keys)) {
+  // keys below `slots` go to slots of `part`, the others to their places
+  const int keys_here = PACKED ? lq : a.lk, slots = far ? keys_here : PACKED ? (L == 0 ? 0 : ga.parts > 1 ? L : ga.far_keys) : ga.near_keys;
+  if (!far && w0 < keys_here && w0 + 32 > slots) {
+    store_rows<HD>(dk, a.scale, sp.at(ga.dk, ga.dks, hk) + w0 * ga.dks[2], ga.dks[2], slots - w0, keys_here - w0, a.hd,
+                   reinterpret_cast<char*>(&even) + kw * 64 * HD, lane);
+    store_rows<HD>(dv, 1.0f, sp.at(ga.dv, ga.dvs, hk) + w0 * ga.dvs[2], ga.dvs[2], slots - w0, keys_here - w0, a.hd,
+                   reinterpret_cast<char*>(&odd) + kw * 64 * HD, lane);
+  }
+  if (far || j < slots) {
     const int slot = far ? far_slots(HD) * job.slot + (SHARED ? 0 : wave & 1) : job.slot;
     int64_t at;
     if constexpr (PACKED) {
@@ -919,9 +958,6 @@ __device__ __forceinline__ bool attn_dkv(const AttnGradArgs& ga, const Span<PACK
     float* out = ga.part + at * 2 * a.hd;
     store_row_values<HD>(dk, a.scale, out, a.hd, lane);
     store_row_values<HD>(dv, 1.0f, out + a.hd, a.hd, lane);
-  } else if (j < (PACKED ? lq : a.lk)) {
-    store_rows<HD>(dk, a.scale, sp.at(ga.dk, ga.dks, hk) + j * ga.dks[2], a.hd, lane);
-    store_rows<HD>(dv, 1.0f, sp.at(ga.dv, ga.dvs, hk) + j * ga.dvs[2], a.hd, lane);
   }
   return true;
 }
