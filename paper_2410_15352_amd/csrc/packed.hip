@@ -45,6 +45,11 @@ __device__ __forceinline__ int block_scan(int v, int* lds, F join) {
   return v;
 }
 
+__device__ __forceinline__ int start_at(const void* starts, int starts64, int64_t stride, int i, int T) {
+  const int64_t x = starts64 ? static_cast<const int64_t*>(starts)[i * stride] : static_cast<const int32_t*>(starts)[i * stride];
+  return x < 0 ? 0 : x > T ? T : static_cast<int>(x);
+}
+
 __device__ __forceinline__ int upper_span(const int32_t* x, int spans, int i) {  // the last span s with x[s] <= i
   int lo = 0, hi = spans - 1;
   while (lo < hi) {
@@ -70,13 +75,8 @@ __global__ __launch_bounds__(kPlanThreads) void k_packed_plan(const void* starts
   for (int i0 = 0; i0 <= spans; i0 += kPlanThreads) {
     const int i = i0 + tid;
     int v = 0;
-    if (i >= 1 && i <= n + 1) {
-      const int64_t x = starts64 ? static_cast<const int64_t*>(starts)[(i - 1) * stride]
-                                 : static_cast<const int32_t*>(starts)[(i - 1) * stride];
-      v = x < 0 ? 0 : x > T ? T : static_cast<int>(x);
-    } else if (i > n + 1) {
-      v = T;
-    }
+    if (i >= 1 && i <= n + 1) v = start_at(starts, starts64, stride, i - 1, T);
+    else if (i > n + 1) v = T;
     v = larger(block_scan(v, lds, larger), carry);
     if (i <= spans) bounds[i] = v;
     __syncthreads();
@@ -139,12 +139,51 @@ __device__ __forceinline__ int head_of(uint32_t i, int heads) {
   return heads % kNumXcd == 0 ? static_cast<int>(i % kNumXcd) * (heads / kNumXcd) + static_cast<int>(i / kNumXcd) : static_cast<int>(i);
 }
 
-template <int HD>
-__global__ __launch_bounds__(256, 2) void k_packed_fwd(AttnArgs a, const int32_t* count, const int4* items) {
+// The starts as the caller gave them.
+struct Starts {
+  const void* at;
+  int64_t stride;
+  int32_t is64, n;
+};
+
+// Few sequences and few workgroups want no table: each wave finds item `at` of the spans in their
+// own order by itself, a span to a lane.  false: there is none.
+constexpr int kOwnSequences = 61, kOwnGrid = 512;
+__device__ __forceinline__ bool own_item(const Starts& s, int T, int at, int4& item) {
+  const int lane = threadIdx.x & 63;
+  int bound = lane == 0 ? 0 : lane <= s.n + 1 ? start_at(s.at, s.is64, s.stride, lane - 1, T) : T;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int w = __shfl_up(bound, d, 64);
+    if (lane >= d) bound = bound > w ? bound : w;
+  }
+  const int next = __shfl_down(bound, 1, 64);  // (asked of every lane: one that does not ask does not answer)
+  const int rows = lane < s.n + 2 ? next - bound : 0, tiles = (rows + 127) / 128;
+  int upto = tiles;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int w = __shfl_up(upto, d, 64);
+    if (lane >= d) upto += w;
+  }
+  const uint64_t behind = __ballot(at < upto);
+  if (behind == 0) return false;
+  const int span = __ffsll(static_cast<unsigned long long>(behind)) - 1;
+  item = make_int4(__builtin_amdgcn_readlane(bound, span), __builtin_amdgcn_readlane(rows, span),
+                   at - __builtin_amdgcn_readlane(upto - tiles, span), span >= 1 && span <= s.n ? span - 1 : -1);
+  return true;
+}
+
+template <int HD, bool OWN>
+__global__ __launch_bounds__(256, 2) void k_packed_fwd(AttnArgs a, const int32_t* count, const int4* items, Starts starts) {
   __shared__ __attribute__((aligned(16))) TilePair<HD> even, odd;
   const uint32_t id = blockIdx.x, at = id / a.heads;
-  const int4 item = item_at(items, at);  // (read beside the count, not behind it: past it is room, too)
-  if (static_cast<int>(at) >= scalar(count[0])) return;
+  int4 item;
+  if constexpr (OWN) {
+    if (!own_item(starts, a.lq, scalar(static_cast<int>(at)), item)) return;
+  } else {
+    item = item_at(items, at);  // (read beside the count, not behind it: past it is room, too)
+    if (static_cast<int>(at) >= scalar(count[0])) return;
+  }
   const Span<true> sp(item.x, item.y, item.w);
 #pragma unroll 1
   for (int mode = kPlain; mode <= kNeg; ++mode) {
@@ -291,9 +330,12 @@ bool grads_fit(const AttnGradArgs& a) {
 }
 
 template <int HD>
-void launch_fwd(const AttnArgs& a, const Plan& plan, hipStream_t s) {
-  const int grid = static_cast<int>(most_items(plan.spans - 2, a.lk) * a.heads);
-  hipLaunchKernelGGL((k_packed_fwd<HD>), dim3(grid), dim3(256), 0, s, a, plan.base, plan.items());
+void launch_fwd(const AttnArgs& a, const Plan& plan, const Starts& starts, hipStream_t s) {
+  const int grid = static_cast<int>(most_items(starts.n, a.lk) * a.heads);
+  if (plan.base == nullptr)
+    hipLaunchKernelGGL((k_packed_fwd<HD, true>), dim3(grid), dim3(256), 0, s, a, nullptr, nullptr, starts);
+  else
+    hipLaunchKernelGGL((k_packed_fwd<HD, false>), dim3(grid), dim3(256), 0, s, a, plan.base, plan.items(), starts);
 }
 
 template <int HD, bool FINE>
@@ -323,15 +365,18 @@ using namespace compact;
 extern "C" {
 
 // q, k, v and o as a padded batch of one: (1, heads, T, hd).  plan: 4 + 2 round4(n + 3) + 4
-// (T / 128 + min(n + 2, T)) int32, which the backward reads too.
+// (T / 128 + min(n + 2, T)) int32, which the backward reads too; NULL where kOwnSequences and kOwnGrid
+// allow it.
 int compact_packed_fwd(const AttnArgs* a, const void* starts, int starts64, int64_t stride, int n, int32_t* table, void* stream) {
   if (!packed_ok(*a, n)) return -1;
+  if (table == nullptr && (n > kOwnSequences || most_items(n, a->lk) * a->heads > kOwnGrid)) return -1;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const Plan plan(table, n);
-  hipLaunchKernelGGL(k_packed_plan, dim3(1), dim3(kPlanThreads), 0, s, starts, starts64, stride, n, a->lk, table);
-  if (a->hd <= 64) launch_fwd<64>(*a, plan, s);
-  else if (a->hd <= 96) launch_fwd<96>(*a, plan, s);
-  else launch_fwd<128>(*a, plan, s);
+  const Starts given = {starts, stride, starts64, n};
+  if (table != nullptr) hipLaunchKernelGGL(k_packed_plan, dim3(1), dim3(kPlanThreads), 0, s, starts, starts64, stride, n, a->lk, table);
+  if (a->hd <= 64) launch_fwd<64>(*a, plan, given, s);
+  else if (a->hd <= 96) launch_fwd<96>(*a, plan, given, s);
+  else launch_fwd<128>(*a, plan, given, s);
   return status();
 }
 
@@ -349,7 +394,7 @@ int64_t compact_packed_bwd_scratch(const AttnArgs* a, int n) {
 int compact_packed_bwd(const AttnGradArgs* args, int n, int32_t* table, void* stream) {
   AttnGradArgs a = *args;
   a.sequences = n;
-  if (!packed_ok(a.f, n) || a.f.o_low == nullptr || a.gs[2] < 0 || a.gs[2] > kMaxStride || (a.f.lq > 1 && a.gs[2] < a.f.hd)) return -1;
+  if (table == nullptr || !packed_ok(a.f, n) || a.f.o_low == nullptr || a.gs[2] < 0 || a.gs[2] > kMaxStride || (a.f.lq > 1 && a.gs[2] < a.f.hd)) return -1;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const bool kv = a.dk != nullptr;
   const bool parts = plan_packed(&a) > 0;
