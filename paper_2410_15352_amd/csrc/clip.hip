@@ -17,8 +17,8 @@
 namespace compact {
 namespace {
 
-constexpr int kPieceBytes = 1 << 16;  // per workgroup
-constexpr int kMostTensors = 160;     // per launch: 4 KB of arguments
+constexpr int kPieceBytes = 1 << 16;  // per workgroup.  (32 KB to 256 KB are within 2%, 16 KB 10% slower: 320 MB in 220 tensors.)
+constexpr int kMostTensors = 160;  // per launch: a launch has 4 KB of arguments
 
 struct Tensors {
   uint64_t at[kMostTensors];

@@ -209,9 +209,11 @@ __global__ __launch_bounds__(256) void k_pairs(PairArgs a) {
   if (threadIdx.x == 0) a.loss_pair[blockIdx.x] = static_cast<float>(loss);
 }
 
-// A few pairs: a wave each, and their mean, in one workgroup.
-constexpr int kFewPairs = 64;
-constexpr int64_t kFewPairRows = 32768;
+// A few pairs: a wave each, and their mean, in one workgroup.  us, this / a workgroup per pair and the
+// mean's launch: 200 rows, 2 pairs 4.1 / 6.8; 8192 rows, 2 pairs 7.2 / 7.2, 16 pairs 6.3 / 6.9, 64
+// pairs 18 / 6.9; 32768 rows, 16 pairs 8.0 / 6.7.  (A launch on the host is 3 more.)
+constexpr int kFewPairs = 16;
+constexpr int64_t kFewPairRows = 16384;
 __global__ __launch_bounds__(1024) void k_few_pairs(PairArgs a) {
   __shared__ double loss[kFewPairs];
   const int lane = threadIdx.x & 63;
@@ -391,6 +393,14 @@ void launch_policy(const PolicyArgs& a, hipStream_t s) {
 
 template <bool F32>
 void launch_policy(const PolicyArgs& a, hipStream_t s) {
+  // The smallest workgroup whose registers hold a row, or all but the last 3% of it.  us by threads x
+  // chunks, loss and gradient in bf16, all rows counting (the rule's *):
+  //             256 x 1  256 x 4  256 x 16  512 x 16  1024 x 16
+  //   16384 x   1000  62*      94      255       507      1015
+  //    8192 x   8000  72       60*     136       265       524
+  //    8192 x  32001 280      264      227*      300       544
+  //    2048 x  65536 181      174      154       121*      171
+  //    1024 x 200000 322      317      303       255       225*
   const int64_t chunks = a.V / (F32 ? 4 : 8);
   if (chunks <= 256) launch_policy<F32, 256, 1>(a, s);
   else if (chunks <= 1024) launch_policy<F32, 256, 4>(a, s);

@@ -378,7 +378,6 @@ def policy_loss(logits, targets, old, advantages, reference=None, clip=0.2, kl=0
 
 # ------------------------------- clipping -----------------------------------
 
-CLIP_PIECE = 1 << 16  # bytes that a workgroup adds up
 _CLIP_KINDS = {_bf16: 0, _f32: 1}
 
 
