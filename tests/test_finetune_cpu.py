@@ -317,3 +317,13 @@ def test_clip_entries(monkeypatch):
     assert calls[1][1] == [t[0].data_ptr(), 24, 0, t[2].data_ptr(), 3, 1] and calls[1][2][:2] == (0.0, False)
     FT.clip_grad_norm([t[0], t[2].half()], 1.0)
     assert len(calls) == 2
+
+
+def test_functorch_takes_the_expressions():
+    x, t = _inputs()
+    g = torch.func.grad(lambda x: FT.policy_loss(x, t, _rand(9, seed=3) - 2, _rand(9, seed=4))[0])(x)
+    y = x.clone().requires_grad_()
+    (e,) = torch.autograd.grad(FT.policy_loss(y, t, _rand(9, seed=3) - 2, _rand(9, seed=4))[0], y)
+    assert torch.allclose(g, e)
+    l = torch.func.vmap(lambda x: FT.token_logprobs(x, t))(torch.stack((x, 2 * x)))
+    assert torch.allclose(l[1], FT.token_logprobs(2 * x, t))

@@ -595,3 +595,46 @@ def test_policy_step(kernels_only, monkeypatch):
     assert abs(float(loss.detach()) + float(A[counts].double().mean())) <= (off + 2.0 ** -21) * float(A[counts].abs().mean())
     loss.backward()
     assert FT.clip_grad_norm(blk.gradients(model), 1.0).isfinite()
+
+
+def test_offsets_past_32_bits(kernels_only):
+    """Logits of more than 2^31 elements: the last rows are what they are alone."""
+    if torch.cuda.get_device_properties(0).total_memory < 64 << 30:
+        pytest.skip("memory")
+    rows, V, few = 70001, 32000, 6
+    x = torch.zeros(rows, V, dtype=bf16, device=dev())
+    x[-few:] = _rand(few, V, seed=1, dtype=bf16, scale=2.0)
+    t = torch.full((rows,), -100, device=dev())
+    t[-few:] = torch.arange(few, device=dev()) * 1000
+    old, A = torch.full((rows,), -11.0, device=dev()), torch.ones(rows, device=dev())
+    starts = torch.tensor([0, rows - 3, rows], device=dev())
+    x.requires_grad_(True)
+    y = x.detach()[-few:].clone().requires_grad_(True)
+    last = torch.tensor([0, few - 3, few], device=dev())
+    for run in (lambda x, n: FT.token_logprobs(x, t[-n:])[-few:],
+                lambda x, n: FT.preference_loss(x, t[-n:], starts if n == rows else last)[0],
+                lambda x, n: FT.policy_loss(x, t[-n:], old[-n:], A[-n:], clip=0.9)[0]):
+        a, b = run(x, rows), run(y, few)
+        (g,), (h,) = torch.autograd.grad(a, x, torch.ones_like(a)), torch.autograd.grad(b, y, torch.ones_like(b))
+        assert torch.equal(a, b) and torch.equal(g[-few:], h) and h.any() and not g[:-few].any()
+        del a, g
+
+
+def test_clip_of_a_large_tensor(kernels_only):
+    """Elements past 2^31: found and scaled."""
+    if torch.cuda.get_device_properties(0).total_memory < 32 << 30:
+        pytest.skip("memory")
+    t = torch.zeros((1 << 31) + 5, dtype=bf16, device=dev())
+    t[-1], t[3] = 3.0, 4.0
+    assert float(FT.clip_grad_norm([t], 2.5)) == 5.0
+    assert float(t[-1]) == 1.5 and float(t[3]) == 2.0 and float(t.double().sum()) == 3.5
+
+
+@pytest.mark.parametrize("n,rows", [(16, 300), (17, 300), (2, 16384), (2, 16385)])
+def test_pairs_on_both_sides_of_the_rule(kernels_only, n, rows):
+    x, t = _inputs(rows, 24, f32)
+    starts = [i * rows // (2 * n) for i in range(2 * n + 1)]
+    ref = _rand(rows, seed=4, scale=0.2) - 3.0
+    x.requires_grad_(True)
+    loss, rewards = FT.preference_loss(x, t, torch.tensor(starts, device=dev()), reference=ref, beta=0.05, smoothing=0.2)
+    _check_preference(x, t, starts, ref, 0.05, 0.2, loss.detach(), rewards, torch.autograd.grad(loss, x)[0])

@@ -272,3 +272,64 @@ def test_against_differences():
         slope = (loss(*up) - loss(*down)) / (2 * h)
         # each element is off by the rounding of the operands and of itself: 2^-6 of the terms' sum
         assert abs((g.double() * d).sum() - slope) <= 2.0 ** -6 * (g.double() * d).abs().sum()
+
+
+def test_offsets_past_32_bits(kernels_only):
+    """Rows 2^23 elements apart: the last ones past 2^31."""
+    if torch.cuda.get_device_properties(0).total_memory < 32 << 30:
+        pytest.skip("memory")
+    rows, apart, hd = 300, 1 << 23, 64
+    buf = torch.empty(rows * apart, dtype=torch.bfloat16, device=dev())
+    t = []
+    for i, heads in enumerate((2, 1, 1)):
+        x = buf[256 * i:].as_strided((rows, heads, hd), (apart, hd, 1))
+        t.append(x.copy_(_rand(rows, heads, hd, seed=i)))
+    starts, do = torch.tensor([0, 20, 290], device=dev()), _rand(rows, 2, hd, seed=9)
+
+    def run(*t):
+        t = [x.detach().requires_grad_(True) for x in t]
+        o = F.packed_attention(*t, starts, window=100, sinks=2)
+        return o, *torch.autograd.grad(o, t, do)
+
+    for x, y in zip(run(*t), run(*(x.contiguous() for x in t))):
+        assert torch.equal(x, y)
+
+
+def test_more_heads_and_sequences_than_one_launch_finds_itself(kernels_only):
+    """On both sides of the rule for a forward without the table: the same bits."""
+    for n, heads in ((F.OWN_SEQUENCES, 2), (F.OWN_SEQUENCES + 1, 2), (3, 64), (3, 200)):
+        rows = 10 * n + 3
+        starts = [1 + 10 * i for i in range(n + 1)]
+        q, k, v, do = _inputs(rows, heads, 2, 64)
+        table = F.packed_wants_table(n, rows, heads)
+        assert table == (n > F.OWN_SEQUENCES or heads == 200)
+        at = torch.tensor(starts, device=dev())
+        plain = F.packed_attention(q.detach(), k.detach(), v.detach(), at, window=7)
+        o = F.packed_attention(q, k, v, at, window=7)
+        assert torch.equal(plain, o)
+        if n == 3:
+            _check((o,), q, k, v, do, starts, 7, 0)
+
+
+def test_two_streams_at_once(kernels_only):
+    """Calls that run beside each other share nothing."""
+    starts = [torch.tensor(s, device=dev()) for s in ([0, 300, 700], [100, 200, 650])]
+    t = [_inputs(700, 8, 2, 64, seed=10 * i) for i in range(2)]
+
+    def step(i):
+        q, k, v, do = t[i]
+        o = F.packed_attention(q, k, v, starts[i], window=150, sinks=3)
+        return o, *torch.autograd.grad(o, (q, k, v), do)
+
+    expect = [[x.detach().clone() for x in step(i)] for i in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [None, None]
+    for _ in range(3):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i] = step(i)
+    torch.cuda.synchronize()
+    for a, b in zip(got, expect):
+        for x, y in zip(a, b):
+            assert torch.equal(x, y)

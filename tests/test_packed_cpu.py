@@ -187,3 +187,16 @@ def test_strides_that_the_kernels_take(launches):
         F.packed_attention(t, k, v, torch.tensor([0, 4]))
         args = struct.unpack("@" + F._ATTN, launches[-1][1][0])
         assert args[7:10] in ((0, 144, 16), (0, 16, 32)) and args[0] % 16 == 0 and (args[9] >= 16)
+
+
+def test_no_heads():
+    q, k = torch.zeros(4, 0, 8), torch.zeros(4, 2, 8)
+    assert F.packed_attention(q, k, k, torch.tensor([0, 4])).shape == (4, 0, 8)
+
+
+def test_functorch_and_compile_take_the_expressions():
+    q, k, v = (_rand(3, 9, 2, 8, seed=s) for s in (1, 2, 3))
+    starts = torch.tensor([0, 4, 9])
+    o = torch.func.vmap(lambda a, b, c: F.packed_attention(a, b, c, starts, window=3))(q, k, v)
+    for i in range(3):
+        assert torch.allclose(o[i], F.packed_attention(q[i], k[i], v[i], starts, window=3))
