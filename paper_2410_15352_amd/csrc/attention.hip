@@ -24,9 +24,9 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnArgs a) {
 // Few rows over many keys: the rows of the heads that share keys (32 of the G lq at a time)
 // are the columns of one wave, and each wave takes a range of the keys on its own: K straight
 // from memory as the A operand, V by copies into its own part of LDS, both a tile of 32 keys
-// ahead.  Bound by HBM where there are keys enough: 165 us, 5.2 TB/s, for one token of 4
-// sequences of up to 70000 keys, 32 heads on 8 of 128 (with the join 175 us), as a large copy;
-// 16 us and the join's 4 for 16 sequences, 16 heads of 64, 1028 keys seen (4.3 TB/s over both
+// ahead.  Bound by HBM where there are keys enough: 157 us, 5.5 TB/s, for one token of 4
+// sequences of up to 70000 keys, 32 heads on 8 of 128 (with the join 167 us), as a large copy;
+// 15 us and the join's 4 for 16 sequences, 16 heads of 64, 1028 keys seen (4.3 TB/s over both
 // would be 13 us), where each wave's few tiles in a row are what counts.
 template <int HD>
 struct WaveTiles {
@@ -207,8 +207,8 @@ __global__ __launch_bounds__(shared_keys(HD) ? 512 : 256, 2) void k_attn_dkv(Att
   __shared__ int bad_row[kBN];
   // A head's blocks stay on one XCD where the heads are a multiple of 8 (on two, where 4): what
   // its workgroups walk at a time is rows that an L2 holds.  (Runs of 8 or of 32 neighbouring
-  // blocks, for fewer heads, were no faster: 2405 and 2530 us for 2404 at 16384 rows, 4 heads of
-  // k, with the gradient of q.)  The first keys' blocks, whose windows are whole, go first, and
+  // blocks, for fewer heads, were no faster, within 0 and 5%, at 16384 rows, 4 heads of k, with
+  // the gradient of q.)  The first keys' blocks, whose windows are whole, go first, and
   // the far work, in shorter pieces, last: with a workgroup or two to a CU a long one that
   // starts late is all that runs at the end.
   const int nkb = (ga.f.lk + 127) / 128, nfb = (ga.far_keys + far_block(HD) - 1) / far_block(HD), bk_all = ga.f.b * ga.f.kv;
@@ -260,9 +260,8 @@ __global__ __launch_bounds__(256) void k_attn_dkv_sum(AttnGradArgs ga) {
 // parts: 512 workgroups (two per CU) of at least 8 tiles where the blocks of keys are fewer.
 // chunks: a far workgroup walks a quarter of a near one's tiles, at least 8.
 // The whole backward, us, with at least 4 / 8 tiles: 3 x 1531 rows, 10 heads on 2 of 80, window
-// 301: 117 / 91; 2 x 5000, 4 on 1 of 64, window 700: 110 / 102; 1000, 16 on 2 of 96: 79 / 80.
-// Far work of at least 16 / 8 tiles: 4 x 4096, 16 heads of 64, window 1024: 356 / 346; as much
-// as a near workgroup's: 396.
+// 301: 97 / 83; 2 x 5000, 4 on 1 of 64, window 700: 75 / 71; 1000, 16 on 2 of 96: 62 / 61.
+// Far work of at least 16 / 8 tiles: 4 x 4096, 16 heads of 64, window 1024: 326 / 325.
 int64_t plan_dkv(AttnGradArgs* g) {
   const AttnArgs& a = g->f;
   const int64_t bk = int64_t(a.b) * a.kv, G = a.heads / a.kv;

@@ -39,8 +39,8 @@ constexpr float kLog2e = 1.44269504088896340736f;
 // dS rounded to bf16 alone leaves dq and dk, rounded themselves, 1.42 times as far from the
 // exact gradients as their own rounding; with few keys to a row the error of o in D comes on
 // top (1.49 at windows of 16 and 20).  In two parts: 1.02 to 1.08.  Two more products of nine:
-// where windows are long 10% of the backward's time with heads of 64 (355 to 390 us at 4 x 4096
-// rows, window 1024) and 18% with heads of 128 (1885 to 2230 us at 16384, window 4096).
+// where windows are long 10% of the backward's time with heads of 64 (325 to 357 us at 4 x 4096
+// rows, window 1024) and 19% with heads of 128 (1723 to 2048 us at 16384, window 4096).
 constexpr int kFineKeys = 512;
 constexpr int kBN = 64;  // keys (or queries) per staged tile
 
@@ -205,7 +205,8 @@ __device__ __forceinline__ f32x16 zero16() {
 
 // N products in order, use(i, factor), of factors that are read from LDS, AHEAD of them on their
 // way.  (Left alone the compiler reads each factor right before its product, which then waits for
-// LDS every time.)  Only vector and scalar arithmetic may be moved across a product's place.
+// LDS every time: 4 documents in 32768 rows, 16 heads on 4 of 128, window 4096, forward and backward
+// 4229 us, so 3839.)  Only vector and scalar arithmetic may be moved across a product's place.
 template <int N, int AHEAD, typename Read, typename Use>
 __device__ __forceinline__ void products(Read read, Use use) {
   constexpr int kArithmetic = 0x2 | 0x4 | 0x400;
@@ -278,7 +279,8 @@ __device__ __forceinline__ bool seen(int j, int p, int window, int sinks) {
 }
 
 // Elements 32 kb + 8 (e / 4) + e mod 4 behind a lane's first: hidden where past(that number).  (Numbers
-// that the compare holds as a constant: differences of them would each want a register.)
+// that the compare holds as a constant: differences of them would each want a register, and the
+// gradient of q at heads of 64 its third wave: 123 us, so 107, for 24 documents in 16384 rows.)
 template <int NB, typename F>
 __device__ __forceinline__ void hide(f32x16 (&s)[NB], float hidden, F past) {
 #pragma unroll
@@ -359,8 +361,8 @@ __device__ __forceinline__ void in_order() {
 // Columns of a transposed result (lane mod 32: the row of the output) as rows of bf16: those from
 // `begin` up to `end` of 32.  A lane holds four values of its row here and there; they go through a
 // wave's own 64 HD bytes of LDS (its rows as in a tile), so that neighbouring lanes store a row's
-// neighbouring chunks.  (Stored as they stand, 8 bytes at a time to 32 rows, a large part of short
-// sequences' time went into four times as many requests to L2.)
+// neighbouring chunks.  (Stored as they stand, 8 bytes at a time to 32 rows, they are four times as
+// many requests to L2: 24 documents in 16384 rows, 16 heads of 64, forward and backward 324 us, so 313.)
 // low: also what the rounding took off, in rows of hd bytes that follow one another, by way of
 // 32 HD bytes at t_low.
 template <int HD>
@@ -457,13 +459,14 @@ struct Softmax {
 // flight has nothing to do with.)  The work with V's values of `mode`; false: not finite, to be
 // done by modes.
 //
-// Bound by the latency of a wave's own chain (scores, maximum, exponentials, P V) with two or
-// three waves on a SIMD: at heads of 64 the matrix units work 23 % of the time and the vector
-// units 65 %, at 128 the matrix units 40 %; LDS has no bank conflicts.  Tried and slower: the
-// next tile's scores among this one's exponentials (heads of 64: 125-145 us for 105, alone, at
-// 4 x 4096, 16 heads, window 1024; heads of 128: 3-7 % faster, but its two tiles of scores do
-// not fit the registers), 64 columns per wave (no longer two workgroups per CU).
-// Measured: there 112 us, 540 TFLOP/s over the pairs that are seen; 551 us, 875 TFLOP/s, at
+// Bound by a wave's own chain (scores, maximum, exponentials, P V) with two or three waves on a
+// SIMD; LDS has no bank conflicts.  Tried and slower: the next tile's scores among this one's
+// exponentials (heads of 64: 125-145 us for 105, alone, at 4 x 4096, 16 heads, window 1024; heads
+// of 128: 3-7 % faster, but its two tiles of scores do not fit the registers), 64 columns per wave
+// (no longer two workgroups per CU), tiles of 32 keys and a wave more on a SIMD (heads of 64: 382
+// us for 358 at 12288 rows, all earlier keys; heads of 128 spill), a wave's priority raised for its
+// products (no difference).
+// Measured: there 115 us, 526 TFLOP/s over the pairs that are seen; 513 us, 940 TFLOP/s, at
 // 16384 rows, 16 heads on 4 of 128, window 4096; 28 us at 3 x 1531 rows, 10 on 2 of 80, window
 // 301; 19 us at 32 x 256 rows, 8 heads, window 128.  A large matrix product: 1223 TFLOP/s.
 template <int HD>
@@ -580,10 +583,9 @@ __device__ __forceinline__ bool attn_fwd(const AttnArgs& a, const Span<PACKED>& 
 // too.  Where the sums are not finite the work is done again with clean values, and NaN in the
 // rows that see a key that had others.
 //
-// Bound as the forward.  Measured: 148 us at 4 x 4096 rows, 16 heads of 64, window 1024; 744 us,
-// 970 TFLOP/s of its three products, at 16384 rows, 16 heads on 4 of 128, window 4096; 24 us at
-// 32 x 256 rows, 8 heads of 64, window 128.  (Three waves to a SIMD at heads of 64, with places
-// in LDS formed for each tile: 352 us with the other gradients for 344.)
+// Bound as the forward, with three waves to a SIMD at heads of 64.  Measured: 133 us at 4 x 4096
+// rows, 16 heads of 64, window 1024; 691 us, 1044 TFLOP/s of its three products, at 16384 rows, 16
+// heads on 4 of 128, window 4096; 23 us at 32 x 256 rows, 8 heads of 64, window 128.
 constexpr int kDqAhead = 4, kDkvAhead = 2;
 
 template <int HD, bool FINE, bool PACKED>
@@ -702,11 +704,9 @@ __device__ __forceinline__ bool attn_dq(const AttnGradArgs& ga, const Span<PACKE
 //
 // Bound by the chain of one wave (products, exponentials, products) with two to a SIMD, and with
 // 128 columns by LDS too: a step's fragments take 1.5 times as long to read as its products.
-// Measured: 194 us at 4 x 4096 rows, 16 heads of 64, window 1024; 1187 us, 810 TFLOP/s of its four
-// products, at 16384 rows, 16 heads on 4 of 128, window 4096; 27 us at 32 x 256 rows, 8 heads of
-// 64, window 128.  Both halves of a tile in one stretch of code were slower (2702 us with the
-// gradient of q for 2580, spilled or at one wave to a SIMD), and so were three waves at heads of
-// 64 (369 for 344).
+// Measured: 180 us at 4 x 4096 rows, 16 heads of 64, window 1024; 1078 us, 892 TFLOP/s of its four
+// products, at 16384 rows, 16 heads on 4 of 128, window 4096; 25 us at 32 x 256 rows, 8 heads of
+// 64, window 128.  Both halves of a tile in one stretch of code spill, or leave one wave to a SIMD.
 template <int HD>
 struct RowPair {
   char q[Tile<HD>::kBytes], g[Tile<HD>::kBytes];
@@ -722,8 +722,8 @@ struct DkvJob {
 // Else four waves with both halves, k and v in registers.  With 128 columns of dk and dv the
 // latter is one wave to a SIMD, with nothing to run while it waits; 64 columns leave room for
 // two anyway, and the reads of k and v cost them more.  The whole backward, us, with eight / four
-// waves: 16384 rows, 16 heads on 4 of 128, window 4096: 1917 / 2411; 2 x 4096, 16 of 128, all
-// keys: 608 / 722; 4 x 4096, 16 of 64, window 1024: 431 / 364; 1000, 16 on 2 of 96: 96 / 95.
+// waves: 16384 rows, 16 heads on 4 of 128, window 4096: 1723 / 2346; 2 x 4096, 16 of 128, all
+// keys: 530 / 663; 4 x 4096, 16 of 64, window 1024: 382 / 325; 1000, 16 on 2 of 96: 60 / 61.
 __host__ __device__ constexpr bool shared_keys(int hd) { return hd > 96; }
 __host__ __device__ constexpr int far_block(int hd) { return shared_keys(hd) ? 128 : 64; }
 __host__ __device__ constexpr int far_slots(int hd) { return shared_keys(hd) ? 1 : 2; }
@@ -964,9 +964,9 @@ __device__ __forceinline__ bool attn_dkv(const AttnGradArgs& ga, const Span<PACK
 
 // Far workgroups are 1024 at most, or one to a block of sinks: a chunk costs a slot in fp32 for each
 // sink.  us (MB of scratch beside the gradients) without a limit / 2048 / 1024 / 512: 4 x 16384 rows, 16
-// heads of 64, window 1024, 4 sinks 1493 (6) / 1483 (6) / 1477 (2) / 1465; 1024 sinks 3146 (2046) /
-// 2443 (167) / 2470 (100) / 2472; 16384 rows, window 128, 4096 sinks 1996 (2183) / 1200 (168) / 1244
-// (101) / 1245; 16 heads on 4 of 128, window 4096, 4096 sinks 3219 (220) / 3223 / 3156 (153) / 3227.
+// heads of 64, window 1024, 4 sinks 1294 (6) / 1295 (6) / 1287 (2) / 1290; 1024 sinks 2862 (2046) /
+// 2243 (167) / 2236 (100) / 2242; 16384 rows, window 128, 4096 sinks 1858 (2183) / 1076 (168) / 1114
+// (101) / 1109; 16 heads on 4 of 128, window 4096, 4096 sinks 2920 (220) / 2925 / 2872 (153) / 2944.
 constexpr int64_t kFarWork = 1024;
 
 constexpr int64_t kSumGrid = int64_t(1) << 20;  // workgroups that add slots

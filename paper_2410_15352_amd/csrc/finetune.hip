@@ -16,7 +16,12 @@
 //
 // All are bound by HBM: the logits of a row that counts are read once for l, and once more for the
 // gradient where that needs sums over other rows first (log-probabilities, preference); the policy
-// loss holds a row in registers and forms both.  l is put together in fp64 (a few operations a
+// loss holds a row in registers and forms both.  Measured, of 32000 bf16 logits, 7 of 10 rows counting:
+// l of 8192 rows 69 us, 5.3 TB/s, the same right after the gradient of others was written 104 us; the
+// gradient 150 us, 5.9 TB/s (some of the logits are still in the cache); the policy loss with its
+// gradient 192 us, 4.6 TB/s, and of 4096 rows of 131072 400 us, 4.6 TB/s, where a large copy reaches
+// 5.2.  (The rows that count dealt out evenly first: no faster.  Exponents by one fused operation in
+// place of two: 1%.)  l is put together in fp64 (a few operations a
 // row): the sums of exponentials are fp32, and what is left of l - reference is a difference of
 // near numbers.
 #include <hip/hip_runtime.h>
