@@ -194,8 +194,8 @@ class LlamaBlock(torch.nn.Module):
 def block_saved_bytes(b, l, d, heads, ffn, rank=None, rank_down=None, compress_o=False, window=None):
     """Table 7 for this block: bytes of the activations one block keeps for
     its backward (bf16 tensors, fp32 inverse RMS and attention log-sum-exp,
-    two int64 scalars of the attention's dropout state, or with a window a
-    byte more for each element of x3).  A CompAct z of r columns is stored
+    two int64 scalars of the attention's dropout state, or with a window, and for
+    packed sequences, a byte more for each element of x3; their table is not counted).  A CompAct z of r columns is stored
     with its rows padded to a multiple of 8 elements."""
     T = b * l
     attention = 4 * b * heads * l + 16 if window is None else 4 * ((b * heads * l + 3) // 4 * 4) + T * d
