@@ -200,7 +200,7 @@ extern "C" {
 // of its entries.  `order`: room for n indexes.  -1: sizes it does not take; -2: two tensors overlap.
 int64_t compact_clip_pieces(ClipTensor* list, int64_t n, int64_t* order) {
   for (int64_t i = 0; i < n; ++i) {
-    if (list[i].count < 0 || list[i].count >= int64_t(1) << 40 || list[i].at % (list[i].f32 ? 4 : 2) != 0) return -1;
+    if (list[i].count < 0 || list[i].count >= int64_t(1) << 40 || (list[i].count > 0 && list[i].at == 0) || list[i].at % (list[i].f32 ? 4 : 2) != 0) return -1;
     order[i] = i;
   }
   std::sort(order, order + n, [&](int64_t a, int64_t b) { return list[a].at != list[b].at ? list[a].at < list[b].at : a < b; });
