@@ -98,6 +98,7 @@ struct PairArgs {
   float* slope;                  // [rows]
   float* loss_pair;              // [n] scratch
   float* loss;
+  int32_t* bounds;               // [2 n + 1] scratch: the starts' running maximum, or NULL for few pairs
   int64_t stride, rows, n;
   int32_t starts64;
   float beta, smoothing;

@@ -34,7 +34,7 @@ _Tensor = torch.Tensor
 
 # The argument blocks of csrc/functional.hpp as native struct layouts, passed by address.
 _token_pack = struct.Struct("@8Q3q2i").pack
-_pair_pack = struct.Struct("@6Q3qi2f4x").pack
+_pair_pack = struct.Struct("@7Q3qi2f4x").pack
 _policy_pack = struct.Struct("@11Q3q3i3f").pack
 
 ops._SIGNATURES.update({
@@ -185,6 +185,9 @@ def _preference_torch(logits, targets, starts, reference, beta, smoothing):
     return loss.mean().to(wide), rewards.detach().to(wide)
 
 
+OWN_PAIRS = 2048  # more have the starts' running maximum formed before, by a launch of its own
+
+
 class _PreferenceFn(torch.autograd.Function):
     """Keeps the logits and three fp32 numbers of each row."""
 
@@ -195,11 +198,12 @@ class _PreferenceFn(torch.autograd.Function):
         stats = torch.empty(2 * rows, dtype=_f32, device=device) if tracked else None
         gain, slope = torch.empty(rows, dtype=_f32, device=device), torch.empty(rows, dtype=_f32, device=device)
         loss, rewards = torch.empty((), dtype=_f32, device=device), torch.empty(pairs, 2, dtype=_f32, device=device)
-        each = torch.empty(pairs, dtype=_f32, device=device)
+        bounds = pairs > OWN_PAIRS
+        each = torch.empty(pairs + (2 * pairs + 1) * bounds, dtype=_f32, device=device)  # scratch
         _token_call(logits, targets, reference=reference, out=gain, stats=stats)
         ops._call("compact_preference_pairs",
                   _pair_pack(gain.data_ptr(), starts.data_ptr(), rewards.data_ptr(), slope.data_ptr(), each.data_ptr(),
-                             loss.data_ptr(), starts.stride(0), rows, pairs, starts.dtype == torch.int64, beta, smoothing),
+                             loss.data_ptr(), each.data_ptr() + 4 * pairs if bounds else 0, starts.stride(0), rows, pairs, starts.dtype == torch.int64, beta, smoothing),
                   _stream(logits))
         if tracked:
             ctx.rule = beta, smoothing

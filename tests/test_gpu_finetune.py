@@ -638,3 +638,41 @@ def test_pairs_on_both_sides_of_the_rule(kernels_only, n, rows):
     x.requires_grad_(True)
     loss, rewards = FT.preference_loss(x, t, torch.tensor(starts, device=dev()), reference=ref, beta=0.05, smoothing=0.2)
     _check_preference(x, t, starts, ref, 0.05, 0.2, loss.detach(), rewards, torch.autograd.grad(loss, x)[0])
+
+
+@pytest.mark.parametrize("n", [FT.OWN_PAIRS, FT.OWN_PAIRS + 1, 4500])
+def test_pairs_on_both_sides_of_the_bounds_launch(kernels_only, n):
+    """Starts' running maximum by each pair, and before all of them: 4500 pairs take more than one
+    round of 4096 starts."""
+    rows = 3 * n
+    x, t = _inputs(rows, 8, f32)
+    starts = [2 + i * (rows - 5) // (2 * n) for i in range(2 * n + 1)]
+    ref = _rand(rows, seed=4, scale=0.2) - 2.0
+    x.requires_grad_(True)
+    loss, rewards = FT.preference_loss(x, t, torch.tensor(starts, device=dev()), reference=ref, beta=0.05, smoothing=0.2)
+    (dx,) = torch.autograd.grad(loss, x)
+    _check_preference(x, t, starts, ref, 0.05, 0.2, loss.detach(), rewards, dx)
+    # out of order, of 32 bits, not dense
+    given = torch.tensor(starts, device=dev(), dtype=torch.int32)
+    meant = given.clone()
+    given[1000], given[4095], given[-3] = rows + 9, -7, 0
+    apart = torch.stack([given, given + 1], 1)[:, 0]
+    out = FT.preference_loss(x, t, apart, reference=ref)
+    meant[1000:] = rows
+    for a, b in zip((*out, *torch.autograd.grad(out[0], x)), (*(o := FT.preference_loss(x, t, meant, reference=ref)), *torch.autograd.grad(o[0], x))):
+        assert torch.equal(a, b)
+
+
+def test_a_million_pairs(kernels_only):
+    """Most of them empty: their reward is 0, their loss log 2."""
+    n, rows = 1 << 20, 64
+    x, t = _inputs(rows, 50, f32)
+    l, _, e, _ = _reference(x, t)
+    at = torch.arange(rows, device=dev()) * 1009
+    starts = torch.searchsorted(at, torch.arange(2 * n + 1, device=dev()))
+    loss, rewards = FT.preference_loss(x, t, starts, beta=1.0)
+    sums = torch.zeros(2 * n, dtype=f64, device=dev())
+    sums[at] = l  # row i is the sequence between two starts that differ by it
+    _within(rewards, sums.view(n, 2), (e + 2 * U32 * l.abs().max()) * (sums != 0).view(n, 2), "rewards")
+    D = sums[0::2] - sums[1::2]
+    _within(loss, torch.nn.functional.softplus(-D).mean(), 2 * e * (rows / n) + 2 * U32, "loss")
