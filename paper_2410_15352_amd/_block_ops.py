@@ -70,6 +70,17 @@ def _stream(t):
     return torch._C._cuda_getCurrentRawStream(t.get_device())
 
 
+def _capture(stream):
+    """Which graph capture work on the stream goes into; 0: none.  What one call forms ahead for another
+    is there, and as it was, only where both go into the same: replays come in any order and number."""
+    fn = _fns.get("capture")
+    if fn is None:
+        fn = _lib.load().compact_stream_capture
+        fn.restype, fn.argtypes = _i64, [_vp]
+        _fns["capture"] = fn
+    return fn(stream)
+
+
 _TYPES = (torch.Tensor, torch.nn.Parameter)
 _is_compiling, _is_tracing, _autocast = torch.compiler.is_compiling, torch._C._is_tracing, torch.is_autocast_enabled
 _dispatch_modes, _functorch_level = torch._C._len_torch_dispatch_stack, torch._C._functorch.peek_interpreter_stack

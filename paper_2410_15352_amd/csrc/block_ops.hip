@@ -445,6 +445,17 @@ using namespace compact;
 
 extern "C" {
 
+// Which graph capture the stream's work goes into: another number above 0 for each; 0: it runs as it is launched.
+int64_t compact_stream_capture(void* stream) {
+  hipStreamCaptureStatus state = hipStreamCaptureStatusNone;
+  unsigned long long id = 0;
+  if (hipStreamGetCaptureInfo(static_cast<hipStream_t>(stream), &state, &id) != hipSuccess) {
+    (void)hipGetLastError();
+    return 0;
+  }
+  return state == hipStreamCaptureStatusNone ? 0 : static_cast<int64_t>(id) + 1;
+}
+
 int compact_block_rmsnorm_fwd(const RmsNormArgs* a, void* stream) {
   if (a->rows < 1 || a->rows > int64_t(1) << 31 || a->d < 8 || a->d % 8 != 0 || a->d > kRmsNormMaxD) return -1;
   hipStream_t s = static_cast<hipStream_t>(stream);

@@ -308,7 +308,7 @@ class _PolicyFn(torch.autograd.Function):
     """The loss, and with it the gradient for dloss = 1, while a row is in registers: the
     backward finds dloss to be 1 on the GPU and leaves it, or forms it again.  (The gradient is
     held beside the logits till then, not as a saved tensor: what the backward returns must not
-    be shared.)"""
+    be shared.)  A backward that is captured without its forward, or the other way round, forms its own."""
 
     @staticmethod
     def forward(ctx, logits, targets, old, advantages, reference, rule):
@@ -316,6 +316,7 @@ class _PolicyFn(torch.autograd.Function):
         logp = torch.empty(logits.shape[0], dtype=_f32, device=logits.device)
         ctx.dx = torch.empty_like(logits)
         ctx.scratch = _policy_call(logits, targets, old, advantages, reference, rule, None, loss=loss, logp=logp, dx=ctx.dx)
+        ctx.capture = ops._capture(_stream(logits))
         ctx.rule = rule
         ctx.size = logits.dtype, logits.shape
         ctx.save_for_backward(logits, targets, old, advantages, reference)
@@ -334,7 +335,8 @@ class _PolicyFn(torch.autograd.Function):
                 or not _rows_usable(logits, targets, *rows)):
             return ops._torch_grad(lambda t: _policy_torch(t, targets.to(torch.int64), *rows, *ctx.rule)[0], logits, dloss), *none
         dx, ctx.dx = ctx.dx, None
-        first = dx is not None  # a second backward over a retained graph forms its own
+        # (a second backward over a retained graph forms its own, too)
+        first = dx is not None and ctx.capture == ops._capture(_stream(logits))
         dx = dx if first else torch.empty_like(logits)
         _policy_call(logits, targets, *rows, ctx.rule, ctx.scratch, dx=dx, dloss=dloss.float(), unless_one=first)
         return dx, *none

@@ -886,13 +886,14 @@ class _DistillFn(torch.autograd.Function):
     """The loss, and with it the gradient for dloss = 1, while a row is in registers: the
     backward finds dloss to be 1 on the GPU and leaves it, or forms it again.  (The gradient is
     held beside the logits till then, not as a saved tensor: what the backward returns must not
-    be shared.)"""
+    be shared.)  A backward that is captured without its forward, or the other way round, forms its own."""
 
     @staticmethod
     def forward(ctx, logits, top, ids, targets, temperature, weight):
         loss = torch.empty((), dtype=torch.float32, device=logits.device)
         ctx.dx = torch.empty_like(logits)
         ctx.scratch = _distill_call(logits, top, ids, targets, None, temperature, weight, loss=loss, dx=ctx.dx)
+        ctx.capture = ops._capture(_stream(logits))
         ctx.rule = temperature, weight
         ctx.size = logits.dtype, logits.shape, top.shape
         ctx.save_for_backward(logits, top, ids, targets)
@@ -910,7 +911,8 @@ class _DistillFn(torch.autograd.Function):
             return (ops._torch_grad(lambda t: _distill_torch(t, top, ids, targets, *rule), logits, dloss),
                     None, None, None, None, None)
         dx, ctx.dx = ctx.dx, None
-        first = dx is not None  # a second backward over a retained graph forms its own
+        # (a second backward over a retained graph forms its own, too)
+        first = dx is not None and ctx.capture == ops._capture(_stream(logits))
         dx = dx if first else torch.empty_like(logits)
         _distill_call(logits, top, ids, targets, ctx.scratch, *rule, dx=dx, dloss=dloss.float(), unless_one=first)
         return dx, None, None, None, None, None

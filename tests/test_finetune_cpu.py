@@ -327,3 +327,25 @@ def test_functorch_takes_the_expressions():
     assert torch.allclose(g, e)
     l = torch.func.vmap(lambda x: FT.token_logprobs(x, t))(torch.stack((x, 2 * x)))
     assert torch.allclose(l[1], FT.token_logprobs(2 * x, t))
+
+
+@pytest.mark.parametrize("forward,backward,held", [(0, 0, True), (7, 7, True), (0, 7, False), (7, 0, False), (7, 8, False)])
+def test_the_gradient_held_for_the_backward(launches, monkeypatch, forward, backward, held):
+    """The one that the forward formed is given only where both go into the same graph, or into none, and once."""
+    where, buffers = [forward], []
+    monkeypatch.setattr(FT.ops, "_capture", lambda stream: where[0])
+    call = FT._policy_call
+
+    def policy_call(*a, dx=None, unless_one=False, **k):
+        buffers.append((dx.data_ptr(), unless_one))
+        return call(*a, dx=dx, unless_one=unless_one, **k)
+
+    monkeypatch.setattr(FT, "_policy_call", policy_call)
+    x, t = _inputs(9, 16, bf16)
+    x.requires_grad_()
+    y = _fns(x, t)["policy"][0](x)
+    where[0] = backward
+    g, h = (torch.autograd.grad(y, x, retain_graph=True)[0] for _ in range(2))
+    formed = buffers[0][0]
+    assert buffers[1] == (g.data_ptr(), held) and (g.data_ptr() == formed) == held
+    assert buffers[2] == (h.data_ptr(), False) and h.data_ptr() != g.data_ptr()
