@@ -454,8 +454,9 @@ def clip_grad_norm(tensors, max_norm=None):
         min(1, max_norm / (norm + 1e-6)).
 
     tensors: gradients of any shapes on one device, one or an iterable of them; None among them,
-    as of a parameter without a gradient, is passed over, and one that is given twice counts once.
-    Of a norm that is infinite, finite gradients become 0; of one that is NaN, all become NaN.
+    as of a parameter without a gradient, is passed over, and one that is given twice, in whatever
+    shape or order of its dimensions, counts once.  Tensors that share a part of their elements are
+    refused, also where only the norm is asked for.  Of a norm that is infinite, finite gradients become 0; of one that is NaN, all become NaN.
 
     The kernels take dense bf16 and fp32 tensors, mixed, in any order of their dimensions; views of
     others that are not dense are copied, and back.  Squares are added in fp64.  Nothing is
@@ -482,8 +483,8 @@ def clip_grad_norm(tensors, max_norm=None):
     if any(t.device != device for t in given):
         raise ValueError("clip_grad_norm: tensors of one device")
     given = [t for t in given if t.numel() > 0]
-    if all(map(_plain, given)):
-        given = list({(t.data_ptr(), t.shape, t.stride(), t.dtype): t for t in given}.values())
+    if given and device.type != "meta" and all(map(_plain, given)):
+        given = _distinct(given)
     if max_norm is not None and any(not t.is_contiguous() and torch._debug_has_internal_overlap(t) == 1 for t in given):
         raise ValueError("clip_grad_norm: a tensor whose elements lie on one another is not scaled")
     if given and _eager():
@@ -498,6 +499,67 @@ def clip_grad_norm(tensors, max_norm=None):
                 _changed(given)
             return norm
     return _clip_torch(given, max_norm, device)
+
+
+def _memory(t):
+    """Where a tensor's elements lie, whatever their order and shape: (address, an element's bytes, ((stride in bytes,
+    count), ..)), the widest stride first, dimensions that continue one another joined."""
+    size, dims = t.element_size(), []
+    if t.is_contiguous():
+        n = t.numel()
+        return t.data_ptr(), size, ((size, n),) if n > 1 else ()
+    for stride, n in sorted(((s * size, n) for s, n in zip(t.stride(), t.shape) if n > 1), reverse=True):
+        if dims and dims[-1][0] == stride * n:
+            dims[-1] = (stride, dims[-1][1] * n)
+        else:
+            dims.append((stride, n))
+    return t.data_ptr(), size, tuple(dims)
+
+
+def _extent(memory):
+    """Bytes from the first element's to the last one's end."""
+    _, size, dims = memory
+    return size + sum(stride * (n - 1) for stride, n in dims)
+
+
+def _apart(a, b):
+    """No byte of one tensor is the other's."""
+    if a[0] > b[0]:
+        a, b = b, a
+    ahead = b[0] - a[0]
+    if ahead >= _extent(a):
+        return True
+    if all(not dims or len(dims) == 1 and dims[0][0] == size for _, size, dims in (a, b)):
+        return False  # dense, both
+    # slices of one tensor: the strides of the dimensions outside are multiples of g, and what lies inside
+    # takes places of its own in every g bytes
+    for least in {stride for _, _, dims in (a, b) for stride, _ in dims if stride > 0}:
+        outside = [stride for _, _, dims in (a, b) for stride, _ in dims if stride >= least]
+        g = math.gcd(*outside)
+        inside = [_extent((at, size, [d for d in dims if d[0] < least])) for at, size, dims in (a, b)]
+        if inside[0] <= ahead % g <= g - inside[1]:
+            return True
+    unit = math.gcd(ahead, a[1], b[1], *(stride for _, _, dims in (a, b) for stride, _ in dims))
+    mark = torch.zeros(max(_extent(a), ahead + _extent(b)) // unit, dtype=torch.bool)
+    places = []
+    for first, (_, size, dims) in ((0, a), (ahead, b)):
+        dims = [d for d in dims if d[0] > 0] + [(unit, size // unit)]
+        places.append(mark.as_strided([n for _, n in dims], [stride // unit for stride, _ in dims], first // unit))
+    places[0].fill_(True)
+    return not places[1].any()
+
+
+def _distinct(tensors):
+    """The tensors, without those that hold an earlier one's elements."""
+    found, live = {}, []
+    for t in tensors:
+        found.setdefault((_memory(t), t.dtype), t)
+    for memory, _ in sorted(found, key=lambda m: m[0][0]):
+        live = [m for m in live if m[0] + _extent(m) > memory[0]]
+        if not all(_apart(m, memory) for m in live):
+            raise ValueError("clip_grad_norm: two of the tensors overlap")
+        live.append(memory)
+    return list(found.values())
 
 
 def _changed(tensors):
