@@ -385,12 +385,13 @@ __global__ __launch_bounds__(THREADS, 4) void k_policy(PolicyArgs a) {
       const double l = log_prob(xt, m, s);
       const float lo = 1.0f - a.low, hi = 1.0f + a.high, ratio = expf(static_cast<float>(l - static_cast<double>(old)));
       const bool clamped = (A > 0.0f && ratio > hi) || (A < 0.0f && ratio < lo);
+      const bool idle = A == 0.0f && ratio == ratio;  // (a ratio that overflowed must not become 0 x inf)
       const float away = a.reference != nullptr ? static_cast<float>(static_cast<double>(ref) - l) : 0.0f;
       const float odds = a.reference != nullptr ? expm1f(away) : 0.0f;
-      g = clamped ? 0.0f : -A * ratio;
+      g = clamped || idle ? 0.0f : -A * ratio;
       if (a.reference != nullptr) g -= a.kl * odds;
       if (a.loss_row != nullptr && tid == 0) {
-        float loss = -A * (clamped ? (A > 0.0f ? hi : lo) : ratio);
+        float loss = idle ? 0.0f : -A * (clamped ? (A > 0.0f ? hi : lo) : ratio);
         if (a.reference != nullptr) loss += a.kl * (odds - away);
         a.loss_row[row] = loss;
         a.logp[row] = static_cast<float>(l);

@@ -281,8 +281,9 @@ def _policy_torch(logits, targets, old, advantages, reference, low, high, kl):
     with torch.no_grad():
         ratio = torch.exp(log_ratio)
         clamped = (A > 0) & (ratio > 1 + high) | (A < 0) & (ratio < 1 - low)
-    # (not a minimum: past its bound the ratio may be infinite, and its gradient NaN)
-    ratio = torch.exp(torch.where(clamped, 0.0, log_ratio))
+        idle = (A == 0) & ~ratio.isnan()
+    # (not a minimum: past its bound, or without an advantage, the ratio may be infinite, and its gradient NaN)
+    ratio = torch.exp(torch.where(clamped | idle, 0.0, log_ratio))
     each = -A * torch.where(clamped, torch.where(A > 0, A.new_full((), 1 + high), A.new_full((), 1 - low)), ratio)
     if reference is not None:
         away = torch.where(counts, reference.to(wide), 0.0) - l
@@ -353,7 +354,8 @@ def policy_loss(logits, targets, old, advantages, reference=None, clip=0.2, kl=0
     of the same tokens under the policy that sampled, and under the model that it is held to (needed
     where kl > 0).  clip: low and high, or one number for both; low at most 1.  logprobs (rows,):
     l, 0 where a row does not count, without a gradient.  A row that counts for none of it (r
-    clamped away, no KL term) has a gradient of zero; a target past V makes its row and the loss NaN.
+    clamped away or A zero, no KL term) has a gradient of zero, also where r overflows; a target past V
+    makes its row and the loss NaN.
 
     fp32 results (fp64 of fp64 logits).  The kernels form the gradient with the loss and hold it
     for the backward, as many bytes as the logits.  Of a loss that is multiplied before its backward

@@ -349,3 +349,27 @@ def test_the_gradient_held_for_the_backward(launches, monkeypatch, forward, back
     formed = buffers[0][0]
     assert buffers[1] == (g.data_ptr(), held) and (g.data_ptr() == formed) == held
     assert buffers[2] == (h.data_ptr(), False) and h.data_ptr() != g.data_ptr()
+
+
+@pytest.mark.parametrize("dtype", [f32, f64])
+@pytest.mark.parametrize("kl", [0.0, 0.3])
+def test_policy_of_no_advantage(dtype, kl):
+    """A row whose advantage is zero has no part but the KL term's, however far its ratio is off; one whose
+    ratio is not a number has it all the same."""
+    x, t, old, A, ref = _policy_inputs()
+    x = x.to(dtype).requires_grad_()
+    A[1] = A[2] = 0.0
+
+    def run(old):
+        loss, _ = FT.policy_loss(x, t, old, A, reference=ref, kl=kl)
+        return loss, torch.autograd.grad(loss, x)[0]
+
+    loss, g = run(old)
+    for far in (-1000.0, 1000.0, -math.inf):
+        o = old.clone()
+        o[1] = far
+        assert all(torch.equal(a, b) for a, b in zip(run(o), (loss, g)))
+    assert g[1].any() == (kl > 0)
+    o[2] = math.nan
+    bad, h = run(o)
+    assert bad.isnan() and h[2].isnan().all() and h[3].isfinite().all()
