@@ -405,8 +405,9 @@ def _clip_torch(tensors, max_norm, device):
 def _clip_pieces(entries, n):
     fn = _fns.get("pieces")
     if fn is None:
-        fn = _fns["pieces"] = _lib.load().compact_clip_pieces
+        fn = _lib.load().compact_clip_pieces
         fn.restype, fn.argtypes = _i64, [_vp, _i64, _vp]
+        _fns["pieces"] = fn  # (for other threads to find: complete)
     order = array("q", bytes(8 * n))
     return fn(entries, n, order.buffer_info()[0])
 

@@ -490,8 +490,9 @@ def _empty_heads(shape, device):
 def _attn_scratch(block):
     fn = _fns.get("scratch")
     if fn is None:
-        fn = _fns["scratch"] = _lib.load().compact_attention_bwd_scratch
+        fn = _lib.load().compact_attention_bwd_scratch
         fn.restype, fn.argtypes = _i64, [_block]
+        _fns["scratch"] = fn  # (for other threads to find: complete)
     return fn(block)
 
 
@@ -702,8 +703,9 @@ def packed_wants_table(n, rows, heads):
 def _packed_scratch(block, n):
     fn = _fns.get("packed")
     if fn is None:
-        fn = _fns["packed"] = _lib.load().compact_packed_bwd_scratch
+        fn = _lib.load().compact_packed_bwd_scratch
         fn.restype, fn.argtypes = _i64, [_block, ctypes.c_int]
+        _fns["packed"] = fn
     return fn(block, n)
 
 
