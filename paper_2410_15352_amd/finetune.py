@@ -442,8 +442,8 @@ def _clip_apply(entries, device, max_norm):
         raise ValueError("clip_grad_norm: two of the tensors overlap")
     if pieces < 0:
         return None
-    scratch = torch.empty(pieces + 1, dtype=torch.float64, device=device)
-    out = scratch[pieces:].view(_f32)
+    scratch = torch.empty(pieces, dtype=torch.float64, device=device)
+    out = torch.empty(2, dtype=_f32, device=device)  # (not a part of the scratch, which a norm that is kept would keep)
     ops._call("compact_clip", at, n, 0.0 if max_norm is None else max_norm, max_norm is not None, scratch.data_ptr(), pieces,
               out.data_ptr(), _stream(scratch))
     return out[0]

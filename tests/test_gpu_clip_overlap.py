@@ -45,3 +45,9 @@ def test_slices_beside_one_another(beside):
     t = [m[:32, :40], m[:32, 40:], m[32:, ::2], m[32:, 1::2], m[:0]]
     got = FT.clip_grad_norm([*t, *BESIDE[beside](), t[1].t()], 1.0)
     assert math.isclose(float(got), m.numel() ** 0.5, rel_tol=1e-6) and (m - m.numel() ** -0.5).abs().max() < 1e-8
+
+
+def test_a_norm_that_is_kept_keeps_nothing_else():
+    t = [torch.ones(1 << 22, device=dev()) for _ in range(3)]
+    norms = [FT.clip_grad_norm(t, bound) for bound in (None, 1e9, 1.0)]
+    assert all(n.untyped_storage().nbytes() <= 16 for n in norms)
