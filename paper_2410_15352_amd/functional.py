@@ -635,7 +635,15 @@ def _bounds(starts, rows):
 
 
 def packed_positions(starts, rows):
-    """The position of each of `rows` rows in its sequence (int64; 0 for rows of none), for Rotary."""
+    """The position of each of `rows` rows in its sequence (int64; 0 for rows of none), for Rotary.
+    starts (n + 1,): as packed_attention takes them."""
+    if not isinstance(starts, _Tensor):
+        raise TypeError("packed_positions: starts is a tensor")
+    if starts.dim() != 1 or starts.shape[0] < 2 or starts.dtype not in (torch.int32, torch.int64):
+        raise ValueError("packed_positions: starts (n + 1,), n >= 1, of int32 or int64")
+    rows = rows if isinstance(rows, torch.SymInt) else index(rows)  # (a traced size stays one)
+    if rows < 0:
+        raise ValueError("packed_positions: rows >= 0")
     e, i = _bounds(starts, rows), torch.arange(rows, device=starts.device)
     s = torch.searchsorted(e, i, right=True)
     return torch.where((s > 0) & (s < len(e)), i - e[(s - 1).clamp(min=0)], 0)

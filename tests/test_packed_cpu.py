@@ -200,3 +200,22 @@ def test_functorch_and_compile_take_the_expressions():
     o = torch.func.vmap(lambda a, b, c: F.packed_attention(a, b, c, starts, window=3))(q, k, v)
     for i in range(3):
         assert torch.allclose(o[i], F.packed_attention(q[i], k[i], v[i], starts, window=3))
+
+
+@pytest.mark.parametrize("error,call", [
+    (TypeError, lambda: F.packed_positions([0, 4], 4)),
+    (ValueError, lambda: F.packed_positions(torch.empty(0, dtype=torch.int64), 4)),  # (nothing to look a row's start up in)
+    (ValueError, lambda: F.packed_positions(torch.tensor([0]), 4)),
+    (ValueError, lambda: F.packed_positions(torch.tensor([[0, 4]]), 4)),
+    (ValueError, lambda: F.packed_positions(torch.tensor([0.0, 4.0]), 4)),
+    (ValueError, lambda: F.packed_positions(torch.tensor([0, 4]), -1)),
+    (TypeError, lambda: F.packed_positions(torch.tensor([0, 4]), 4.0))])
+def test_positions_refuse(error, call):
+    with pytest.raises(error):
+        call()
+
+
+def test_positions_of_no_rows_and_empty_sequences():
+    assert F.packed_positions(torch.tensor([0, 0]), 0).tolist() == []
+    assert F.packed_positions(torch.tensor([2, 2, 2], dtype=torch.int32), 4).tolist() == [0, 0, 0, 0]
+    assert F.packed_positions(torch.tensor([1, 3, 3, 5]), 6).tolist() == [0, 0, 1, 0, 1, 0]
