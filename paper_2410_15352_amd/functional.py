@@ -410,15 +410,15 @@ def _attention_expressions(q, k, v, window, sinks, lengths, scale):
 
 def _attend(qw, kw, vw, seen, scale):
     """softmax(scale q k^T) v over the keys seen."""
-    used = seen.any(2).unsqueeze(-1)  # (what lies past a sequence, or before every window, may be anything)
-    kw, vw = torch.where(used, kw, 0.0), torch.where(used, vw, 0.0)
+    # (what lies past a sequence, or before every window, may be anything; so may rows that see no key, and their gradient)
+    used, some = seen.any(2).unsqueeze(-1), seen.any(-1, keepdim=True)
+    qw, kw, vw = torch.where(some, qw, 0.0), torch.where(used, kw, 0.0), torch.where(used, vw, 0.0)
     s = torch.matmul(qw, kw.transpose(2, 3).contiguous()) * scale
     s = torch.where(seen, s, -math.inf)
-    some = seen.any(-1, keepdim=True)
     top = torch.where(some, s.detach().amax(-1, keepdim=True), 0.0)
     e = torch.exp(s - top)
     p = e / torch.where(some, e.sum(-1, keepdim=True), 1.0)
-    return torch.matmul(p, vw)
+    return torch.where(some, torch.matmul(p, vw), 0.0)
 
 
 FEW_ROWS = 32

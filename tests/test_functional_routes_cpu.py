@@ -461,3 +461,21 @@ def test_factors_past_fp32_are_the_torch_expressions(launches):
     assert launches == []
     F.window_attention(q, k, v, scale=1e-3)
     assert launches == ["compact_attention_fwd"]
+
+
+@pytest.mark.parametrize("which", ["q", "do"])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_rows_that_see_no_key_may_hold_anything(which, bad):
+    """They pass no gradient, whatever stands in them or comes to them."""
+    given = {n: _rand(2, h, l, 8, seed=s, dtype=f64) for n, h, l, s in (("q", 4, 5, 1), ("k", 2, 6, 2), ("v", 2, 6, 3), ("do", 4, 5, 4))}
+
+    def run(given):
+        q, k, v = (given[n].clone().requires_grad_() for n in "qkv")
+        o = F.window_attention(q, k, v, lengths=torch.tensor([3, 6]), window=4, sinks=1)
+        return o, *torch.autograd.grad(o, (q, k, v), given["do"])
+
+    want = run(given)
+    given[which] = given[which].clone()
+    given[which][0, :, :2] = bad
+    for a, b in zip(run(given), want):
+        assert torch.equal(a, b)

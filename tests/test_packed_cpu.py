@@ -219,3 +219,23 @@ def test_positions_of_no_rows_and_empty_sequences():
     assert F.packed_positions(torch.tensor([0, 0]), 0).tolist() == []
     assert F.packed_positions(torch.tensor([2, 2, 2], dtype=torch.int32), 4).tolist() == [0, 0, 0, 0]
     assert F.packed_positions(torch.tensor([1, 3, 3, 5]), 6).tolist() == [0, 0, 1, 0, 1, 0]
+
+
+@pytest.mark.parametrize("which", ["q", "k", "v", "do"])
+@pytest.mark.parametrize("dtype", [torch.float16, f32, f64])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_rows_of_no_sequence_may_hold_anything(which, dtype, bad):
+    """Neither the rows before the first sequence nor those behind the last reach a result or a gradient."""
+    given = {n: _rand(9, h, 8, seed=s, dtype=dtype) for n, h, s in (("q", 4, 1), ("k", 2, 2), ("v", 2, 3), ("do", 4, 4))}
+    starts = torch.tensor([1, 4, 4, 7])
+
+    def run(given):
+        q, k, v = (given[n].clone().requires_grad_() for n in "qkv")
+        o = F.packed_attention(q, k, v, starts, window=2, sinks=1)
+        return o, *torch.autograd.grad(o, (q, k, v), given["do"])
+
+    want = run(given)
+    given[which] = given[which].clone()
+    given[which][0], given[which][7:] = bad, bad
+    for a, b in zip(run(given), want):
+        assert torch.equal(a, b) and not a[0].any() and not a[7:].any()
