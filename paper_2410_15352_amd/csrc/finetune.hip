@@ -116,8 +116,9 @@ __global__ __launch_bounds__(256) void k_token_bwd(TokenArgs a) {
   float g = 0.0f;
   if (target != a.ignore_index) {
     g = a.grad[row];
+    // (of a pair with a target past V the slope is NaN already; in a row of no pair it does not count)
     if (a.dloss != nullptr) g *= a.dloss[0];
-    if (target < 0 || target >= a.V) g = __builtin_nanf("");
+    else if (target < 0 || target >= a.V) g = __builtin_nanf("");
   }
   g = uniform(g);
   if (g == 0.0f) {

@@ -169,12 +169,12 @@ def token_logprobs(logits, targets):
 def _preference_torch(logits, targets, starts, reference, beta, smoothing):
     """The loss and the rewards as torch expressions, in fp32 with sums in fp64 (fp64 for fp64)."""
     rows, pairs = logits.shape[0], (starts.shape[0] - 1) // 2
-    l, counts = _logprobs_torch(logits, targets)
+    e = _bounds(starts, rows)
+    s = torch.searchsorted(e, torch.arange(rows, device=e.device), right=True)
+    l, counts = _logprobs_torch(logits, torch.where((s > 0) & (s < len(e)), targets, IGNORE))
     gain = l.double()
     if reference is not None:
         gain = torch.where(counts, gain - reference.double(), 0.0)
-    e = _bounds(starts, rows)
-    s = torch.searchsorted(e, torch.arange(rows, device=e.device), right=True)
     sums = torch.zeros(2 * pairs + 2, dtype=torch.float64, device=e.device).index_add(0, s, gain)[1:-1].view(pairs, 2)
     rewards = beta * sums
     delta = rewards[:, 0] - rewards[:, 1]

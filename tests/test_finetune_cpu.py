@@ -373,3 +373,28 @@ def test_policy_of_no_advantage(dtype, kl):
     o[2] = math.nan
     bad, h = run(o)
     assert bad.isnan() and h[2].isnan().all() and h[3].isfinite().all()
+
+
+@pytest.mark.parametrize("spoil", ["logits", "reference", "target"])
+def test_preference_rows_of_no_sequence(spoil):
+    """They may hold anything, a target past V too: no part in the loss, and a gradient of zero."""
+    x, t = _inputs()
+    t[8], starts, ref = 3, torch.tensor([2, 4, 7]), _rand(9, seed=3)
+
+    def run(x, t, ref):
+        x = x.clone().requires_grad_()
+        loss, rewards = FT.preference_loss(x, t, starts, reference=ref)
+        return loss, rewards, torch.autograd.grad(loss, x)[0]
+
+    want = run(x, t, ref)
+    x, t, ref = x.clone(), t.clone(), ref.clone()
+    for row in (1, 7, 8):
+        if spoil == "logits":
+            x[row] = math.nan
+        elif spoil == "reference":
+            ref[row] = math.nan
+        else:
+            t[row] = 7
+    for a, b in zip(run(x, t, ref), want):
+        assert torch.equal(a, b)
+    assert not want[2][:2].any() and not want[2][7:].any()
