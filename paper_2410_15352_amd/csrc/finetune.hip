@@ -262,14 +262,21 @@ __global__ __launch_bounds__(256) void k_pairs(PairArgs a) {
 }
 
 // A few pairs: a wave each, and their mean, in one workgroup.  us, this / a workgroup per pair and the
-// mean's launch: 200 rows, 2 pairs 4.1 / 6.8; 8192 rows, 2 pairs 7.2 / 7.2, 16 pairs 6.3 / 6.9, 64
-// pairs 18 / 6.9; 32768 rows, 16 pairs 8.0 / 6.7.  (A launch on the host is 3 more.)
+// mean's launch (which on the host is 3 more), by rows and pairs:
+//             1 pair       2            4           8          16          64
+//     200   3.7 / 5.9   3.7 / 6.0   4.1 / 6.1   4.6 / 6.2   5.4 / 6.2
+//    2048   5.0 / 6.0   4.3 / 6.2   4.5 / 6.1   4.9 / 6.3   5.6 / 6.2
+//    4096   6.8 / 6.3   5.3 / 6.3   4.9 / 6.4   4.7 / 6.2   5.9 / 6.3
+//    8192  10.5 / 7.4   7.1 / 6.7   5.8 / 6.4   5.2 / 6.5   5.8 / 6.3    18 / 6.9
+//   16384  17.9 / 9.2  10.7 / 7.6   7.6 / 6.8   6.2 / 6.6   6.4 / 6.5
+//   32768  32.3 / 12.9 18.2 / 9.4  11.2 / 7.7   8.1 / 6.9   7.6 / 6.5
 constexpr int kFewPairs = 16;
-constexpr int64_t kFewPairRows = 16384;
+constexpr int64_t kFewPairRows = 16384, kFewRowsEach = 4096;
+bool few_pairs(int64_t n, int64_t rows) { return n <= kFewPairs && rows <= kFewPairRows && rows <= n * kFewRowsEach; }
 __global__ __launch_bounds__(1024) void k_few_pairs(PairArgs a) {
   __shared__ double loss[kFewPairs];
-  const int lane = threadIdx.x & 63;
-  for (int pair = threadIdx.x >> 6; pair < a.n; pair += 16) {
+  const int lane = threadIdx.x & 63, pair = threadIdx.x >> 6;
+  if (pair < a.n) {
     const double v = pair_loss<64>(a, pair, lane, nullptr);
     if (lane == 0) loss[pair] = v;
   }
@@ -490,7 +497,7 @@ int compact_token_logprobs(const TokenArgs* a, void* stream) {
 int compact_preference_pairs(const PairArgs* a, void* stream) {
   if (!rows_ok(a->rows, 1) || a->n < 1 || a->n >= int64_t(1) << 24) return -1;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (a->n <= kFewPairs && a->rows <= kFewPairRows && a->bounds == nullptr) {
+  if (few_pairs(a->n, a->rows) && a->bounds == nullptr) {
     hipLaunchKernelGGL(k_few_pairs, dim3(1), dim3(1024), 0, s, *a);
     return status();
   }
