@@ -16,7 +16,8 @@
 //
 // All are bound by HBM: the logits of a row that counts are read once for l, and once more for the
 // gradient where that needs sums over other rows first (log-probabilities, preference); the policy
-// loss holds a row in registers and forms both.  Measured, of 32000 bf16 logits, 7 of 10 rows counting:
+// loss holds a row in registers and forms both.  (Up to 131072 bf16 or 65536 fp32 logits; what a row has
+// past them is read for its maximum, its sum and its gradient.)  Measured, of 32000 bf16 logits, 7 of 10 rows counting:
 // l of 8192 rows 69 us, 5.3 TB/s, the same right after the gradient of others was written 104 us; the
 // gradient 150 us, 5.9 TB/s (some of the logits are still in the cache); the policy loss with its
 // gradient 192 us, 4.6 TB/s, and of 4096 rows of 131072 400 us, 4.6 TB/s, where a large copy reaches
@@ -461,6 +462,15 @@ void launch_policy(const PolicyArgs& a, hipStream_t s) {
   //    8192 x  32001 280      264      227*      300       544
   //    2048 x  65536 181      174      154       121*      171
   //    1024 x 200000 322      317      303       255       225*
+  // in fp32, with the launches of the count and the mean:
+  //   16384 x   1000  53*      67      148       291       599
+  //   16384 x   2000  66       68*     150       291       605
+  //    8192 x   4096  55       53*      82       153       309
+  //    8192 x   8000 137      122      115*      172       319
+  //    8192 x  16384 278      256      218*      227       350
+  //    4096 x  32000 316      301      254       210*      245
+  //    2048 x  65536 380      369      330       259       228*
+  //    1024 x 131072 379      375      362       330       284*  (3.8 TB/s of one read and one write: half of a row in registers)
   const int64_t chunks = a.V / (F32 ? 4 : 8);
   if (chunks <= 256) launch_policy<F32, 256, 1>(a, s);
   else if (chunks <= 1024) launch_policy<F32, 256, 4>(a, s);

@@ -203,7 +203,8 @@ class _PreferenceFn(torch.autograd.Function):
         _token_call(logits, targets, reference=reference, out=gain, stats=stats)
         ops._call("compact_preference_pairs",
                   _pair_pack(gain.data_ptr(), starts.data_ptr(), rewards.data_ptr(), slope.data_ptr(), each.data_ptr(),
-                             loss.data_ptr(), each.data_ptr() + 4 * pairs if bounds else 0, starts.stride(0), rows, pairs, starts.dtype == torch.int64, beta, smoothing),
+                             loss.data_ptr(), each.data_ptr() + 4 * pairs if bounds else 0, starts.stride(0), rows, pairs,
+                             starts.dtype == torch.int64, beta, smoothing),
                   _stream(logits))
         if tracked:
             ctx.rule = beta, smoothing
@@ -358,8 +359,9 @@ def policy_loss(logits, targets, old, advantages, reference=None, clip=0.2, kl=0
     makes its row and the loss NaN.
 
     fp32 results (fp64 of fp64 logits).  The kernels form the gradient with the loss and hold it
-    for the backward, as many bytes as the logits.  Of a loss that is multiplied before its backward
-    it is formed a second time there."""
+    for the backward, as many bytes as the logits.  Of a loss that is multiplied before its backward,
+    or whose forward and backward are not captured into one graph but into two, or one of them alone, it
+    is formed a second time there."""
     _check_logits("policy_loss", logits, targets)
     if old is None or advantages is None:
         raise TypeError("policy_loss: old and advantages are tensors")
@@ -459,7 +461,8 @@ def clip_grad_norm(tensors, max_norm=None):
     tensors: gradients of any shapes on one device, one or an iterable of them; None among them,
     as of a parameter without a gradient, is passed over, and one that is given twice, in whatever
     shape or order of its dimensions, counts once.  Tensors that share a part of their elements are
-    refused, also where only the norm is asked for.  Of a norm that is infinite, finite gradients become 0; of one that is NaN, all become NaN.
+    refused, also where only the norm is asked for.  Of a norm that is infinite, finite gradients
+    become 0; of one that is NaN, all become NaN.
 
     The kernels take dense bf16 and fp32 tensors, mixed, in any order of their dimensions; views of
     others that are not dense are copied, and back.  Squares are added in fp64.  Nothing is
