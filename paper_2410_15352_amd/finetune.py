@@ -489,7 +489,7 @@ def clip_grad_norm(tensors, max_norm=None):
     if any(t.device != device for t in given):
         raise ValueError("clip_grad_norm: tensors of one device")
     given = [t for t in given if t.numel() > 0]
-    if given and device.type != "meta" and all(map(_plain, given)):
+    if all(map(_plain, given)):
         given = _distinct(given)
     if max_norm is not None and any(not t.is_contiguous() and torch._debug_has_internal_overlap(t) == 1 for t in given):
         raise ValueError("clip_grad_norm: a tensor whose elements lie on one another is not scaled")
@@ -558,14 +558,16 @@ def _apart(a, b):
 def _distinct(tensors):
     """The tensors, without those that hold an earlier one's elements."""
     found, live = {}, []
+    nowhere = [t for t in tensors if t.data_ptr() == 0]  # (of the meta device, zeros without memory)
     for t in tensors:
-        found.setdefault((_memory(t), t.dtype), t)
+        if t.data_ptr() != 0:
+            found.setdefault((_memory(t), t.dtype), t)
     for memory, _ in sorted(found, key=lambda m: m[0][0]):
         live = [m for m in live if m[0] + _extent(m) > memory[0]]
         if not all(_apart(m, memory) for m in live):
             raise ValueError("clip_grad_norm: two of the tensors overlap")
         live.append(memory)
-    return list(found.values())
+    return [*found.values(), *nowhere]
 
 
 def _changed(tensors):

@@ -93,3 +93,4 @@ def test_against_every_byte():
 def test_no_memory_to_look_at():
     """Tensors of the meta device lie nowhere."""
     assert FT.clip_grad_norm([torch.ones(3, device="meta"), torch.ones(2, device="meta")], 1.0).shape == ()
+    assert FT.clip_grad_norm([torch._efficientzerotensor(3), torch.ones(4), torch._efficientzerotensor(4)]) == 2.0
