@@ -23,8 +23,7 @@
 // gradient 192 us, 4.6 TB/s, and of 4096 rows of 131072 400 us, 4.6 TB/s, where a large copy reaches
 // 5.2.  (The rows that count dealt out evenly first: no faster.  Exponents by one fused operation in
 // place of two: 1%.)  l is put together in fp64 (a few operations a
-// row): the sums of exponentials are fp32, and what is left of l - reference is a difference of
-// near numbers.
+// row), what is left of l - reference being a difference of near numbers.
 #include <hip/hip_runtime.h>
 
 #include "common.hpp"
@@ -34,17 +33,21 @@
 namespace compact {
 namespace {
 
-__device__ __forceinline__ double log_prob(float xt, float m, float s) {
-  return static_cast<double>(xt) - static_cast<double>(m) - log(static_cast<double>(s));
+__device__ __forceinline__ double log_prob(float xt, float m, double s) {
+  return static_cast<double>(xt) - static_cast<double>(m) - log(s);
 }
 
 // ---------------------------- log-probabilities ------------------------------
-// A workgroup per row: each thread keeps a running maximum and sum over its chunks, four at a time.
+// A workgroup per row: each thread keeps a running maximum and sum over its chunks, four at a time.  The
+// sums of a chunk and of the four are fp32, all longer ones fp64: added one by one in fp32, terms below half a unit
+// in the last place of the sum so far are lost (131072 logits, the target's 0 and all others -17.5: l = -0.00329 was
+// off by 1.3e-5).
 template <bool F32>
 __global__ __launch_bounds__(256) void k_token_fwd(TokenArgs a) {
   using R = Row<F32>;
   constexpr int N = R::kN, U = 4;
   __shared__ float red[4];
+  __shared__ double sums[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t row = blockIdx.x, target = a.target[row];
   const float ninf = -__builtin_inff();
@@ -53,17 +56,18 @@ __global__ __launch_bounds__(256) void k_token_fwd(TokenArgs a) {
     return;
   }
   const R r(row, a.V);
-  float m = ninf, s = 0.0f;
+  float m = ninf;
+  double s = 0.0;
   auto add = [&](float top) {  // a new maximum
     if (top > m) {
-      s *= __builtin_amdgcn_exp2f((m - top) * kLog2e);
+      s *= static_cast<double>(__builtin_amdgcn_exp2f((m - top) * kLog2e));
       m = top;
     }
   };
   if (r.end_of(tid) >= 0) {
     const float x = r.one(a.x, r.end_of(tid));
     add(x);
-    s += __builtin_amdgcn_exp2f((x - (m == ninf ? 0.0f : m)) * kLog2e);
+    s += static_cast<double>(__builtin_amdgcn_exp2f((x - (m == ninf ? 0.0f : m)) * kLog2e));
   }
 #pragma unroll 1
   for (int c = 0; c + tid < r.chunks; c += 256 * U) {
@@ -79,29 +83,33 @@ __global__ __launch_bounds__(256) void k_token_fwd(TokenArgs a) {
     }
     add(top);
     const float shift = m == ninf ? 0.0f : m;
+    float four = 0.0f;
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int u = 0; u < U; ++u) {
+      float one = 0.0f;
 #pragma unroll
-      for (int e = 0; e < N; ++e) s += __builtin_amdgcn_exp2f((R::value(x[u], e) - shift) * kLog2e);
+      for (int e = 0; e < N; ++e) one += __builtin_amdgcn_exp2f((R::value(x[u], e) - shift) * kLog2e);
+      four += one;
+    }
+    s += static_cast<double>(four);
   }
   float top = wave_max(m);
   if (lane == 0) red[wave] = top;
   __syncthreads();
   top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
   const float shift = top == ninf ? 0.0f : top;
-  __syncthreads();
   // (a thread without a logit above -inf has m = -inf; its sum is 0, or NaN)
-  s = wave_sum(s * __builtin_amdgcn_exp2f(((m == ninf ? shift : m) - shift) * kLog2e));
-  if (lane == 0) red[wave] = s;
+  s = wave_sum(s * static_cast<double>(__builtin_amdgcn_exp2f(((m == ninf ? shift : m) - shift) * kLog2e)));
+  if (lane == 0) sums[wave] = s;
   __syncthreads();
   if (tid == 0) {
-    s = (red[0] + red[1]) + (red[2] + red[3]);
+    s = (sums[0] + sums[1]) + (sums[2] + sums[3]);
     const bool in = target >= 0 && target < a.V;
     const double l = in ? log_prob(r.one(a.x, static_cast<uint32_t>(target)), shift, s) : __builtin_nan("");
     a.out[row] = static_cast<float>(a.reference != nullptr ? l - static_cast<double>(a.reference[row]) : l);
     if (a.stats != nullptr) {
       a.stats[2 * row] = shift;
-      a.stats[2 * row + 1] = s;
+      a.stats[2 * row + 1] = static_cast<float>(s);
     }
   }
 }
@@ -328,7 +336,8 @@ template <bool F32, int THREADS, int NC>
 __global__ __launch_bounds__(THREADS, 4) void k_policy(PolicyArgs a) {
   using R = Row<F32>;
   constexpr int N = R::kN, NW = THREADS / 64;
-  __shared__ float smax[NW], ssum[NW];
+  __shared__ float smax[NW];
+  __shared__ double ssum[NW];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const float ninf = -__builtin_inff();
   float scale = 1.0f;
@@ -382,15 +391,17 @@ __global__ __launch_bounds__(THREADS, 4) void k_policy(PolicyArgs a) {
       __syncthreads();
       m = wave_max(smax[lane & (NW - 1)]);
       m = uniform(m == ninf ? 0.0f : m);
-      float s = __builtin_amdgcn_exp2f((xe - m) * kLog2e);
-      walk([&](const u32x4& c) {
+      double s = static_cast<double>(__builtin_amdgcn_exp2f((xe - m) * kLog2e));
+      walk([&](const u32x4& c) {  // (a chunk's sum is fp32, longer ones fp64, as in k_token_fwd)
+        float one = 0.0f;
 #pragma unroll
-        for (int e = 0; e < N; ++e) s += __builtin_amdgcn_exp2f((R::value(c, e) - m) * kLog2e);
+        for (int e = 0; e < N; ++e) one += __builtin_amdgcn_exp2f((R::value(c, e) - m) * kLog2e);
+        s += static_cast<double>(one);
       });
       s = wave_sum(s);
       if (lane == 0) ssum[wave] = s;
       __syncthreads();
-      s = uniform(wave_sum(lane < NW ? ssum[lane & (NW - 1)] : 0.0f));
+      s = wave_sum(lane < NW ? ssum[lane & (NW - 1)] : 0.0);
       const double l = log_prob(xt, m, s);
       const float lo = 1.0f - a.low, hi = 1.0f + a.high, ratio = expf(static_cast<float>(l - static_cast<double>(old)));
       const bool clamped = (A > 0.0f && ratio > hi) || (A < 0.0f && ratio < lo);
@@ -406,7 +417,7 @@ __global__ __launch_bounds__(THREADS, 4) void k_policy(PolicyArgs a) {
         a.logp[row] = static_cast<float>(l);
       }
       g = uniform(g * scale);
-      f = uniform(g == 0.0f ? 0.0f : -g / s);
+      f = uniform(g == 0.0f ? 0.0f : -g / static_cast<float>(s));
     } else if (a.loss_row != nullptr && tid == 0) {
       a.loss_row[row] = 0.0f;
       a.logp[row] = 0.0f;
