@@ -37,6 +37,13 @@ __device__ __forceinline__ double log_prob(float xt, float m, double s) {
   return static_cast<double>(xt) - static_cast<double>(m) - log(s);
 }
 
+// e^t for t <= 0.  (The constant's own rounding makes every term too large, by 1.3e-8 |t|, and with it a
+// sum of differences l - reference over many rows.)
+__device__ __forceinline__ float exp_of(float t) {
+  constexpr float kLow = static_cast<float>(1.44269504088896340736 - static_cast<double>(kLog2e));
+  return __builtin_amdgcn_exp2f(__builtin_fmaf(t, kLog2e, t * kLow));
+}
+
 // ---------------------------- log-probabilities ------------------------------
 // A workgroup per row: each thread keeps a running maximum and sum over its chunks, four at a time.  The
 // sums of a chunk and of the four are fp32, all longer ones fp64: added one by one in fp32, terms below half a unit
@@ -60,14 +67,14 @@ __global__ __launch_bounds__(256) void k_token_fwd(TokenArgs a) {
   double s = 0.0;
   auto add = [&](float top) {  // a new maximum
     if (top > m) {
-      s *= static_cast<double>(__builtin_amdgcn_exp2f((m - top) * kLog2e));
+      s *= static_cast<double>(exp_of(m - top));
       m = top;
     }
   };
   if (r.end_of(tid) >= 0) {
     const float x = r.one(a.x, r.end_of(tid));
     add(x);
-    s += static_cast<double>(__builtin_amdgcn_exp2f((x - (m == ninf ? 0.0f : m)) * kLog2e));
+    s += static_cast<double>(exp_of(x - (m == ninf ? 0.0f : m)));
   }
 #pragma unroll 1
   for (int c = 0; c + tid < r.chunks; c += 256 * U) {
@@ -88,7 +95,7 @@ __global__ __launch_bounds__(256) void k_token_fwd(TokenArgs a) {
     for (int u = 0; u < U; ++u) {
       float one = 0.0f;
 #pragma unroll
-      for (int e = 0; e < N; ++e) one += __builtin_amdgcn_exp2f((R::value(x[u], e) - shift) * kLog2e);
+      for (int e = 0; e < N; ++e) one += exp_of(R::value(x[u], e) - shift);
       four += one;
     }
     s += static_cast<double>(four);
@@ -99,7 +106,7 @@ __global__ __launch_bounds__(256) void k_token_fwd(TokenArgs a) {
   top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
   const float shift = top == ninf ? 0.0f : top;
   // (a thread without a logit above -inf has m = -inf; its sum is 0, or NaN)
-  s = wave_sum(s * static_cast<double>(__builtin_amdgcn_exp2f(((m == ninf ? shift : m) - shift) * kLog2e)));
+  s = wave_sum(s * static_cast<double>(exp_of((m == ninf ? shift : m) - shift)));
   if (lane == 0) sums[wave] = s;
   __syncthreads();
   if (tid == 0) {
