@@ -18,9 +18,9 @@
 // gradient where that needs sums over other rows first (log-probabilities, preference); the policy
 // loss holds a row in registers and forms both.  (Up to 131072 bf16 or 65536 fp32 logits; what a row has
 // past them is read for its maximum, its sum and its gradient.)  Measured, of 32000 bf16 logits, 7 of 10 rows counting:
-// l of 8192 rows 69 us, 5.3 TB/s, the same right after the gradient of others was written 104 us; the
+// l of 8192 rows 70 us, 5.3 TB/s, the same right after the gradient of others was written 105 us; the
 // gradient 150 us, 5.9 TB/s (some of the logits are still in the cache); the policy loss with its
-// gradient 192 us, 4.6 TB/s, and of 4096 rows of 131072 400 us, 4.6 TB/s, where a large copy reaches
+// gradient 192 us, 4.6 TB/s, and of 4096 rows of 131072 380 us, 4.8 TB/s, where a large copy reaches
 // 5.2.  (The rows that count dealt out evenly first: no faster.  Exponents by one fused operation in
 // place of two: 1%.)  l is put together in fp64 (a few operations a
 // row), what is left of l - reference being a difference of near numbers.
